@@ -10,6 +10,8 @@ from ._lib import (EXPORTS, KEY_DTYPE, SCORE_DTYPE, WF_EHIP, WF_EINVAL, WF_ENOME
                    WF_EUNSUPPORTED, WF_SEARCH_RULES, WF_SEARCH_UNIFORM, WF_ST_CAPACITY, WF_ST_INELIGIBLE,
                    WF_ST_REPLICA, Context, WFError, load, wf_plan_argmin_noalloc, wf_plan_validate_window,
                    wf_plan_version)
+from ._lib import KV_EXPORTS
+from .kv import (WF_KV_BF16, WF_KV_F16, KVContext, kv_attend, kv_load, kv_step, kv_store, wf_kv_cache_bytes)
 
 __all__ = [
     "Context", "WFError", "wf_plan_argmin_noalloc", "SCORE_DTYPE", "KEY_DTYPE", "EXPORTS", "load", "wf_plan_validate_window",
@@ -17,6 +19,8 @@ __all__ = [
     "keys_to_numpy",
     "WF_OK", "WF_EINVAL", "WF_ENOWINDOW", "WF_ENOMEM", "WF_EHIP", "WF_EUNSUPPORTED",
     "WF_ST_INELIGIBLE", "WF_ST_CAPACITY", "WF_ST_REPLICA", "WF_SEARCH_UNIFORM", "WF_SEARCH_RULES",
+    "KVContext", "KV_EXPORTS", "WF_KV_BF16", "WF_KV_F16", "kv_step", "kv_store", "kv_load", "kv_attend",
+    "wf_kv_cache_bytes",
 ]
 
 

@@ -49,6 +49,10 @@ EXPORTS = ("wf_plan_ctx_create", "wf_plan_ctx_destroy", "wf_plan_last_error",
            "wf_plan_prefix", "wf_plan_time_bits", "wf_plan_score_kernel",
            "wf_plan_batch_kernel", "wf_plan_version")
 
+# every symbol declared in include/wf_kv.h
+KV_EXPORTS = ("wf_kv_cache_bytes", "wf_kv_ctx_create", "wf_kv_ctx_destroy", "wf_kv_last_error",
+              "wf_kv_step", "wf_kv_store", "wf_kv_load", "wf_kv_attend")
+
 
 class WFError(RuntimeError):
     def __init__(self, status: int, message: str):
@@ -80,6 +84,18 @@ class wf_plan_sched(ctypes.Structure):
     _fields_ = [("start_us", ctypes.c_void_p), ("finish_us", ctypes.c_void_p),
                 ("load_start_us", ctypes.c_void_p), ("peak_mib", ctypes.c_void_p),
                 ("reclaimed_models", ctypes.c_void_p)]
+
+
+class wf_kv_desc(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("block_tokens", ctypes.c_int32), ("n_blocks", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class wf_kv_norm_rope(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_pos", ctypes.c_int32),
+                ("cos_sin", ctypes.c_void_p)]
 
 
 _lib = None
@@ -133,9 +149,23 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.wf_plan_batch_kernel.restype = ctypes.c_char_p
     lib.wf_plan_version.argtypes = []
     lib.wf_plan_version.restype = ctypes.c_char_p
+    f32 = ctypes.c_float
+    lib.wf_kv_cache_bytes.argtypes = [vp, ctypes.POINTER(i64)]
+    lib.wf_kv_ctx_create.argtypes = [i32, vp, ctypes.POINTER(vp)]
+    lib.wf_kv_ctx_destroy.argtypes = [vp]
+    lib.wf_kv_ctx_destroy.restype = None
+    lib.wf_kv_last_error.argtypes = [vp]
+    lib.wf_kv_last_error.restype = ctypes.c_char_p
+    lib.wf_kv_step.argtypes = [vp, vp, i32, i32] + [vp] * 11
+    lib.wf_kv_store.argtypes = [vp, vp, vp, vp, i64, i64, i64, i32] + [vp] * 6
+    lib.wf_kv_load.argtypes = [vp, vp, vp, i32, vp, vp, vp]
+    lib.wf_kv_attend.argtypes = [vp, vp, i64, i32, vp, vp, vp, vp, vp, i32, f32, i32, i32, i32, vp, vp]
+    for name in KV_EXPORTS:
+        if name not in ("wf_kv_ctx_destroy", "wf_kv_last_error"):
+            getattr(lib, name).restype = i32
     # an entry point without a declared signature would take Python ints as
     # 32-bit C ints and cut device addresses short
-    for name in EXPORTS:
+    for name in EXPORTS + KV_EXPORTS:
         if getattr(lib, name).argtypes is None:
             raise RuntimeError(f"{name}: no ctypes signature declared")
     if path is None:

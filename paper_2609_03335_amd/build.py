@@ -13,7 +13,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libwfplan.so"
 LIB_PATH = os.path.join(PKG, LIB_NAME)
 SOURCES = ["host.hip", "score.hip", "score_keys.hip", "argmin.hip", "prefix.hip", "lean.hip",
-           "lanes.hip"]
+           "lanes.hip", "kv_host.hip", "kv_step.hip", "kv_store.hip", "kv_attend.hip"]
 ARCH = "gfx950"
 
 HIP_FLAGS = [

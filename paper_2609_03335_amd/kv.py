@@ -1,0 +1,205 @@
+"""The paged 4-bit key/value cache of a replica: binding of include/wf_kv.h
+(same names) and helpers that allocate the outputs.  Only marshalling: every
+step runs in the gfx950 kernels.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+from typing import Optional
+
+from ._lib import WF_OK, WFError, _buf, _stream, load, wf_kv_desc, wf_kv_norm_rope
+
+WF_KV_BF16, WF_KV_F16 = 0, 1
+_TYPES = {"bf16": WF_KV_BF16, "f16": WF_KV_F16}
+
+
+def _desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, dtype) -> wf_kv_desc:
+    return wf_kv_desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, _TYPES.get(dtype, dtype))
+
+
+def wf_kv_cache_bytes(q_heads: int, kv_heads: int, head_dim: int, block_tokens: int, n_blocks: int,
+                      max_blocks: int = 1, dtype="bf16") -> int:
+    """Bytes of one layer's cache (host only)."""
+    lib, out = load(), ctypes.c_int64()
+    d = _desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, dtype)
+    st = lib.wf_kv_cache_bytes(ctypes.byref(d), ctypes.byref(out))
+    if st != WF_OK:
+        raise WFError(st, lib.wf_kv_last_error(None).decode())
+    return out.value
+
+
+class KVContext:
+    """A wf_kv_ctx on one HIP device: the geometry of a cache.  Tensor
+    arguments are checked before any call reaches the library (GPU tensor, the
+    context's device, enough bytes; the 16-bit ones also for their type)."""
+
+    def __init__(self, device: int = 0, *, q_heads: int, kv_heads: int, head_dim: int, block_tokens: int,
+                 n_blocks: int, max_blocks: int, dtype="bf16"):
+        self.lib = load()
+        self.handle = None
+        d = _desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, dtype)
+        h = ctypes.c_void_p()
+        st = self.lib.wf_kv_ctx_create(device, ctypes.byref(d), ctypes.byref(h))
+        if st != WF_OK:
+            raise WFError(st, self.lib.wf_kv_last_error(None).decode())
+        self.handle = h
+        self.device = device
+        self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
+        self.block_tokens, self.n_blocks, self.max_blocks = block_tokens, n_blocks, max_blocks
+        self.dtype = d.dtype
+        self.cache_bytes = n_blocks * kv_heads * block_tokens * (head_dim + 4)
+
+    def _check(self, st):
+        if st != WF_OK:
+            raise WFError(st, self.lib.wf_kv_last_error(self.handle).decode())
+
+    def _b(self, x, need: int, name: str, size: int = 4) -> Optional[int]:
+        """A buffer of `size`-byte elements."""
+        if hasattr(x, "element_size") and x.element_size() != size:
+            raise TypeError(f"{name}: elements of {x.element_size()} bytes, {size} needed")
+        return _buf(x, max(int(need), 0), self.device, name)
+
+    def _wide(self, x, need: int, name: str) -> Optional[int]:
+        """A buffer of 16-bit floats."""
+        self._type(x, name)
+        return _buf(x, max(int(need), 0), self.device, name)
+
+    def _type(self, x, name: str) -> None:
+        if x is not None and not isinstance(x, int) and x.dtype != torch_type(self.dtype):
+            raise TypeError(f"{name}: {x.dtype}, the context takes {torch_type(self.dtype)}")
+
+    def _tokens(self, x, n: int, heads: int, name: str, stride: Optional[int] = None):
+        """(address, token stride) of n tokens of heads: a tensor [n, heads, D]
+        or [n, heads * D] whose heads are contiguous, or a raw address with
+        its stride (default: dense)."""
+        width = heads * self.head_dim
+        if x is None or isinstance(x, int):
+            return x, width if stride is None else int(stride)
+        if not hasattr(x, "data_ptr"):
+            raise TypeError(f"{name}: expected a torch tensor or a device address")
+        self._type(x, name)
+        if not x.is_cuda:
+            raise ValueError(f"{name}: a host tensor cannot be passed to the GPU library")
+        if x.device.index != self.device:
+            raise ValueError(f"{name}: tensor on cuda:{x.device.index}, context on cuda:{self.device}")
+        shape, st = tuple(x.shape), x.stride()
+        dense = (len(shape) == 3 and shape[1:] == (heads, self.head_dim) and st[2] == 1 and
+                 (st[1] == self.head_dim or heads == 1)) or (len(shape) == 2 and shape[1] == width and st[1] == 1)
+        if not dense or shape[0] < n:
+            raise ValueError(f"{name}: shape {shape} and strides {st}; [{n}, {heads}, {self.head_dim}] with "
+                             "contiguous heads needed")
+        return x.data_ptr(), st[0] if n > 1 else max(st[0], width)
+
+    def wf_kv_step(self, new_tokens, n_rows: int, n_tokens: int, len_in, len_out, pool_in, pool_out, ring, table,
+                   q_off, slot, pos, granted, stream=None) -> None:
+        b, r, t = self._b, max(int(n_rows), 0), max(int(n_tokens), 0)
+        self._check(self.lib.wf_kv_step(
+            self.handle, b(new_tokens, 4 * r, "new_tokens"), int(n_rows), int(n_tokens), b(len_in, 4 * r, "len_in"),
+            b(len_out, 4 * r, "len_out"), b(pool_in, 8, "pool_in"), b(pool_out, 8, "pool_out"),
+            b(ring, 4 * self.n_blocks, "ring"), b(table, 4 * r * self.max_blocks, "table"),
+            b(q_off, 4 * r + 4, "q_off"), b(slot, 8 * t, "slot", 8), b(pos, 4 * t, "pos"), b(granted, r, "granted", 1),
+            _stream(stream)))
+
+    def wf_kv_store(self, q, k, v, n_tokens: int, pos, slot, q_out, cache, *, cos_sin=None, n_pos: int = 0,
+                    rot_dim: int = 0, interleaved: bool = False, q_weight=None, k_weight=None, eps: float = 1e-6,
+                    strides=(None, None, None), stream=None) -> None:
+        n, d = max(int(n_tokens), 0), self.head_dim
+        (qp, qs), (kp, ks), (vp, vs) = (self._tokens(q, n, self.q_heads, "q", strides[0]),
+                                        self._tokens(k, n, self.kv_heads, "k", strides[1]),
+                                        self._tokens(v, n, self.kv_heads, "v", strides[2]))
+        how = wf_kv_norm_rope(self._wide(q_weight, 2 * d, "q_weight"), self._wide(k_weight, 2 * d, "k_weight"), eps,
+                              rot_dim, int(interleaved), n_pos, self._b(cos_sin, 4 * n_pos * rot_dim, "cos_sin"))
+        self._check(self.lib.wf_kv_store(
+            self.handle, qp, kp, vp, qs, ks, vs, int(n_tokens), ctypes.byref(how), self._b(pos, 4 * n, "pos"),
+            self._b(slot, 8 * n, "slot", 8), self._wide(q_out, 2 * n * self.q_heads * d, "q_out"),
+            self._b(cache, self.cache_bytes, "cache", 1), _stream(stream)))
+
+    def wf_kv_load(self, cache, slot, n_tokens: int, k_out, v_out, stream=None) -> None:
+        n = max(int(n_tokens), 0)
+        need = 2 * n * self.kv_heads * self.head_dim
+        self._check(self.lib.wf_kv_load(
+            self.handle, self._b(cache, self.cache_bytes, "cache", 1), self._b(slot, 8 * n, "slot", 8), int(n_tokens),
+            self._wide(k_out, need, "k_out"), self._wide(v_out, need, "v_out"), _stream(stream)))
+
+    def wf_kv_attend(self, q, n_tokens: int, cache, table, kv_len, q_off, pos, n_rows: int, scale: float, out, *,
+                     window: int = 0, max_q: int = 0, max_kv: int = 0, q_stride=None, stream=None) -> None:
+        n, r, b = max(int(n_tokens), 0), max(int(n_rows), 0), self._b
+        qp, qs = self._tokens(q, n, self.q_heads, "q", q_stride)
+        self._check(self.lib.wf_kv_attend(
+            self.handle, qp, qs, int(n_tokens), b(cache, self.cache_bytes, "cache", 1),
+            b(table, 4 * r * self.max_blocks, "table"), b(kv_len, 4 * r, "kv_len"), b(q_off, 4 * r + 4, "q_off"),
+            b(pos, 4 * n, "pos"), int(n_rows), float(scale), int(window), int(max_q), int(max_kv),
+            self._wide(out, 2 * n * self.q_heads * self.head_dim, "out"), _stream(stream)))
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self.lib.wf_kv_ctx_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+@functools.lru_cache(maxsize=None)
+def torch_type(dtype: int):
+    import torch
+    return torch.bfloat16 if dtype == WF_KV_BF16 else torch.float16
+
+
+def kv_step(ctx: KVContext, new_tokens, n_tokens: int, lens, pool, ring, table, stream=None):
+    """Allocate the outputs of wf_kv_step and enqueue it.  table and ring are
+    updated in place; returns (lens, pool, q_off, slot, pos, granted)."""
+    import torch
+    r, kw = new_tokens.shape[0], dict(dtype=torch.int32, device=new_tokens.device)
+    # one allocation for the int32 outputs: lens, pool, q_off, pos
+    flat = torch.empty(r + 2 + r + 1 + n_tokens, **kw)
+    lens_out, pool_out, q_off, pos = flat.split((r, 2, r + 1, n_tokens))
+    slot = torch.empty(n_tokens, dtype=torch.int64, device=flat.device)
+    granted = torch.empty(r, dtype=torch.uint8, device=flat.device)
+    ctx.wf_kv_step(new_tokens, r, n_tokens, lens, lens_out, pool, pool_out, ring, table, q_off, slot, pos, granted,
+                   stream)
+    return lens_out, pool_out, q_off, slot, pos, granted
+
+
+def kv_store(ctx: KVContext, q, k, v, pos, slot, cache, cos_sin=None, *, rot_dim: int = 0, interleaved: bool = False,
+             q_weight=None, k_weight=None, eps: float = 1e-6, stream=None):
+    """Norm, rotate and store the tokens of q [T, q_heads, D], k and v [T,
+    kv_heads, D]; returns the queries [T, q_heads, D]."""
+    import torch
+    n = q.shape[0]
+    out = torch.empty((n, ctx.q_heads, ctx.head_dim), dtype=q.dtype, device=q.device)
+    ctx.wf_kv_store(q, k, v, n, pos, slot, out, cache, cos_sin=cos_sin, n_pos=0 if cos_sin is None else cos_sin.shape[0],
+                    rot_dim=rot_dim, interleaved=interleaved, q_weight=q_weight, k_weight=k_weight, eps=eps,
+                    stream=stream)
+    return out
+
+
+def kv_load(ctx: KVContext, cache, slot, stream=None):
+    """The cached keys and values [T, kv_heads, D] at the given slots."""
+    import torch
+    n = slot.shape[0]
+    k, v = torch.empty((2, n, ctx.kv_heads, ctx.head_dim), dtype=torch_type(ctx.dtype), device=slot.device)
+    ctx.wf_kv_load(cache, slot, n, k, v, stream)
+    return k, v
+
+
+def kv_attend(ctx: KVContext, q, cache, table, kv_len, q_off, pos, *, scale: float, window: int = 0, max_q: int = 0,
+              max_kv: int = 0, stream=None):
+    """Attention of the packed queries q [T, q_heads, D] over the cache:
+    [T, q_heads, D].  Rows of tokens past q_off[-1] are not written."""
+    import torch
+    n = q.shape[0]
+    out = torch.empty((n, ctx.q_heads, ctx.head_dim), dtype=q.dtype, device=q.device)
+    ctx.wf_kv_attend(q, n, cache, table, kv_len, q_off, pos, kv_len.shape[0], scale, out, window=window, max_q=max_q,
+                     max_kv=max_kv, stream=stream)
+    return out

@@ -1,0 +1,511 @@
+"""The paged 4-bit cache on the GPU against the 64-bit oracle of kv_oracle.py:
+block tables and slots, norm + rotation + store, load, attention."""
+import numpy as np
+import pytest
+import torch
+
+import kv_oracle as K
+import paper_2609_03335_amd as pkg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16}
+UNIT = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}      # of rounding to nearest
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    assert torch.cuda.is_available(), "GPU tests need a HIP device"
+
+
+def ctx_of(hq=8, hk=2, d=64, b=16, n=64, width=8, dtype="bf16"):
+    return pkg.KVContext(0, q_heads=hq, kv_heads=hk, head_dim=d, block_tokens=b, n_blocks=n, max_blocks=width, dtype=dtype)
+
+
+def dev(x, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+    return t if dtype is None else t.to(dtype)
+
+
+# ---- block tables and slots --------------------------------------------------------------------
+
+def random_step(rng, rows, b, width, spare, released=0.2, most_new=60):
+    lens = rng.integers(0, width * b + 1, rows) * (rng.random(rows) < 0.8)
+    new = np.where(rng.random(rows) < 0.5, 1, rng.integers(0, most_new, rows))
+    new = np.where(rng.random(rows) < released, -1, new)
+    have = -(-lens // b)
+    need = np.where((new >= 0) & (lens + new <= width * b), -(-(lens + np.maximum(new, 0)) // b) - have, 0)
+    free = max(0, int(need.sum() * spare))
+    n = max(1, int(have.sum()) + free)
+    ids = rng.permutation(n).astype(np.int32)
+    table = np.full((rows, width), -1, np.int32)
+    at = 0
+    for r in range(rows):
+        table[r, :have[r]] = ids[at:at + have[r]]
+        at += have[r]
+    head = int(rng.integers(0, n))
+    ring = np.full(n, -7, np.int32)
+    ring[(head + np.arange(free)) % n] = ids[at:at + free]
+    return lens.astype(np.int32), new.astype(np.int32), table, ring, np.array([head, free], np.int32)
+
+
+def check_step(lens, new, table, ring, pool, b, pad=0, cut=0):
+    tokens = max(0, int(np.maximum(new, 0).sum()) + pad - cut)
+    want = K.step(new, lens, pool, ring, table, b, tokens)
+    with ctx_of(b=b, n=len(ring), width=table.shape[1]) as ctx:
+        t, r = dev(table), dev(ring)
+        args = (ctx, dev(new), tokens, dev(lens), dev(pool), r, t)
+        for _ in range(2):   # the inputs are left as they were: a second call gives the same
+            got = pkg.kv_step(*args)
+        got = dict(zip(("lens", "pool", "q_off", "slot", "pos", "granted"), got), ring=r, table=t)
+        for name, x in want.items():
+            assert np.array_equal(got[name].cpu().numpy(), x), name
+
+
+@pytest.mark.parametrize("b", [16, 32, 256])
+@pytest.mark.parametrize("rows", [1, 2, 63, 64, 65, 1023, 1024, 1025, 2500])
+def test_step(rows, b):
+    rng = np.random.default_rng(rows * 1000 + b)
+    for spare in (1.0, 0.5):
+        check_step(*random_step(rng, rows, b, 6, spare), b, pad=5)
+
+
+def test_step_edges():
+    rng = np.random.default_rng(0)
+    z = np.zeros(0, np.int32)
+    # no rows; no tokens; every row released; none free; more tokens than asked for, and fewer
+    check_step(z, z, np.zeros((0, 4), np.int32), np.arange(9, dtype=np.int32), np.array([3, 6], np.int32), 16, pad=3)
+    check_step(*random_step(rng, 40, 16, 5, 1.0, most_new=1), 16)
+    check_step(*random_step(rng, 40, 16, 5, 1.0, released=1.0), 16)
+    check_step(*random_step(rng, 40, 16, 5, 0.0), 16)
+    check_step(*random_step(rng, 40, 16, 5, 1.0), 16, pad=1000)
+    check_step(*random_step(rng, 40, 16, 5, 1.0), 16, cut=37)
+
+
+def test_step_one_long_prompt():
+    # thousands of blocks for one row, and as many released by another
+    b, width = 16, 8000
+    lens, new = np.array([0, 100000, 5], np.int32), np.array([120000, -1, 1], np.int32)
+    n = 7500 + 6250 + 1
+    ids = np.random.default_rng(3).permutation(n).astype(np.int32)
+    table = np.full((3, width), -1, np.int32)
+    table[1, :6250], table[2, 0] = ids[:6250], ids[6250]
+    ring = np.full(n, -1, np.int32)
+    ring[(n - 10 + np.arange(7500)) % n] = ids[6251:]
+    check_step(lens, new, table, ring, np.array([n - 10, 7500], np.int32), b)
+
+
+def test_step_invalid_device_values_stay_in_bounds():
+    """Lengths, counters and ring contents outside their range: unspecified
+    results, but nothing outside the arrays is written."""
+    rows, b, width, n = 70, 16, 4, 50
+    rng = np.random.default_rng(5)
+    wild = lambda k: rng.integers(-2 ** 31, 2 ** 31 - 1, k).astype(np.int32)
+    with ctx_of(b=b, n=n, width=width) as ctx:
+        for pool in ([-5, 10 ** 9], [10 ** 9, -3], [7, 50]):
+            guard = torch.full((64 + rows * width + 64,), 77, dtype=torch.int32, device=DEV)
+            ring = torch.full((64 + n + 64,), 78, dtype=torch.int32, device=DEV)
+            table = guard[64:-64].view(rows, width)
+            table.copy_(dev(wild(rows * width)).view(rows, width))
+            pkg.kv_step(ctx, dev(wild(rows)), 500, dev(wild(rows)), dev(np.array(pool, np.int32)), ring[64:-64], table)
+            torch.cuda.synchronize()
+            for g, x in ((guard, 77), (ring, 78)):
+                assert (g[:64] == x).all() and (g[-64:] == x).all()
+
+
+# ---- store and load ----------------------------------------------------------------------------
+
+def store_case(rng, hq, hk, d, b, T, dtype, rot, pad=0, scale=1.0):
+    width = (hq + 2 * hk) * d + pad
+    qkv = dev((rng.standard_normal((T, width)) * scale).astype(np.float32), TYPES[dtype])
+    part = lambda a, n: qkv[:, a * d:(a + n) * d].unflatten(-1, (n, d))
+    n = T // b + 3
+    slots = rng.permutation(n * b)[:T].astype(np.int64)
+    n_pos = 977
+    angle = np.arange(n_pos)[:, None] * 1e4 ** (-np.arange(0, max(rot, 2), 2) / max(rot, 2))
+    cs = np.concatenate([np.cos(angle), np.sin(angle)], 1).astype(np.float32)
+    return part(0, hq), part(hq, hk), part(hq + hk, hk), slots, n, rng.integers(0, n_pos, T).astype(np.int32), cs
+
+
+def host(t):
+    return t.float().cpu().numpy()
+
+
+def check_store(hq, hk, d, b, T, dtype, rot, interleaved, norm, seed=0, pad=0, scale=1.0, eps=1e-6):
+    rng = np.random.default_rng(seed)
+    q, k, v, slots, n, pos, cs = store_case(rng, hq, hk, d, b, T, dtype, rot, pad, scale)
+    wq, wk = (dev((1 + 0.2 * rng.standard_normal(d)).astype(np.float32), TYPES[dtype]) for _ in range(2))
+    before = K.Cache(n, hk, b, d, rng)
+    skip = rng.random(T) < 0.1     # tokens without a slot
+    slot = np.where(skip, np.where(rng.random(T) < 0.5, -1, n * b + 3), slots)
+    with ctx_of(hq, hk, d, b, n, 4, dtype) as ctx:
+        cache = dev(before.bytes)
+        out = pkg.kv_store(ctx, q, k, v, dev(pos), dev(slot), cache, dev(cs) if rot else None, rot_dim=rot,
+                           interleaved=interleaved, q_weight=wq if norm else None, k_weight=wk if norm else None, eps=eps)
+        lk, lv = pkg.kv_load(ctx, cache, dev(slot))
+        got = K.Cache(n, hk, b, d)
+        got.bytes = cache.cpu().numpy()
+    u = UNIT[dtype]
+    # queries: 64-bit value, one rounding to 16 bits, and fp32 roundings: the
+    # norm's (D/2 + 8 of its sum's terms at most, halved by the root) and two of the rotation's
+    want = K.normed_rotated(host(q), host(wq) if norm else None, eps, cs, pos, rot, interleaved)
+    size = np.abs(want).max(-1, keepdims=True) * 2 + 1e-30
+    tiny = 2.0 ** -25 if dtype == "f16" else 2.0 ** -134
+    assert (np.abs(host(out) - want) <= u * np.abs(want) + 16 * 2.0 ** -24 * size + tiny).all()
+    # stored: values of the cache
+    live = ~skip
+    gk, gv = got.get(slot[live])
+    code, bits = K.quantised(host(v)[live])
+    assert np.array_equal(gv, K.values(code) * (bits.astype(np.uint32) << 16).view(np.float32).astype(np.float64)[..., None])
+    want = K.normed_rotated(host(k), host(wk) if norm else None, eps, cs, pos, rot, interleaved)[live]
+    s = want.__abs__().max(-1, keepdims=True) / 6
+    # the scale is within a bf16 rounding of largest / 6, and no grid value is nearer:
+    # half the gap around the value (the top may pass 6 by the scale's rounding)
+    a = np.abs(want) / s
+    gap = np.where(a < 2, 0.5, np.where(a < 4, 1.0, 2.0))
+    assert (np.abs(gk - want) <= (gap / 2 + 6 * 2.0 ** -8 + 1e-5) * s).all()
+    _, _, sc = got.parts()
+    sk = (sc[slot[live] // b, :, 0, slot[live] % b].astype(np.uint32) << 16).view(np.float32)
+    assert (np.abs(sk - s[..., 0]) <= (2.0 ** -8 + 1e-5) * s[..., 0]).all()
+    ratio = np.divide(gk, sk[..., None], out=np.zeros_like(gk), where=sk[..., None] != 0)
+    near = np.abs(np.abs(want)[..., None] / sk[..., None, None] - np.array([.25, .75, 1.25, 1.75, 2.5, 3.5, 5])).min(-1)
+    best = K.values(K.quantised_with(want, sk))
+    assert ((ratio == best) | (near < 1e-5)).all()
+    # nothing else in the cache changed
+    blk, off = slots[live] // b, slots[live] % b
+    for x, y, axis in zip(got.parts(), before.parts(), (2, 3, 3)):
+        x, y = (np.moveaxis(z, axis, 1).copy() for z in (x, y))
+        x[blk, off] = y[blk, off] = 0
+        assert np.array_equal(x, y)
+    # load gives the same values, rounded; zeros without a slot
+    for t, w in ((lk, gk), (lv, gv)):
+        t = host(t)
+        assert (t[skip] == 0).all()
+        assert np.array_equal(t[live], host(torch.from_numpy(w).to(TYPES[dtype])))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d", [(4, 2, 64), (5, 1, 128), (2, 2, 256)])
+def test_store(hq, hk, d, dtype):
+    for i, (T, b, rot, inter, norm) in enumerate([(1, 16, d, False, True), (33, 32, d // 2, True, True),
+                                                  (70, 64, 16, False, False), (5, 16, 0, False, True),
+                                                  (129, 128, d, True, False), (40, 256, d // 4, False, True)]):
+        check_store(hq, hk, d, b, T, dtype, rot, inter, norm, seed=i, pad=8 * (i % 3))
+
+
+@pytest.mark.parametrize("T", [16, 48, 200])
+def test_store_runs_of_tokens(T):
+    """Prompts: consecutive slots, from an offset inside a block and across blocks."""
+    hq, hk, d, b = 4, 2, 128, 32
+    rng = np.random.default_rng(T)
+    q, k, v, _, n, pos, cs = store_case(rng, hq, hk, d, b, T, "bf16", d)
+    for first in (0, 5, 16, 31):
+        order = rng.permutation(n + 1)
+        slot = np.array([order[(first + i) // b] * b + (first + i) % b for i in range(T)])
+        want = K.Cache(n + 1, hk, b, d)
+        want.bytes[:] = 170
+        cache = dev(want.bytes)
+        for t in range(T):
+            want.put(slot[t], host(k)[t], host(v)[t])
+        with ctx_of(hq, hk, d, b, n + 1, 4) as ctx:
+            pkg.kv_store(ctx, q, k, v, dev(pos), dev(slot), cache)
+        assert np.array_equal(cache.cpu().numpy(), want.bytes)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_store_extremes(dtype):
+    """Zeros, one large channel, ties, the type's largest and smallest values,
+    infinities and NaN, without norm and rotation: bytes as the oracle's."""
+    d, b = 64, 16
+    big, small = float(torch.finfo(TYPES[dtype]).max), float(torch.finfo(TYPES[dtype]).smallest_normal)
+    x = np.zeros((12, 1, d), np.float32)
+    rng = np.random.default_rng(1)
+    x[1, 0, 7] = 3
+    x[2, 0, :8] = [6, 2.5, 3.5, 5, 0.25, 0.75, -1.75, -1.25]
+    x[3] = rng.choice([big, -big, 0, big / 2], (1, d))
+    x[4] = rng.choice([small, -small, 0, 2 * small], (1, d))
+    x[5] = rng.standard_normal((1, d))
+    x[5, 0, 9] = np.inf
+    x[6, 0, 0] = -np.inf
+    x[7] = rng.standard_normal((1, d))
+    x[7, 0, 63] = np.nan
+    x[8] = -0.0
+    x[9] = rng.standard_normal((1, d)) * 1e-3
+    x[10, 0, ::2] = 1
+    x[11] = rng.integers(-6, 7, (1, d))
+    t = dev(x, TYPES[dtype])
+    slot = np.arange(12) + 3
+    want = K.Cache(2, 1, b, d)
+    with ctx_of(1, 1, d, b, 2, 1, dtype) as ctx:
+        cache = dev(want.bytes)
+        out = pkg.kv_store(ctx, t, t, t, None, dev(slot), cache)
+        k, v = pkg.kv_load(ctx, cache, dev(slot))
+    for i in range(12):
+        want.put(slot[i], host(t)[i], host(t)[i])
+    assert np.array_equal(cache.cpu().numpy(), want.bytes)
+    assert np.array_equal(host(out), host(t), equal_nan=True)
+    for y in (host(k), host(v)):
+        assert np.isnan(y[5:8]).all() and np.isfinite(np.delete(y, [5, 6, 7], 0)).all()
+
+
+# ---- attention ---------------------------------------------------------------------------------
+
+def attend_case(rng, hq, hk, d, b, rows, dtype, extra=2):
+    """rows: (cached, queries, first position or None)."""
+    kv = np.array([r[0] for r in rows])
+    width = max(1, int((-(-kv // b)).max()))
+    n = int((-(-kv // b)).sum()) + extra
+    cache = K.Cache(n, hk, b, d)
+    cache.bytes[..., :b * d] = rng.integers(0, 256, (n, hk, b * d), dtype=np.uint8)
+    s = rng.uniform(0.1, 0.4, (n, hk, 2 * b)).astype(np.float32)
+    cache.bytes[..., b * d:] = K.bf16(s)[1].view(np.uint8).reshape(n, hk, 4 * b)
+    ids, at = rng.permutation(n).astype(np.int32), 0
+    table = np.full((len(rows), width), -1, np.int32)
+    q_off, pos = [0], []
+    for r, (m, nq, first) in enumerate(rows):
+        blocks = -(-m // b)
+        table[r, :blocks] = ids[at:at + blocks]
+        at += blocks
+        q_off.append(q_off[-1] + nq)
+        first = m - nq if first is None else first
+        pos += list(range(first, first + nq))
+    q = rng.standard_normal((q_off[-1], hq, d)).astype(np.float32)
+    return (dev(q, TYPES[dtype]), cache, table, kv.astype(np.int32), np.array(q_off, np.int32), np.array(pos, np.int32))
+
+
+def bound(dtype, want, mag, dots, d, n):
+    """|error| of an output: its rounding, the rounding of p * scale (relative u,
+    or half the type's smallest step), fp32 products and sums (n terms and the
+    exponentials'), and the error of the scores, which multiplies p by at most 1 + 2 delta."""
+    u = UNIT[dtype]
+    tiny = 6 * n * 2.0 ** -25 if dtype == "f16" else 0.0
+    delta = (d + 16) * 2.0 ** -24 * dots[..., None]
+    return u * np.abs(want) + (u * 1.01 + 2.2 * delta + (n + 64) * 2.0 ** -23) * mag + tiny + 2.0 ** -25
+
+
+def check_attend(hq, hk, d, b, rows, dtype="bf16", window=0, seed=0, scale=None, hints=True, pad=0):
+    rng = np.random.default_rng(seed)
+    q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, rows, dtype)
+    scale = d ** -0.5 if scale is None else scale
+    want, mag, dots = K.attend(host(q), cache, table, kv, q_off, pos, scale, window)
+    if pad:   # queries inside a wider buffer
+        wide = torch.zeros(len(q), hq * d + pad, dtype=q.dtype, device=DEV)
+        wide[:, :hq * d] = q.flatten(1)
+        q = wide[:, :hq * d].unflatten(-1, (hq, d))
+    nq = max(1, int(np.diff(q_off).max()))
+    with ctx_of(hq, hk, d, b, cache.n, table.shape[1], dtype) as ctx:
+        args = (ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos))
+        every = [(nq, int(kv.max())), (0, 0), (1, 1)] if hints else [(nq, int(kv.max()))]
+        for max_q, max_kv in every:
+            got = host(pkg.kv_attend(*args, scale=scale, window=window, max_q=max_q, max_kv=max_kv))
+            err = np.abs(got - want)
+            lim = bound(dtype, want, mag, dots, d, max(1, int(kv.max())))
+            assert np.isfinite(got).all()
+            assert (err <= lim).all(), (float((err / lim).max()), np.argwhere(err > lim)[:4], max_q, max_kv)
+            empty = mag.sum(-1) == 0
+            assert (got[empty] == 0).all()
+
+
+HEADS = [(1, 1, 64), (8, 2, 64), (14, 2, 64), (4, 4, 128), (8, 1, 128), (10, 2, 128), (17, 1, 128), (33, 1, 64), (4, 2, 256)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d", HEADS)
+def test_attend_single_tokens(hq, hk, d, dtype):
+    rows = [(n, 1, None) for n in (1, 2, 15, 16, 17, 63, 64, 65, 130, 257, 0)]
+    check_attend(hq, hk, d, 16, rows, dtype, seed=d)
+
+
+@pytest.mark.parametrize("b", [16, 32, 64, 128, 256])
+def test_attend_blocks(b):
+    check_attend(8, 2, 128, b, [(n, 1, None) for n in (1, b - 1, b, b + 1, 3 * b + 7, 700)], seed=b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d", [(8, 2, 64), (5, 1, 128), (2, 2, 256), (17, 1, 64)])
+def test_attend_prompts(hq, hk, d, dtype):
+    check_attend(hq, hk, d, 32, [(70, 70, None), (200, 33, None), (1, 1, None), (129, 2, None), (64, 64, None)], dtype, seed=d)
+
+
+@pytest.mark.parametrize("window", [1, 2, 16, 63, 64, 100, 5000])
+def test_attend_window(window):
+    check_attend(8, 2, 64, 16, [(300, 1, None), (150, 90, None), (40, 40, None), (1, 1, None)], window=window, seed=window)
+
+
+def test_attend_empty_rows():
+    """Rows without cached tokens (refused), positions before the first token and
+    past the last, rows without queries."""
+    check_attend(8, 2, 128, 16, [(0, 3, 0), (5, 9, -4), (50, 0, None), (20, 4, 18), (0, 0, 0), (33, 5, 60), (7, 1, -1)],
+                 window=0, seed=1)
+    check_attend(8, 2, 128, 16, [(20, 6, 18), (33, 5, 60), (40, 3, -1)], window=4, seed=2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_attend_longer(dtype):
+    check_attend(8, 2, 128, 64, [(5000, 1, None), (1100, 1, None), (3, 1, None)], dtype, seed=7)
+    check_attend(4, 1, 64, 16, [(2100, 17, None), (900, 1, None)], dtype, seed=8)
+
+
+def test_attend_large_scores():
+    # one token takes nearly all the weight; negative and zero scales
+    for scale in (4.0, -1.0, 0.0):
+        check_attend(8, 2, 64, 16, [(500, 1, None), (60, 20, None)], scale=scale, seed=3)
+
+
+def test_attend_strided_queries():
+    check_attend(8, 2, 64, 16, [(90, 1, None), (60, 5, None)], pad=24, seed=4, hints=False)
+
+
+def test_attend_many_rows():
+    rng = np.random.default_rng(9)
+    check_attend(4, 2, 64, 16, [(int(n), 1, None) for n in rng.integers(0, 90, 300)], seed=9)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_attend_masked_garbage_does_not_leak(dtype):
+    """NaN and infinite scales past a row's end, before its window, and in blocks of
+    no row; ids of unused table entries out of range."""
+    hq, hk, d, b, window = 8, 2, 64, 16, 50
+    rng = np.random.default_rng(11)
+    rows = [(37, 1, None), (100, 1, None), (90, 13, None), (0, 1, 0)]
+    q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, rows, dtype)
+    want, mag, dots = K.attend(host(q), cache, table, kv, q_off, pos, d ** -0.5, window)
+    raw = cache.bytes[..., b * d:].copy().view(np.uint16).reshape(cache.n, hk, 2, b)
+    seen = np.zeros((cache.n, b), bool)
+    for r, (n, nq, _) in enumerate(rows):
+        for j in range(max(0, n - nq - window + 1), n):
+            seen[table[r, j // b], j % b] = True
+    bad = rng.choice(np.array([0x7fc0, 0x7f80, 0xff80, 0x7f7f], np.uint16), raw.shape)
+    raw = np.where(seen[:, None, None, :], raw, bad)
+    cache.bytes[..., b * d:] = np.ascontiguousarray(raw).view(np.uint8).reshape(cache.n, hk, 4 * b)
+    table = np.where(table < 0, rng.choice(np.array([-1, 2 ** 31 - 1, -2 ** 31, cache.n], np.int32), table.shape), table).astype(np.int32)
+    with ctx_of(hq, hk, d, b, cache.n, table.shape[1], dtype) as ctx:
+        got = host(pkg.kv_attend(ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos), scale=d ** -0.5, window=window))
+    assert (np.abs(got - want) <= bound(dtype, want, mag, dots, d, 100)).all()
+
+
+def test_attend_nan_in_sight_shows():
+    """A stored NaN reaches the queries that see it, and no others."""
+    hq, hk, d, b = 4, 2, 64, 16
+    rng = np.random.default_rng(12)
+    q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, [(40, 40, None)], "bf16")
+    cell = cache.bytes[table[0, 1], 1]                 # token 20 of kv head 1: its key
+    cell[b * d:].view(np.uint16)[4] = 0x7fc0
+    with ctx_of(hq, hk, d, b, cache.n, table.shape[1]) as ctx:
+        got = host(pkg.kv_attend(ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos), scale=0.125))
+    assert np.isnan(got[20:, 2:]).all()
+    assert np.isfinite(got[:20]).all() and np.isfinite(got[:, :2]).all()
+
+
+def test_attend_cache_past_32_bits():
+    """Blocks whose bytes lie past 2^32: the first and the last block of a 5 GiB cache."""
+    hq, hk, d, b = 8, 8, 128, 64
+    n = (5 << 30) // (hk * b * (d + 4)) + 1
+    rng = np.random.default_rng(13)
+    q, small, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, [(100, 1, None)], "bf16", extra=0)
+    want, mag, dots = K.attend(host(q), small, table, kv, q_off, pos, d ** -0.5, 0)
+    with ctx_of(hq, hk, d, b, n, 2) as ctx:
+        cache = torch.zeros(ctx.cache_bytes, dtype=torch.uint8, device=DEV).view(n, hk, -1)
+        cache[n - 1], cache[0] = dev(small.bytes[table[0, 0]]), dev(small.bytes[table[0, 1]])
+        far = dev(np.array([[n - 1, 0]], np.int32))
+        got = host(pkg.kv_attend(ctx, q, cache, far, dev(kv), dev(q_off), dev(pos), scale=d ** -0.5))
+        assert (np.abs(got - want) <= bound("bf16", want, mag, dots, d, 100)).all()
+        # stored and read back there
+        x = dev(rng.standard_normal((2, hk, d)).astype(np.float32), torch.bfloat16)
+        slot = dev(np.array([n * b - 1, (n - 1) * b + 3]))
+        pkg.kv_store(ctx, x, x, x, None, slot, cache)
+        k, v = pkg.kv_load(ctx, cache, slot)
+        for t in (k, v):
+            code, bits = K.quantised(host(x))
+            w = K.values(code) * (bits.astype(np.uint32) << 16).view(np.float32)[..., None]
+            assert np.array_equal(host(t), host(torch.from_numpy(w).to(torch.bfloat16)))
+
+
+# ---- calls -------------------------------------------------------------------------------------
+
+def test_streams_and_replays():
+    """On a stream of its own and replayed from a graph: the eager results."""
+    rng = np.random.default_rng(21)
+    hq, hk, d, b = 8, 2, 128, 16
+    q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, [(900, 1, None), (70, 1, None), (333, 5, None)], "bf16")
+    with ctx_of(hq, hk, d, b, cache.n, table.shape[1]) as ctx:
+        c, tb, ln, qo, ps = dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos)
+        run = lambda x, **kw: pkg.kv_attend(ctx, x, c, tb, ln, qo, ps, scale=d ** -0.5, max_q=5, max_kv=900, **kw)
+        q2 = torch.roll(q, 1, 0)
+        eager = [run(x).clone() for x in (q, q2)]
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            side = run(q)
+        side2 = run(q, stream=s)
+        torch.cuda.synchronize()
+        assert torch.equal(side, eager[0]) and torch.equal(side2, eager[0])
+        x, out = q.clone(), torch.empty_like(q)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ctx.wf_kv_attend(x, len(x), c, tb, ln, qo, ps, 3, d ** -0.5, out, max_q=5, max_kv=900)
+        for k in range(6):
+            x.copy_((q, q2)[k % 2])
+            run(q2 if k % 2 == 0 else q)              # eager work of the same context between
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, eager[k % 2]), k
+
+
+def test_refusals():
+    hq, hk, d, b = 4, 2, 64, 16
+    with ctx_of(hq, hk, d, b, 8, 4) as ctx:
+        x = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt, device=DEV)
+        i32, i64 = torch.int32, torch.int64
+        cache, q, k, slot, pos = x(ctx.cache_bytes, dt=torch.uint8), x(3, hq, d), x(3, hk, d), x(3, dt=i64), x(3, dt=i32)
+        store = lambda **kw: ctx.wf_kv_store(**{**dict(q=q, k=k, v=k, n_tokens=3, pos=pos, slot=slot, q_out=x(3, hq, d), cache=cache), **kw})
+        store()
+        for bad in (dict(q=q.cpu()), dict(q=x(2, hq, d)), dict(q=x(3, hq, d, dt=torch.float16)), dict(q=x(3, hk, d)),
+                    dict(k=x(3, hk, 2 * d)[..., ::2]), dict(v=k.transpose(1, 2)), dict(slot=x(2, dt=i64)),
+                    dict(slot=x(3, dt=i32)), dict(cache=cache[:-1]), dict(q_out=x(2, hq, d)), dict(pos=x(3, dt=i64)),
+                    dict(q_weight=x(d - 1)), dict(cos_sin=x(4, 16, dt=torch.float32), n_pos=5, rot_dim=16)):
+            with pytest.raises((ValueError, TypeError)):
+                store(**bad)
+        cs = x(4, 64, dt=torch.float32)
+        for bad in (dict(n_tokens=-1), dict(rot_dim=8, cos_sin=cs, n_pos=4), dict(rot_dim=80, cos_sin=cs, n_pos=1),
+                    dict(rot_dim=16), dict(rot_dim=16, cos_sin=cs, n_pos=0), dict(rot_dim=16, cos_sin=cs, n_pos=4, pos=None),
+                    dict(eps=-1.0), dict(eps=float("nan")), dict(slot=None), dict(q=None), dict(cache=None),
+                    dict(q=x(4 * 3 * hq * d)[4:][:3 * hq * d].view(3, hq, d)),           # 8 bytes off
+                    dict(k=x(3, hk * d + 4)[:, :hk * d].unflatten(-1, (hk, d)))):         # stride not a multiple of 8
+            with pytest.raises(pkg.WFError) as e:
+                store(**bad)
+            assert e.value.status == pkg.WF_EINVAL and e.value.message
+        table, lens, off = x(2, 4, dt=i32), x(2, dt=i32), x(3, dt=i32)
+        att = lambda **kw: ctx.wf_kv_attend(**{**dict(q=q, n_tokens=3, cache=cache, table=table, kv_len=lens, q_off=off, pos=pos,
+                                                      n_rows=2, scale=1.0, out=x(3, hq, d)), **kw})
+        att()
+        for bad in (dict(table=x(2, 3, dt=i32)), dict(kv_len=x(1, dt=i32)), dict(q_off=x(2, dt=i32)), dict(out=x(3, hk, d)),
+                    dict(q=q.float()), dict(pos=pos.long()), dict(table=table.cpu())):
+            with pytest.raises((ValueError, TypeError)):
+                att(**bad)
+        for bad in (dict(n_rows=-1), dict(n_tokens=-2), dict(window=-1), dict(max_q=-1), dict(max_kv=-1), dict(table=None),
+                    dict(scale=float("inf")), dict(scale=float("nan")), dict(out=None)):
+            with pytest.raises(pkg.WFError) as e:
+                att(**bad)
+            assert e.value.status == pkg.WF_EINVAL
+        att(n_tokens=0)
+        att(n_rows=0)
+        new, pool, pool2, ring = x(2, dt=i32), x(2, dt=i32), x(2, dt=i32), x(8, dt=i32)
+        stp = lambda **kw: ctx.wf_kv_step(**{**dict(new_tokens=new, n_rows=2, n_tokens=3, len_in=lens, len_out=x(2, dt=i32), pool_in=pool,
+                                                    pool_out=pool2, ring=ring, table=table, q_off=off, slot=slot, pos=pos,
+                                                    granted=x(2, dt=torch.uint8)), **kw})
+        stp()
+        for bad in (dict(ring=x(7, dt=i32)), dict(q_off=x(2, dt=i32)), dict(slot=x(2, dt=i64)), dict(new_tokens=new.long())):
+            with pytest.raises((ValueError, TypeError)):
+                stp(**bad)
+        for bad in (dict(n_rows=-1), dict(n_tokens=-1), dict(n_rows=1 << 17, new_tokens=0, len_in=0, len_out=0, table=0, granted=0, q_off=0),
+                    dict(len_out=lens), dict(pool_out=pool), dict(new_tokens=None), dict(slot=None)):
+            with pytest.raises(pkg.WFError) as e:
+                stp(**bad)
+            assert e.value.status == pkg.WF_EINVAL
+        with pytest.raises(pkg.WFError):
+            ctx.wf_kv_load(cache, slot, -1, k, k)
+        with pytest.raises(pkg.WFError):
+            ctx.wf_kv_load(cache, None, 3, k, k)
+        torch.cuda.synchronize()
