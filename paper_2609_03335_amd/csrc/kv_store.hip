@@ -32,6 +32,15 @@ __device__ __forceinline__ uint4 pack(const float* x) {
   return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
+// 1 / sqrt(x) rounded to nearest: the instruction is within an ulp, one Newton
+// step with the products' rounding errors carried along gives the rest.
+__device__ __forceinline__ float inv_sqrt(float x) {
+  const float r = rsqrtf(x), t = x * r;
+  const float e = fmaf(-t, r, 1.0f) - fmaf(x, r, -t) * r;
+  const float y = fmaf(0.5f * r, e, r);
+  return fabsf(y) <= 3.4e38f ? y : r;  // x = 0 or infinite
+}
+
 // x * rsqrt(mean(x^2) + eps) * w over a vector of L lanes.
 template <int L, class T>
 __device__ __forceinline__ void norm(float* x, const void* weight, int lane, float eps) {
@@ -41,7 +50,7 @@ __device__ __forceinline__ void norm(float* x, const void* weight, int lane, flo
   float t = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
 #pragma unroll
   for (int off = 1; off < L; off <<= 1) t += __shfl_xor(t, off, 64);
-  const float r = rsqrtf(t * (1.0f / (8 * L)) + eps);
+  const float r = inv_sqrt(t * (1.0f / (8 * L)) + eps);
   float w[8];
   unpack<T>(reinterpret_cast<const uint4*>(weight)[lane], w);
 #pragma unroll
