@@ -30,6 +30,15 @@ HIP_FLAGS = [
 ]
 
 
+def flags(src: str) -> list:
+    """Compiler flags of a source.  The cache kernels (kv_*) take the default
+    schedule: the compiler fails on attention with the other."""
+    if not src.startswith("kv_"):
+        return HIP_FLAGS
+    return [f for f in HIP_FLAGS if "sched-strategy" not in f and f != "-mllvm"]
+
+
+
 def hipcc() -> str:
     for c in (os.environ.get("HIPCC"), "/opt/rocm/bin/hipcc", shutil.which("hipcc")):
         if c and os.path.exists(c):
@@ -46,7 +55,7 @@ def build(verbose: bool = False) -> str:
     procs = []
     for src in SOURCES:
         obj = os.path.join(build_dir, src.replace(".hip", ".o"))
-        cmd = [hipcc(), *HIP_FLAGS, "-I", INCLUDE, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc(), *flags(src), "-I", INCLUDE, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), file=sys.stderr)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "wf_kv.h"
 
 namespace wfkv {
@@ -63,10 +65,21 @@ struct AttendArgs {
   void* out;
 };
 
+// The work area of launch_attend: partial sums, and for each query's head the
+// number of shares that wrote them.
+constexpr size_t kPartBytes = size_t(32) << 20, kUsedBytes = size_t(1) << 20;
+struct AttendWork {
+  int n_cu;
+  float* part;
+  size_t part_bytes;
+  int32_t* used;
+  size_t used_bytes;
+};
+
 hipError_t launch_step(const Geo& g, const StepArgs& a, hipStream_t s);
 hipError_t launch_store(const Geo& g, int dtype, const StoreArgs& a, hipStream_t s);
 hipError_t launch_load(const Geo& g, int dtype, const LoadArgs& a, hipStream_t s);
-hipError_t launch_attend(const Geo& g, int dtype, const AttendArgs& a, hipStream_t s);
+hipError_t launch_attend(const Geo& g, int dtype, const AttendArgs& a, const AttendWork& w, hipStream_t s);
 
 // A 16-bit type of the queries and values: to and from fp32 (nearest even).
 struct Bf16 {

@@ -11,6 +11,7 @@ struct wf_kv_ctx {
   int device = 0;
   int dtype = 0;
   wfkv::Geo g{};
+  wfkv::AttendWork work{};
   char err[256] = "";
 };
 
@@ -112,11 +113,31 @@ wf_status wf_kv_ctx_create(int hip_device, const wf_kv_desc* desc, wf_kv_ctx** o
   g.n_blocks = desc->n_blocks;
   g.width = desc->max_blocks;
   g.cell = (int)cell_bytes(desc);
+  wf_status made = launch(ctx, "wf_kv_ctx_create", [&] {
+    hipError_t e = hipDeviceGetAttribute(&ctx->work.n_cu, hipDeviceAttributeMultiprocessorCount, hip_device);
+    if (e == hipSuccess) e = hipMalloc(&ctx->work.part, wfkv::kPartBytes + wfkv::kUsedBytes);
+    return e;
+  });
+  if (made != WF_OK) {
+    const wf_status st = fail(nullptr, made, "%s", ctx->err);
+    delete ctx;
+    return st;
+  }
+  ctx->work.part_bytes = wfkv::kPartBytes;
+  ctx->work.used = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(ctx->work.part) + wfkv::kPartBytes);
+  ctx->work.used_bytes = wfkv::kUsedBytes;
   *out = ctx;
   return WF_OK;
 }
 
-void wf_kv_ctx_destroy(wf_kv_ctx* ctx) { delete ctx; }
+void wf_kv_ctx_destroy(wf_kv_ctx* ctx) {
+  if (!ctx) return;
+  {
+    OnDevice on(ctx->device);
+    (void)hipFree(ctx->work.part);
+  }
+  delete ctx;
+}
 
 const char* wf_kv_last_error(const wf_kv_ctx* ctx) { return ctx ? ctx->err : g_kv_err; }
 
@@ -202,7 +223,7 @@ wf_status wf_kv_attend(wf_kv_ctx* ctx, const void* q, int64_t q_stride, int32_t 
     return fail(ctx, WF_EINVAL, "q, out and cache must be aligned to 16 bytes");
   const wfkv::AttendArgs a{q, q_stride, n_tokens, cache, table, kv_len, q_off, pos, n_rows, scale,
                            window, max_q, max_kv, out};
-  return launch(ctx, "wf_kv_attend", [&] { return wfkv::launch_attend(g, ctx->dtype, a, (hipStream_t)hip_stream); });
+  return launch(ctx, "wf_kv_attend", [&] { return wfkv::launch_attend(g, ctx->dtype, a, ctx->work, (hipStream_t)hip_stream); });
 }
 
 }  // extern "C"
