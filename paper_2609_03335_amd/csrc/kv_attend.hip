@@ -86,6 +86,10 @@ __device__ __forceinline__ float column_sum(float x) {
   return x + __shfl_xor(x, 32, 64);
 }
 
+// Waves a SIMD that the registers are held to.
+template <int D, int C>
+constexpr int kOcc = D * C <= 64 ? 4 : D * C <= 128 ? 3 : D * C <= 256 ? 2 : 1;
+
 struct Split {
   int tiles, splits;  // of the launch: column tiles of a row, shares of its tokens
   float* part;        // [splits][n_tokens][hq][D + 2] sums, maximum, total
@@ -93,7 +97,7 @@ struct Split {
 };
 
 template <int D, int C, class M>
-__global__ __launch_bounds__(kThreads) void attend(Geo g, AttendArgs a, Split sp) {
+__global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendArgs a, Split sp) {
   constexpr int KS = D / 32;          // products of 32 channels per score tile
   constexpr int RB = D / 32;          // blocks of 16 rows of value codes
   constexpr int MT = D / 16;          // blocks of 16 channels of the output
@@ -206,91 +210,77 @@ __global__ __launch_bounds__(kThreads) void attend(Geo g, AttendArgs a, Split sp
       for (int r = 0; r < RB; ++r)
         vw[r] = *reinterpret_cast<const u32x4*>(vcell + g.b * (D / 2) + (r * 16 + n) * g.b + voff);
 
-      // scores of the 16 tokens of this lane's group
-      f32x4 s[C][4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) s[c][t] = (f32x4){0, 0, 0, 0};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const u32x4 kk = operand<M>(kw[t][k]);
-#pragma unroll
-          for (int c = 0; c < C; ++c) s[c][t] = M::mma(kk, q[c][k], s[c][t]);
-        }
-      }
       const bool whole = base >= lo_max && base + 64 <= hi_min;
-      float most[C];
-      bool up = false;
+      // 32 tokens at a time: score tiles 2h and 2h + 1, one product with the values
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
+      for (int h = 0; h < 2; ++h) {
+        f32x4 s[C][2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const uint32_t w0 = t < 2 ? ks0[2 * t] : ks1[2 * t - 4], w1 = t < 2 ? ks0[2 * t + 1] : ks1[2 * t - 3];
-          s[c][t][0] *= bf_lo(w0) * scale;
-          s[c][t][1] *= bf_hi(w0) * scale;
-          s[c][t][2] *= bf_lo(w1) * scale;
-          s[c][t][3] *= bf_hi(w1) * scale;
-        }
-        if (!whole) {
+        for (int e = 0; e < 2; ++e) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
+          for (int c = 0; c < C; ++c) s[c][e] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int j = base + grp * 16 + t * 4 + i;
-              s[c][t][i] = j >= lo[c] && j < hi[c] ? s[c][t][i] : -INFINITY;
-            }
-        }
-        float m = s[c][0][0];
+          for (int k = 0; k < KS; ++k) {
+            const u32x4 kk = operand<M>(kw[2 * h + e][k]);
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) m = fmaxf(m, s[c][t][i]);
-        most[c] = m;
-        up |= m > top[c] + M::kSlack;
-      }
-      // the running maximum moves only when a score passes it by the slack
-      if (__any(up)) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const float m = fmaxf(top[c], column_max(most[c]));
-          const float r = m == -INFINITY ? 0.0f : m;
-          const float keep = __builtin_amdgcn_exp2f(top[c] - r);
-          top[c] = m;
-          ref[c] = r;
-          sum[c] *= keep;
-#pragma unroll
-          for (int k = 0; k < MT; ++k) o[c][k] *= keep;
-        }
-      }
-      // probabilities times value scales, in the order of the value operand: element
-      // 2b + e of product h is token (2h + e)*4 + b of the group
-      u32x4 p[C][2];
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float x[4][4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const uint32_t w0 = t < 2 ? vs0[2 * t] : vs1[2 * t - 4], w1 = t < 2 ? vs0[2 * t + 1] : vs1[2 * t - 3];
-          const float z[4] = {bf_lo(w0), bf_hi(w0), bf_lo(w1), bf_hi(w1)};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = __builtin_amdgcn_exp2f(s[c][t][i] - ref[c]);
-            sum[c] += e;
-            x[t][i] = e * z[i];
-            if (!whole) {
-              const int j = base + grp * 16 + t * 4 + i;  // a hidden token's scale may be anything
-              x[t][i] = j >= lo[c] && j < hi[c] ? x[t][i] : 0.0f;
-            }
+            for (int c = 0; c < C; ++c) s[c][e] = M::mma(kk, q[c][k], s[c][e]);
           }
         }
+        const u32x4 ks = h ? ks1 : ks0, vs = h ? vs1 : vs0;
+        float kz[8], vz[8];  // of tokens e*4 + i
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int w = 0; w < 4; ++w) {
+          kz[2 * w] = bf_lo(ks[w]) * scale, kz[2 * w + 1] = bf_hi(ks[w]) * scale;
+          vz[2 * w] = bf_lo(vs[w]), vz[2 * w + 1] = bf_hi(vs[w]);
+        }
+        const int j0 = base + grp * 16 + h * 8;
+        float most[C];
+        bool up = false;
 #pragma unroll
-          for (int b = 0; b < 4; ++b) p[c][h][b] = M::pair(x[2 * h][b], x[2 * h + 1][b]);
-      }
+        for (int c = 0; c < C; ++c) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+          for (int i = 0; i < 8; ++i) s[c][i / 4][i % 4] *= kz[i];
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[c][i / 4][i % 4] = j0 + i >= lo[c] && j0 + i < hi[c] ? s[c][i / 4][i % 4] : -INFINITY;
+          }
+          float m = s[c][0][0];
+#pragma unroll
+          for (int i = 1; i < 8; ++i) m = fmaxf(m, s[c][i / 4][i % 4]);
+          most[c] = m;
+          up |= m > top[c] + M::kSlack;
+        }
+        // the running maximum moves only when a score passes it by the slack
+        if (__any(up)) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const float m = fmaxf(top[c], column_max(most[c]));
+            const float r = m == -INFINITY ? 0.0f : m;
+            const float keep = __builtin_amdgcn_exp2f(top[c] - r);
+            top[c] = m;
+            ref[c] = r;
+            sum[c] *= keep;
+#pragma unroll
+            for (int k = 0; k < MT; ++k) o[c][k] *= keep;
+          }
+        }
+        // probabilities times value scales, in the order of the value operand:
+        // element 2b + e is token e*4 + b
+        u32x4 p[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float e = __builtin_amdgcn_exp2f(s[c][i / 4][i % 4] - ref[c]);
+            sum[c] += e;
+            x[i] = e * vz[i];
+            // a hidden token's scale may be anything
+            if (!whole) x[i] = j0 + i >= lo[c] && j0 + i < hi[c] ? x[i] : 0.0f;
+          }
+#pragma unroll
+          for (int b = 0; b < 4; ++b) p[c][b] = M::pair(x[b], x[4 + b]);
+        }
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
           // bytes of four tokens of score tiles 2h and 2h + 1: low nibbles are
@@ -300,10 +290,11 @@ __global__ __launch_bounds__(kThreads) void attend(Geo g, AttendArgs a, Split sp
           const u32x4 vhi = operand<M>((w0 >> 4 & mask) | (w1 & ~mask));
 #pragma unroll
           for (int c = 0; c < C; ++c) {
-            o[c][r] = M::mma(vlo, p[c][h], o[c][r]);
-            o[c][r + RB] = M::mma(vhi, p[c][h], o[c][r + RB]);
+            o[c][r] = M::mma(vlo, p[c], o[c][r]);
+            o[c][r + RB] = M::mma(vhi, p[c], o[c][r + RB]);
           }
         }
+      }
     }
 
     // join the waves
@@ -365,32 +356,47 @@ __global__ __launch_bounds__(kThreads) void attend(Geo g, AttendArgs a, Split sp
   }
 }
 
-// The shares of each query's head joined in order, four channels a thread.
+// The shares of one query's head, joined in a fixed order: four channels a thread,
+// every kParts-th share a group of threads, then the groups.
 template <int D, class M>
 __global__ __launch_bounds__(kThreads) void combine(Geo g, AttendArgs a, Split sp) {
-  const int64_t x = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t head = x / (D / 4), heads = (int64_t)a.n_tokens * g.hq;
-  if (head >= heads) return;
+  constexpr int kParts = kThreads / (D / 4);
+  __shared__ float tops[kWaves], totals[kParts];
+  __shared__ __attribute__((aligned(16))) f32x4 sums[kParts][D / 4];
+  const int64_t head = blockIdx.x, heads = (int64_t)a.n_tokens * g.hq;
   const int64_t t = head / g.hq;
   if (t < a.q_off[0] || t >= a.q_off[a.n_rows]) return;
   const int used = sp.used[head];
   if (used <= 1) return;
-  const int ch = (int)(x % (D / 4)) * 4;
+  const int ch = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
+  const float* from = sp.part + head * (D + 2);
+  const int64_t step = heads * (D + 2);
   float m = -INFINITY;
-  for (int s = 0; s < used; ++s) m = fmaxf(m, sp.part[(s * heads + head) * (D + 2) + D]);
+  for (int s = threadIdx.x; s < used; s += kThreads) m = fmaxf(m, from[s * step + D]);
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = m;
+  __syncthreads();
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, tops[w]);
   const float r = m == -INFINITY ? 0.0f : m;
   float total = 0.0f;
   f32x4 v = {0, 0, 0, 0};
-  for (int s = 0; s < used; ++s) {
-    const float* from = sp.part + (s * heads + head) * (D + 2);
-    const float keep = __builtin_amdgcn_exp2f(from[D] - r);
-    total += from[D + 1] * keep;
-    const f32x2 v0 = *reinterpret_cast<const f32x2*>(from + ch), v1 = *reinterpret_cast<const f32x2*>(from + ch + 2);
+#pragma unroll 4
+  for (int s = part; s < used; s += kParts) {
+    const float* at = from + s * step;
+    const float keep = __builtin_amdgcn_exp2f(at[D] - r);
+    total += at[D + 1] * keep;
+    const f32x2 v0 = *reinterpret_cast<const f32x2*>(at + 4 * ch), v1 = *reinterpret_cast<const f32x2*>(at + 4 * ch + 2);
     v[0] += v0[0] * keep, v[1] += v0[1] * keep, v[2] += v1[0] * keep, v[3] += v1[1] * keep;
   }
+  sums[part][ch] = v;
+  if (ch == 0) totals[part] = total;
+  __syncthreads();
+  if (part) return;
+  for (int k = 1; k < kParts; ++k) v += sums[k][ch], total += totals[k];
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;
   const u32x2 w = {M::pair(v[0] * inv, v[1] * inv), M::pair(v[2] * inv, v[3] * inv)};
-  *reinterpret_cast<u32x2*>((uint16_t*)a.out + head * D + ch) = w;
+  *reinterpret_cast<u32x2*>((uint16_t*)a.out + head * D + 4 * ch) = w;
 }
 
 template <int D, int C, class M>
@@ -405,7 +411,7 @@ hipError_t go(const Geo& g, const AttendArgs& a, const AttendWork& w, hipStream_
   // enough workgroups to fill the chip several times, shares of at least a unit a
   // wave, partial sums that fit the work area
   const int64_t heads = (int64_t)a.n_tokens * g.hq;
-  int64_t splits = std::min({(int64_t)w.n_cu * 8 / items, (units + kWaves - 1) / kWaves,
+  int64_t splits = std::min({(int64_t)w.n_cu * 6 / items, (units + kWaves - 1) / kWaves,
                              (int64_t)(w.part_bytes / (heads * (D + 2) * 4)), (int64_t)(w.used_bytes / 4 / heads ? 1 << 20 : 1)});
   sp.splits = (int)std::max<int64_t>(1, splits);
   sp.part = w.part;
@@ -414,8 +420,7 @@ hipError_t go(const Geo& g, const AttendArgs& a, const AttendWork& w, hipStream_
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   hipLaunchKernelGGL((attend<D, C, M>), dim3((unsigned)grid), dim3(kThreads), 0, s, g, a, sp);
   if (sp.splits > 1) {
-    const int64_t threads = heads * (D / 4);
-    hipLaunchKernelGGL((combine<D, M>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, g, a, sp);
+    hipLaunchKernelGGL((combine<D, M>), dim3((unsigned)heads), dim3(kThreads), 0, s, g, a, sp);
   }
   return hipGetLastError();
 }
