@@ -47,7 +47,8 @@ class KVContext:
         self.device = device
         self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
         self.block_tokens, self.n_blocks, self.max_blocks = block_tokens, n_blocks, max_blocks
-        self.dtype = d.dtype
+        self.dtype, self.torch_dtype = d.dtype, torch_type(d.dtype)
+        self._current = _current_stream()
         self.cache_bytes = n_blocks * kv_heads * block_tokens * (head_dim + 4)
 
     def _check(self, st):
@@ -55,41 +56,56 @@ class KVContext:
             raise WFError(st, self.lib.wf_kv_last_error(self.handle).decode())
 
     def _b(self, x, need: int, name: str, size: int = 4) -> Optional[int]:
-        """A buffer of `size`-byte elements."""
+        """Address of a buffer of `size`-byte elements; an int is an address
+        the caller vouches for."""
+        try:
+            if (x.get_device() == self.device and x.nbytes >= need and x.element_size() == size and
+                    x.is_contiguous()):
+                return x.data_ptr()
+        except AttributeError:
+            pass
         if hasattr(x, "element_size") and x.element_size() != size:
             raise TypeError(f"{name}: elements of {x.element_size()} bytes, {size} needed")
         return _buf(x, max(int(need), 0), self.device, name)
 
     def _wide(self, x, need: int, name: str) -> Optional[int]:
-        """A buffer of 16-bit floats."""
+        """A buffer of the context's 16-bit type."""
+        if x is None or x.__class__ is int:
+            return x
         self._type(x, name)
-        return _buf(x, max(int(need), 0), self.device, name)
+        return self._b(x, need, name, 2)
 
     def _type(self, x, name: str) -> None:
-        if x is not None and not isinstance(x, int) and x.dtype != torch_type(self.dtype):
-            raise TypeError(f"{name}: {x.dtype}, the context takes {torch_type(self.dtype)}")
+        if getattr(x, "dtype", None) is not self.torch_dtype:
+            raise TypeError(f"{name}: {getattr(x, 'dtype', type(x))}, the context takes {self.torch_dtype}")
 
     def _tokens(self, x, n: int, heads: int, name: str, stride: Optional[int] = None):
         """(address, token stride) of n tokens of heads: a tensor [n, heads, D]
         or [n, heads * D] whose heads are contiguous, or a raw address with
         its stride (default: dense)."""
         width = heads * self.head_dim
-        if x is None or isinstance(x, int):
+        if x is None or x.__class__ is int:
             return x, width if stride is None else int(stride)
-        if not hasattr(x, "data_ptr"):
-            raise TypeError(f"{name}: expected a torch tensor or a device address")
         self._type(x, name)
-        if not x.is_cuda:
-            raise ValueError(f"{name}: a host tensor cannot be passed to the GPU library")
-        if x.device.index != self.device:
-            raise ValueError(f"{name}: tensor on cuda:{x.device.index}, context on cuda:{self.device}")
-        shape, st = tuple(x.shape), x.stride()
-        dense = (len(shape) == 3 and shape[1:] == (heads, self.head_dim) and st[2] == 1 and
-                 (st[1] == self.head_dim or heads == 1)) or (len(shape) == 2 and shape[1] == width and st[1] == 1)
+        if x.get_device() != self.device:
+            raise ValueError(f"{name}: tensor on {x.device}, context on cuda:{self.device}"
+                             if x.is_cuda else f"{name}: a host tensor cannot be passed to the GPU library")
+        shape, st = x.shape, x.stride()
+        if len(shape) == 3:
+            dense = (shape[1] == heads and shape[2] == self.head_dim and st[2] == 1 and
+                     (st[1] == self.head_dim or heads == 1))
+        else:
+            dense = len(shape) == 2 and shape[1] == width and st[1] == 1
         if not dense or shape[0] < n:
-            raise ValueError(f"{name}: shape {shape} and strides {st}; [{n}, {heads}, {self.head_dim}] with "
+            raise ValueError(f"{name}: shape {tuple(shape)} and strides {st}; [{n}, {heads}, {self.head_dim}] with "
                              "contiguous heads needed")
-        return x.data_ptr(), st[0] if n > 1 else max(st[0], width)
+        return x.data_ptr(), st[0] if n > 1 else width
+
+    def _s(self, stream) -> Optional[int]:
+        """The stream's handle; by default the current stream of the context's device."""
+        if stream is None and self._current is not None:
+            return self._current(self.device) or None
+        return _stream(stream)
 
     def wf_kv_step(self, new_tokens, n_rows: int, n_tokens: int, len_in, len_out, pool_in, pool_out, ring, table,
                    q_off, slot, pos, granted, stream=None) -> None:
@@ -99,7 +115,7 @@ class KVContext:
             b(len_out, 4 * r, "len_out"), b(pool_in, 8, "pool_in"), b(pool_out, 8, "pool_out"),
             b(ring, 4 * self.n_blocks, "ring"), b(table, 4 * r * self.max_blocks, "table"),
             b(q_off, 4 * r + 4, "q_off"), b(slot, 8 * t, "slot", 8), b(pos, 4 * t, "pos"), b(granted, r, "granted", 1),
-            _stream(stream)))
+            self._s(stream)))
 
     def wf_kv_store(self, q, k, v, n_tokens: int, pos, slot, q_out, cache, *, cos_sin=None, n_pos: int = 0,
                     rot_dim: int = 0, interleaved: bool = False, q_weight=None, k_weight=None, eps: float = 1e-6,
@@ -113,14 +129,14 @@ class KVContext:
         self._check(self.lib.wf_kv_store(
             self.handle, qp, kp, vp, qs, ks, vs, int(n_tokens), ctypes.byref(how), self._b(pos, 4 * n, "pos"),
             self._b(slot, 8 * n, "slot", 8), self._wide(q_out, 2 * n * self.q_heads * d, "q_out"),
-            self._b(cache, self.cache_bytes, "cache", 1), _stream(stream)))
+            self._b(cache, self.cache_bytes, "cache", 1), self._s(stream)))
 
     def wf_kv_load(self, cache, slot, n_tokens: int, k_out, v_out, stream=None) -> None:
         n = max(int(n_tokens), 0)
         need = 2 * n * self.kv_heads * self.head_dim
         self._check(self.lib.wf_kv_load(
             self.handle, self._b(cache, self.cache_bytes, "cache", 1), self._b(slot, 8 * n, "slot", 8), int(n_tokens),
-            self._wide(k_out, need, "k_out"), self._wide(v_out, need, "v_out"), _stream(stream)))
+            self._wide(k_out, need, "k_out"), self._wide(v_out, need, "v_out"), self._s(stream)))
 
     def wf_kv_attend(self, q, n_tokens: int, cache, table, kv_len, q_off, pos, n_rows: int, scale: float, out, *,
                      window: int = 0, max_q: int = 0, max_kv: int = 0, q_stride=None, stream=None) -> None:
@@ -130,7 +146,7 @@ class KVContext:
             self.handle, qp, qs, int(n_tokens), b(cache, self.cache_bytes, "cache", 1),
             b(table, 4 * r * self.max_blocks, "table"), b(kv_len, 4 * r, "kv_len"), b(q_off, 4 * r + 4, "q_off"),
             b(pos, 4 * n, "pos"), int(n_rows), float(scale), int(window), int(max_q), int(max_kv),
-            self._wide(out, 2 * n * self.q_heads * self.head_dim, "out"), _stream(stream)))
+            self._wide(out, 2 * n * self.q_heads * self.head_dim, "out"), self._s(stream)))
 
     def close(self):
         if getattr(self, "handle", None):
@@ -150,6 +166,13 @@ class KVContext:
             pass
 
 
+def _current_stream():
+    """Device index -> handle of torch's current stream there, without building
+    a Stream object (2.9 us a call); None where this torch has no such call."""
+    import torch
+    return getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 @functools.lru_cache(maxsize=None)
 def torch_type(dtype: int):
     import torch
@@ -160,14 +183,15 @@ def kv_step(ctx: KVContext, new_tokens, n_tokens: int, lens, pool, ring, table, 
     """Allocate the outputs of wf_kv_step and enqueue it.  table and ring are
     updated in place; returns (lens, pool, q_off, slot, pos, granted)."""
     import torch
-    r, kw = new_tokens.shape[0], dict(dtype=torch.int32, device=new_tokens.device)
+    r, device = new_tokens.shape[0], new_tokens.device
     # one allocation for the int32 outputs: lens, pool, q_off, pos
-    flat = torch.empty(r + 2 + r + 1 + n_tokens, **kw)
+    flat = torch.empty(2 * r + 3 + n_tokens, dtype=torch.int32, device=device)
+    slot = torch.empty(n_tokens, dtype=torch.int64, device=device)
+    granted = torch.empty(r, dtype=torch.uint8, device=device)
+    at = flat.data_ptr()
+    ctx.wf_kv_step(new_tokens, r, n_tokens, lens, at, pool, at + 4 * r, ring, table, at + 4 * r + 8, slot.data_ptr(),
+                   at + 8 * r + 12, granted.data_ptr(), stream)
     lens_out, pool_out, q_off, pos = flat.split((r, 2, r + 1, n_tokens))
-    slot = torch.empty(n_tokens, dtype=torch.int64, device=flat.device)
-    granted = torch.empty(r, dtype=torch.uint8, device=flat.device)
-    ctx.wf_kv_step(new_tokens, r, n_tokens, lens, lens_out, pool, pool_out, ring, table, q_off, slot, pos, granted,
-                   stream)
     return lens_out, pool_out, q_off, slot, pos, granted
 
 
@@ -178,9 +202,9 @@ def kv_store(ctx: KVContext, q, k, v, pos, slot, cache, cos_sin=None, *, rot_dim
     import torch
     n = q.shape[0]
     out = torch.empty((n, ctx.q_heads, ctx.head_dim), dtype=q.dtype, device=q.device)
-    ctx.wf_kv_store(q, k, v, n, pos, slot, out, cache, cos_sin=cos_sin, n_pos=0 if cos_sin is None else cos_sin.shape[0],
-                    rot_dim=rot_dim, interleaved=interleaved, q_weight=q_weight, k_weight=k_weight, eps=eps,
-                    stream=stream)
+    ctx.wf_kv_store(q, k, v, n, pos, slot, out.data_ptr(), cache, cos_sin=cos_sin,
+                    n_pos=0 if cos_sin is None else cos_sin.shape[0], rot_dim=rot_dim, interleaved=interleaved,
+                    q_weight=q_weight, k_weight=k_weight, eps=eps, stream=stream)
     return out
 
 
@@ -188,8 +212,9 @@ def kv_load(ctx: KVContext, cache, slot, stream=None):
     """The cached keys and values [T, kv_heads, D] at the given slots."""
     import torch
     n = slot.shape[0]
-    k, v = torch.empty((2, n, ctx.kv_heads, ctx.head_dim), dtype=torch_type(ctx.dtype), device=slot.device)
-    ctx.wf_kv_load(cache, slot, n, k, v, stream)
+    k = torch.empty((n, ctx.kv_heads, ctx.head_dim), dtype=ctx.torch_dtype, device=slot.device)
+    v = torch.empty_like(k)
+    ctx.wf_kv_load(cache, slot, n, k.data_ptr(), v.data_ptr(), stream)
     return k, v
 
 
@@ -200,6 +225,6 @@ def kv_attend(ctx: KVContext, q, cache, table, kv_len, q_off, pos, *, scale: flo
     import torch
     n = q.shape[0]
     out = torch.empty((n, ctx.q_heads, ctx.head_dim), dtype=q.dtype, device=q.device)
-    ctx.wf_kv_attend(q, n, cache, table, kv_len, q_off, pos, kv_len.shape[0], scale, out, window=window, max_q=max_q,
-                     max_kv=max_kv, stream=stream)
+    ctx.wf_kv_attend(q, n, cache, table, kv_len, q_off, pos, kv_len.shape[0], scale, out.data_ptr(), window=window,
+                     max_q=max_q, max_kv=max_kv, stream=stream)
     return out

@@ -63,7 +63,7 @@ def check_step(lens, new, table, ring, pool, b, pad=0, cut=0):
 
 
 @pytest.mark.parametrize("b", [16, 32, 256])
-@pytest.mark.parametrize("rows", [1, 2, 63, 64, 65, 1023, 1024, 1025, 2500])
+@pytest.mark.parametrize("rows", [1, 2, 63, 64, 65, 1023, 1024, 1025, 2500, 4096, 4097, 9000])
 def test_step(rows, b):
     rng = np.random.default_rng(rows * 1000 + b)
     for spare in (1.0, 0.5):
