@@ -61,7 +61,7 @@ extern "C" {
 #define WF_KV_MAX_TOKENS (1 << 24)  /* packed tokens of a step                 */
 #define WF_KV_MAX_HEADS 1024        /* query heads                             */
 #define WF_KV_MAX_BLOCKS (1 << 30)  /* blocks of a cache                       */
-#define WF_KV_MAX_WIDTH (1 << 22)   /* blocks of a row; width * block_tokens stays below 2^31 */
+#define WF_KV_MAX_WIDTH (1 << 22)   /* blocks of a row, of at most 2^30 tokens     */
 
 enum { WF_KV_BF16 = 0, WF_KV_F16 = 1 };
 

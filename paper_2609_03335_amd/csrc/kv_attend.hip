@@ -19,7 +19,14 @@
 // The four waves of a workgroup take every fourth 64 tokens of the same columns and
 // join their sums through LDS; with few columns the tokens are also split over
 // workgroups, whose partial sums a second kernel joins in order.
+#include <type_traits>
+
 #include "kv.h"
+#ifndef WIDE_C
+#define WIDE_C 2
+#define WIDE_W 8
+#define WIDE_O 2
+#endif
 
 namespace wfkv {
 namespace {
@@ -40,6 +47,8 @@ struct MmaBf16 : Bf16 {
   typedef __bf16 v8 __attribute__((ext_vector_type(8)));
   typedef __bf16 v2 __attribute__((ext_vector_type(2)));
   static constexpr float kSlack = 8.0f;
+  static constexpr bool kTrack = false;
+  static constexpr float kLow = 0.0f, kHigh = 0.0f;
   static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
@@ -55,6 +64,11 @@ struct MmaF16 : F16 {
   typedef _Float16 v8 __attribute__((ext_vector_type(8)));
   typedef _Float16 v2 __attribute__((ext_vector_type(2)));
   static constexpr float kSlack = 2.0f;
+  // where the largest score may end up against a fixed reference, in powers of two: at
+  // -8 its p z is 2^-10 for values of size 1, and what f16 drops below 2^-24 is 2^-14
+  // of that; 12 leaves room for z up to 16 (above that the sums overflow, and show it)
+  static constexpr bool kTrack = true;
+  static constexpr float kLow = -8.0f, kHigh = 12.0f;
   static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
@@ -90,6 +104,22 @@ __device__ __forceinline__ float column_sum(float x) {
 template <int D, int C>
 constexpr int kOcc = D * C <= 64 ? 4 : D * C <= 128 ? 3 : D * C <= 256 ? 2 : 1;
 
+// A row's cells of one kv head.  id() is the block of a token (of the last cached
+// token for one past it, so that it can be asked early and without a branch), cell() its address.
+struct Pages {
+  const int32_t* table;
+  const uint8_t* base;
+  uint32_t stride;
+  unsigned most;
+  int last, b_log2;
+  __device__ Pages(const Geo& g, const AttendArgs& a, int row, int kvh, int len)
+      : table(a.table + (int64_t)row * g.width), base(a.cache + (int64_t)kvh * g.cell),
+        stride((uint32_t)g.hk * (uint32_t)g.cell), most((unsigned)g.n_blocks - 1u), last(max(len - 1, 0)),
+        b_log2(g.b_log2) {}
+  __device__ __forceinline__ unsigned id(int token) const { return (unsigned)table[(unsigned)min(token, last) >> b_log2]; }
+  __device__ __forceinline__ const uint8_t* cell(unsigned id) const { return base + (uint64_t)min(id, most) * stride; }
+};
+
 struct Split {
   int tiles, splits;  // of the launch: column tiles of a row, shares of its tokens
   float* part;        // [splits][n_tokens][hq][D + 2] sums, maximum, total
@@ -123,7 +153,7 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
   const int q0 = min(max(a.q_off[row], 0), a.n_tokens), q1 = min(max(a.q_off[row + 1], q0), a.n_tokens);
   const int64_t columns = (int64_t)(q1 - q0) * g.group;
   const int len = min(max(a.kv_len[row], 0), g.width << g.b_log2);
-  const int32_t* table = a.table + (int64_t)row * g.width;
+  const Pages pages(g, a, row, kvh, len);
   const float scale = a.scale * kLog2e;
 
   for (int64_t tile = tile0; tile * 16 * C < columns; tile += sp.tiles) {
@@ -171,36 +201,38 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
 #pragma unroll
     for (int c = 0; c < C; ++c) top[c] = -INFINITY, ref[c] = 0.0f, sum[c] = 0.0f;
 
-    // cell and offset of a group's 16 tokens
-    auto cell_at = [&](int token, int& off) {
-      off = token & (g.b - 1);
-      const unsigned id = token < len ? (unsigned)table[token >> g.b_log2] : 0u;
-      return a.cache + ((int64_t)min(id, (unsigned)g.n_blocks - 1u) * g.hk + kvh) * (int64_t)g.cell;
-    };
     const int kgrp = n >> 2;  // the group whose keys this lane loads: row n of a score tile
-
-    for (int u = first + split * share + wave; u < end; u += kWaves) {
-      const int base = u << 6;
-      int koff, voff;
-      const uint8_t* kcell = cell_at(base + kgrp * 16, koff);
-      const uint8_t* vcell = cell_at(base + grp * 16, voff);
-      // keys: token t*4 + n%4 of group n/4, this lane's quarter of the channels
-      uint32_t kw[4][KW];
+    // keys of a unit: token t*4 + n%4 of group n/4, this lane's quarter of the channels
+    uint32_t kw[4][KW];
+    auto load_keys = [&](int u, unsigned id) __attribute__((always_inline)) {
+      const int off = ((u << 6) + kgrp * 16) & (g.b - 1);
+      const uint8_t* at = pages.cell(id) + (off + (n & 3)) * (D / 2) + grp * (D / 8);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const uint8_t* at = kcell + (koff + t * 4 + (n & 3)) * (D / 2) + grp * (D / 8);
         if constexpr (KW == 2) {
-          const u32x2 w = *reinterpret_cast<const u32x2*>(at);
+          const u32x2 w = *reinterpret_cast<const u32x2*>(at + t * 4 * (D / 2));
           kw[t][0] = w[0], kw[t][1] = w[1];
         } else {
 #pragma unroll
           for (int k = 0; k < KW / 4; ++k) {
-            const u32x4 w = reinterpret_cast<const u32x4*>(at)[k];
+            const u32x4 w = reinterpret_cast<const u32x4*>(at + t * 4 * (D / 2))[k];
 #pragma unroll
             for (int j = 0; j < 4; ++j) kw[t][4 * k + j] = w[j];
           }
         }
       }
+    };
+
+    // a unit's keys are loaded while the one before is worked on, its blocks one earlier still
+    const int u0 = first + split * share + wave;
+    unsigned kid = pages.id((u0 << 6) + kgrp * 16), vid = pages.id((u0 << 6) + grp * 16);
+    load_keys(u0, kid);
+    kid = pages.id(((u0 + kWaves) << 6) + kgrp * 16);
+    for (int u = u0; u < end; u += kWaves) {
+      const int base = u << 6;
+      const uint8_t* vcell = pages.cell(vid);
+      const int voff = (base + grp * 16) & (g.b - 1);
+      vid = pages.id(base + (kWaves << 6) + grp * 16);
       const uint8_t* scales = vcell + g.b * D + voff * 2;
       const u32x4 ks0 = reinterpret_cast<const u32x4*>(scales)[0], ks1 = reinterpret_cast<const u32x4*>(scales)[1];
       const u32x4 vs0 = reinterpret_cast<const u32x4*>(scales + g.b * 2)[0];
@@ -225,6 +257,10 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
 #pragma unroll
             for (int c = 0; c < C; ++c) s[c][e] = M::mma(kk, q[c][k], s[c][e]);
           }
+        }
+        if (h) {
+          load_keys(u + kWaves, kid);
+          kid = pages.id(base + (2 * kWaves << 6) + kgrp * 16);
         }
         const u32x4 ks = h ? ks1 : ks0, vs = h ? vs1 : vs0;
         float kz[8], vz[8];  // of tokens e*4 + i
@@ -251,7 +287,7 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
           up |= m > top[c] + M::kSlack;
         }
         // the running maximum moves only when a score passes it by the slack
-        if (__any(up)) {
+        if (__builtin_expect(__any(up), 0)) {
 #pragma unroll
           for (int c = 0; c < C; ++c) {
             const float m = fmaxf(top[c], column_max(most[c]));
@@ -356,6 +392,379 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
   }
 }
 
+// Many columns (prompts): the W waves of a workgroup take different columns, 16 C
+// each, and the same tokens, whose codes they turn into operands once, in LDS.
+//
+// The tokens go by in steps of 32 (half h of a unit: tokens g*16 + h*8 .. +7 of its four
+// groups).  Step n's probabilities are taken while the matrix cores multiply those of
+// step n - 1 with their values and the queries with the keys of step n + 1.  LDS holds
+// four steps of keys and of values; during the two steps of unit u the waves write keys
+// 2u + 3 and 2u + 4 and values 2u + 1 and 2u + 2, whose codes they loaded a unit earlier.
+//
+// There is no running maximum: probabilities are taken against a reference that stands
+// from the start, the largest score among the last tokens that all of a wave's columns
+// see.  A softmax does not depend on it as long as nothing overflows or vanishes.  For
+// bf16, whose range is that of fp32, the total tells at the end whether it did; f16 tracks the
+// largest score.  Where the reference was too far off, the true maximum is found and
+// the workgroup runs once more, so that the loop itself has no branch and touches the sums with
+// matrix instructions alone.
+template <int D, int C, int W, class M>
+__global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs a, Split sp) {
+  constexpr int KS = D / 32, RB = D / 32, MT = D / 16;
+  constexpr int kFrag = 64;  // 16-byte lanes of an operand
+  __shared__ u32x4 kbuf[4][2 * KS][kFrag], vbuf[4][2 * RB][kFrag];
+  __shared__ __attribute__((aligned(16))) float kzbuf[4][32], vzbuf[4][32];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, grp = lane >> 4;
+  unsigned id = blockIdx.x;
+  const int kvh = (int)(id % (unsigned)g.hk);
+  id /= (unsigned)g.hk;
+  const int split = (int)(id % (unsigned)sp.splits);
+  id /= (unsigned)sp.splits;
+  const int tile0 = sp.tiles - 1 - (int)(id % (unsigned)sp.tiles);
+  const int row = (int)(id / (unsigned)sp.tiles);
+
+  const int q0 = min(max(a.q_off[row], 0), a.n_tokens), q1 = min(max(a.q_off[row + 1], q0), a.n_tokens);
+  const int64_t columns = (int64_t)(q1 - q0) * g.group;
+  const int len = min(max(a.kv_len[row], 0), g.width << g.b_log2);
+  const Pages pages(g, a, row, kvh, len);
+  const float scale = a.scale * kLog2e;
+  __shared__ int range[2];
+
+  for (int64_t tile = tile0; tile * 16 * C * W < columns; tile += sp.tiles) {
+    const int64_t col0 = (tile * W + wave) * 16 * C;
+    u32x4 q[C][KS];
+    int lo[C], hi[C];
+    int lo_min = INT32_MAX, lo_max = 0, hi_min = INT32_MAX, hi_max = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const unsigned col = (unsigned)min(col0 + c * 16 + n, columns - 1);
+      const unsigned i = col / (unsigned)g.group, h = col - i * (unsigned)g.group;
+      const u32x4* src = reinterpret_cast<const u32x4*>((const uint16_t*)a.q + (int64_t)(q0 + i) * a.q_stride +
+                                                        (int64_t)(kvh * g.group + h) * D + grp * (D / 4));
+#pragma unroll
+      for (int k = 0; k < KS; ++k) q[c][k] = src[k];
+      const int p = a.pos[q0 + i];
+      hi[c] = p < 0 ? 0 : min(len, p < INT32_MAX ? p + 1 : p);
+      lo[c] = a.window && p >= a.window ? p - a.window + 1 : 0;
+      lo_min = min(lo_min, lo[c]);
+      lo_max = max(lo_max, lo[c]);
+      hi_min = min(hi_min, hi[c]);
+      hi_max = max(hi_max, hi[c]);
+    }
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) {
+      lo_min = min(lo_min, __shfl_xor(lo_min, off, 64));
+      lo_max = max(lo_max, __shfl_xor(lo_max, off, 64));
+      hi_min = min(hi_min, __shfl_xor(hi_min, off, 64));
+      hi_max = max(hi_max, __shfl_xor(hi_max, off, 64));
+    }
+    lo_min = __builtin_amdgcn_readfirstlane(lo_min);
+    lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+    hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+    hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+    // the tokens that any column of the workgroup sees
+    if (threadIdx.x == 0) range[0] = INT32_MAX, range[1] = 0;
+    __syncthreads();
+    if (lane == 0) {
+      atomicMin(&range[0], lo_min);
+      atomicMax(&range[1], hi_max);
+    }
+    __syncthreads();
+    const int first = __builtin_amdgcn_readfirstlane(range[0]) >> 6;
+    const int units = max(0, ((__builtin_amdgcn_readfirstlane(range[1]) + 63) >> 6) - first);
+    const int share = max(kWaves, (units + sp.splits - 1) / sp.splits);
+    const int used = max(1, (units + share - 1) / share);
+    if (split >= used) {
+      __syncthreads();  // range is read by all before it is set again
+      continue;
+    }
+    const int begin = first + split * share, count = min(units - split * share, share);
+
+    // What a wave turns into operands in a unit: of the keys, KP of the KS operands of one
+    // score tile of one of two steps; of the values, VP of the 2 RB row blocks of two
+    // steps.
+    constexpr int KP = KS * 4 / W, KG = KS / KP, VP = (2 * RB + W - 1) / W;
+    static_assert(KP >= 1 && KG * KP == KS && KG * 4 == W, "waves divide the keys' operands");
+    const int kstep = wave / (2 * KG), ktile = wave / KG % 2, kpart = wave % KG;
+    struct Codes {
+      uint32_t k[KP];
+      u32x2 v[VP];
+      uint32_t z;
+    };
+    // ... and the blocks they are in, asked for a unit earlier still
+    struct Ids {
+      unsigned k, v[VP], z;
+    };
+    auto ask = [&](int kat, int vat, int zat, Ids& d) __attribute__((always_inline)) {
+      d.k = pages.id(((begin + ((kat + kstep) >> 1)) << 6) + (n >> 2) * 16);
+#pragma unroll
+      for (int x = 0; x < VP; ++x) d.v[x] = pages.id(((begin + ((vat + (wave + x * W) / RB) >> 1)) << 6) + grp * 16);
+      d.z = pages.id(((begin + (zat >> 1)) << 6) + grp * 16);
+    };
+    auto load_keys = [&](int step, unsigned id, Codes& w) __attribute__((always_inline)) {
+      const int s = step + kstep, t = (s & 1) * 2 + ktile;
+      const int off = (((begin + (s >> 1)) << 6) + (n >> 2) * 16) & (g.b - 1);
+      const uint8_t* at = pages.cell(id) + (off + t * 4 + (n & 3)) * (D / 2) + grp * (D / 8) + kpart * (KP * 4);
+      if constexpr (KP == 1) {
+        w.k[0] = *reinterpret_cast<const uint32_t*>(at);
+      } else if constexpr (KP == 2) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(at);
+        w.k[0] = x[0], w.k[1] = x[1];
+      } else {
+#pragma unroll
+        for (int k = 0; k < KP / 4; ++k) {
+          const u32x4 x = reinterpret_cast<const u32x4*>(at)[k];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w.k[4 * k + j] = x[j];
+        }
+      }
+    };
+    auto store_keys = [&](int step, const Codes& w) {
+      const int s = step + kstep;
+#pragma unroll
+      for (int k = 0; k < KP; ++k) kbuf[s & 3][ktile * KS + kpart * KP + k][lane] = operand<M>(w.k[k]);
+    };
+    auto load_values = [&](int step, const unsigned (&id)[VP], Codes& w) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < VP; ++x) {
+        // (waves beyond the last row block load the same as others, and store nothing)
+        const int job = wave + x * W, s = step + job / RB, r = job % RB;
+        const int off = (((begin + (s >> 1)) << 6) + grp * 16) & (g.b - 1);
+        w.v[x] = *reinterpret_cast<const u32x2*>(pages.cell(id[x]) + g.b * (D / 2) + (r * 16 + n) * g.b + off + (s & 1) * 8);
+      }
+    };
+    auto store_values = [&](int step, const Codes& w) {
+#pragma unroll
+      for (int x = 0; x < VP; ++x) {
+        const int job = wave + x * W, s = step + job / RB, r = job % RB;
+        if (job >= 2 * RB) continue;
+        const uint32_t w0 = w.v[x][0], w1 = w.v[x][1], mask = 0x0f0f0f0fu;
+        vbuf[s & 3][r][lane] = operand<M>((w0 & mask) | (w1 << 4 & ~mask));
+        vbuf[s & 3][r + RB][lane] = operand<M>((w0 >> 4 & mask) | (w1 & ~mask));
+      }
+    };
+    // scales of the two steps of a unit, a token a lane: wave 0 the keys', wave 1 the values'
+    auto load_scales = [&](int step, unsigned id) __attribute__((always_inline)) -> uint32_t {
+      const int off = (((begin + (step >> 1)) << 6) + lane) & (g.b - 1);
+      return reinterpret_cast<const uint16_t*>(pages.cell(id) + g.b * D)[(wave & 1 ? g.b : 0) + off];
+    };
+    auto store_scales = [&](int step, uint32_t z) {
+      if (wave > 1) return;
+      // token grp*16 + x of the unit: step x/8, place grp*8 + x%8
+      float* to = wave ? &vzbuf[0][0] : &kzbuf[0][0];
+      to[((step + (n >> 3)) & 3) * 32 + grp * 8 + (n & 7)] = __uint_as_float(z << 16) * (wave ? 1.0f : scale);
+    };
+
+    f32x4 o[C][MT];
+    float ref[C], sum[C], top[C];
+    u32x4 p[C];
+    f32x4 s[C][2];
+    auto scores = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) s[c][e] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const u32x4 kk = kbuf[step & 3][e * KS + k][lane];
+#pragma unroll
+          for (int c = 0; c < C; ++c) s[c][e] = M::mma(kk, q[c][k], s[c][e]);
+        }
+      }
+    };
+    auto outputs = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+      for (int r = 0; r < 2 * RB; ++r) {
+        const u32x4 vv = vbuf[step & 3][r][lane];
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c][r] = M::mma(vv, p[c], o[c][r]);
+      }
+    };
+    // the largest score of each column among the tokens of units [u0, u1) that it sees,
+    // straight from the cache
+    auto largest = [&](int u0, int u1, float (&m)[C]) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) m[c] = -INFINITY;
+      for (int u = u0; u < u1; ++u)
+        for (int t = 0; t < 4; ++t) {
+          const int ktoken = (u << 6) + (n >> 2) * 16, ztoken = (u << 6) + grp * 16;
+          const uint32_t* at = reinterpret_cast<const uint32_t*>(
+              pages.cell(pages.id(ktoken)) + ((ktoken & (g.b - 1)) + t * 4 + (n & 3)) * (D / 2) + grp * (D / 8));
+          f32x4 x[C] = {};
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            const u32x4 kk = operand<M>(at[k]);
+#pragma unroll
+            for (int c = 0; c < C; ++c) x[c] = M::mma(kk, q[c][k], x[c]);
+          }
+          const int j0 = (u << 6) + grp * 16 + t * 4;
+          const u32x2 z = *reinterpret_cast<const u32x2*>(pages.cell(pages.id(ztoken)) + g.b * D + (j0 & (g.b - 1)) * 2);
+          const float kz[4] = {bf_lo(z[0]) * scale, bf_hi(z[0]) * scale, bf_lo(z[1]) * scale, bf_hi(z[1]) * scale};
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              m[c] = fmaxf(m[c], j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] * kz[i] : -INFINITY);
+        }
+#pragma unroll
+      for (int c = 0; c < C; ++c) m[c] = column_max(m[c]);
+    };
+
+    const int near = max(hi_min - 1, 0) >> 6;
+    largest(near, near + (hi_min > 0), ref);
+#pragma unroll
+    for (int c = 0; c < C; ++c) ref[c] = fabsf(ref[c]) < INFINITY ? ref[c] : 0.0f;
+
+   for (int pass = 0;; ++pass) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      sum[c] = 0.0f, top[c] = -INFINITY, p[c] = (u32x4){0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < MT; ++k) o[c][k] = (f32x4){0, 0, 0, 0};
+    }
+    // keys of steps 0 to 2, values of step 0, scales of steps 0 and 1; no values before
+    Codes w;
+    Ids d;
+    ask(0, 0, 0, d);
+    load_keys(0, d.k, w);
+    load_values(0, d.v, w);
+    w.z = load_scales(0, d.z);
+    store_keys(0, w);
+    store_values(0, w);
+    store_scales(0, w.z);
+    ask(2, 1, 2, d);
+    load_keys(2, d.k, w);
+    store_keys(2, w);  // step 3's come again in unit 0, the same
+    for (int x = threadIdx.x; x < 2 * RB * kFrag; x += 64 * W) (&vbuf[3][0][0])[x] = (u32x4){0, 0, 0, 0};
+    load_values(1, d.v, w);
+    w.z = load_scales(2, d.z);
+    ask(3, 3, 4, d);
+    load_keys(3, d.k, w);
+    ask(5, 3, 4, d);
+    __syncthreads();
+    scores(0);
+    __syncthreads();  // unit 0 writes step 4's keys over step 0's
+
+    auto unit = [&](int u, auto masked) __attribute__((always_inline)) {
+      constexpr bool kMask = decltype(masked)::value;
+      // codes loaded a unit ago into LDS, the next ones on their way
+      store_keys(2 * u + 3, w);
+      store_values(2 * u + 1, w);
+      store_scales(2 * u + 2, w.z);
+      load_keys(2 * u + 5, d.k, w);
+      load_values(2 * u + 3, d.v, w);
+      w.z = load_scales(2 * u + 4, d.z);
+      ask(2 * u + 7, 2 * u + 5, 2 * u + 6, d);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int step = 2 * u + h;
+        float kz[8], vz[8];
+        *reinterpret_cast<f32x4*>(kz) = *reinterpret_cast<const f32x4*>(&kzbuf[step & 3][grp * 8]);
+        *reinterpret_cast<f32x4*>(kz + 4) = *reinterpret_cast<const f32x4*>(&kzbuf[step & 3][grp * 8 + 4]);
+        *reinterpret_cast<f32x4*>(vz) = *reinterpret_cast<const f32x4*>(&vzbuf[step & 3][grp * 8]);
+        *reinterpret_cast<f32x4*>(vz + 4) = *reinterpret_cast<const f32x4*>(&vzbuf[step & 3][grp * 8 + 4]);
+        const int j0 = ((begin + u) << 6) + grp * 16 + h * 8;
+        float x[C][8];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[c][i] = fmaf(s[c][i / 4][i % 4], kz[i], -ref[c]);
+            if (kMask) x[c][i] = j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] : -INFINITY;
+            if (M::kTrack) top[c] = fmaxf(top[c], x[c][i]);
+          }
+        outputs(step - 1);
+        scores(step + 1);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[c][i] = __builtin_amdgcn_exp2f(x[c][i]);
+            sum[c] += x[c][i];
+            x[c][i] *= vz[i];
+            // a hidden token's scale may be anything
+            if (kMask) x[c][i] = j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] : 0.0f;
+          }
+#pragma unroll
+          for (int b = 0; b < 4; ++b) p[c][b] = M::pair(x[c][b], x[c][4 + b]);
+        }
+#if SGB
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * C * (RB + KS); ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
+          __builtin_amdgcn_sched_group_barrier(0x002, SGV, 0);
+          if (i % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+          if (i % C == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+#endif
+      }
+      __syncthreads();
+    };
+    auto whole = [&](int u) {
+      const int base = (begin + u) << 6;
+      return base >= lo_max && base + 64 <= hi_min;
+    };
+    for (int u = 0; u < count;) {
+      while (u < count && !whole(u)) unit(u++, std::true_type());
+      while (u < count && whole(u)) unit(u++, std::false_type());
+    }
+    outputs(2 * count - 1);
+    // was the reference near enough?
+    bool bad = false;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      sum[c] = column_sum(sum[c]);
+      const bool sees = max(lo[c], begin << 6) < min(hi[c], (begin + count) << 6);
+      bool fine = true;
+      if (M::kTrack) {
+        top[c] = column_max(top[c]);
+        fine = top[c] >= M::kLow && top[c] <= M::kHigh;
+      } else {
+        fine = sum[c] >= 0x1p-60f && sum[c] <= 0x1p60f;
+      }
+#pragma unroll
+      for (int k = 0; k < MT; ++k) fine &= fabsf(o[c][k][0] + o[c][k][1] + o[c][k][2] + o[c][k][3]) < INFINITY;
+      bad |= sees && !fine;
+    }
+    // (also: all have read LDS before the next tile or pass writes it)
+    if (!__syncthreads_or(bad) || pass) break;
+    largest(begin, begin + count, ref);
+#pragma unroll
+    for (int c = 0; c < C; ++c) ref[c] = fabsf(ref[c]) < INFINITY ? ref[c] : 0.0f;
+   }
+
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = col0 + c * 16 + n;
+      if (col >= columns) continue;
+      const unsigned i = (unsigned)col / (unsigned)g.group, h = (unsigned)col - i * (unsigned)g.group;
+      const int64_t head = (int64_t)(q0 + i) * g.hq + kvh * g.group + h;
+      const float inv = sum[c] == 0.0f ? 0.0f : 1.0f / sum[c];
+      float* to = sp.part + ((int64_t)split * a.n_tokens * g.hq + head) * (D + 2);
+#pragma unroll
+      for (int k = 0; k < MT; ++k) {
+        // block k of 16 channels, k >= RB: of the upper half
+        const int at = k * 16 + grp * 4;
+        const f32x4 v = o[c][k];
+        if (used == 1) {
+          const u32x2 b = {M::pair(v[0] * inv, v[1] * inv), M::pair(v[2] * inv, v[3] * inv)};
+          *reinterpret_cast<u32x2*>((uint16_t*)a.out + head * D + at) = b;
+        } else {
+          *reinterpret_cast<f32x2*>(to + at) = (f32x2){v[0], v[1]};
+          *reinterpret_cast<f32x2*>(to + at + 2) = (f32x2){v[2], v[3]};
+        }
+      }
+      if (grp == 0) {
+        if (used > 1) to[D] = sum[c] == 0.0f ? -INFINITY : ref[c], to[D + 1] = sum[c];
+        if (split == 0 && sp.splits > 1) sp.used[head] = used;
+      }
+    }
+  }
+}
+
 // The shares of one query's head, joined in a fixed order: four channels a thread,
 // every kParts-th share a group of threads, then the groups.
 template <int D, class M>
@@ -399,39 +808,43 @@ __global__ __launch_bounds__(kThreads) void combine(Geo g, AttendArgs a, Split s
   *reinterpret_cast<u32x2*>((uint16_t*)a.out + head * D + 4 * ch) = w;
 }
 
-template <int D, int C, class M>
-hipError_t go(const Geo& g, const AttendArgs& a, const AttendWork& w, hipStream_t s) {
-  const int max_q = a.max_q > 0 ? std::min(a.max_q, a.n_tokens) : a.n_tokens;
+// Column tiles, shares and work area of a launch whose workgroups take `tile` columns;
+// `want` workgroups fill the chip.
+template <int D>
+Split split_of(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, int tile, int64_t want) {
   const int64_t most_kv = (int64_t)g.width * g.b;
   const int64_t max_kv = a.max_kv > 0 ? std::min((int64_t)a.max_kv, most_kv) : most_kv;
   Split sp;
-  sp.tiles = (int)(((int64_t)max_q * g.group + 16 * C - 1) / (16 * C));
+  sp.tiles = (int)((columns + tile - 1) / tile);
   const int64_t items = (int64_t)a.n_rows * g.hk * sp.tiles;
-  const int64_t units = (max_kv + 63) / 64;
-  // enough workgroups to fill the chip several times, shares of at least a unit a
-  // wave, partial sums that fit the work area
-  const int64_t heads = (int64_t)a.n_tokens * g.hq;
-  int64_t splits = std::min({(int64_t)w.n_cu * 6 / items, (units + kWaves - 1) / kWaves,
-                             (int64_t)(w.part_bytes / (heads * (D + 2) * 4)), (int64_t)(w.used_bytes / 4 / heads ? 1 << 20 : 1)});
+  // shares of at least a unit a wave, partial sums that fit the work area
+  const int64_t heads = (int64_t)a.n_tokens * g.hq, units = (max_kv + 63) / 64;
+  int64_t splits = std::min({want / items, (units + kWaves - 1) / kWaves,
+                             (int64_t)(w.part_bytes / (heads * (D + 2) * 4))});
+  if ((int64_t)(w.used_bytes / 4) < heads) splits = 1;
   sp.splits = (int)std::max<int64_t>(1, splits);
   sp.part = w.part;
   sp.used = w.used;
-  const int64_t grid = items * sp.splits;
+  return sp;
+}
+
+template <int D, class M, class K>
+hipError_t go(K kernel, const Geo& g, const AttendArgs& a, const Split& sp, hipStream_t s, int threads = kThreads) {
+  const int64_t grid = (int64_t)a.n_rows * g.hk * sp.tiles * sp.splits;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((attend<D, C, M>), dim3((unsigned)grid), dim3(kThreads), 0, s, g, a, sp);
-  if (sp.splits > 1) {
-    hipLaunchKernelGGL((combine<D, M>), dim3((unsigned)heads), dim3(kThreads), 0, s, g, a, sp);
-  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, s, g, a, sp);
+  if (sp.splits > 1)
+    hipLaunchKernelGGL((combine<D, M>), dim3((unsigned)(a.n_tokens * g.hq)), dim3(kThreads), 0, s, g, a, sp);
   return hipGetLastError();
 }
 
 template <int D, class M>
 hipError_t by_columns(const Geo& g, const AttendArgs& a, const AttendWork& w, hipStream_t s) {
   const int64_t columns = (int64_t)(a.max_q > 0 ? std::min(a.max_q, a.n_tokens) : a.n_tokens) * g.group;
-  if (columns <= 16) return go<D, 1, M>(g, a, w, s);
-  if (columns <= 32 || D == 256) return go<D, 2, M>(g, a, w, s);
-  if constexpr (D < 256) return go<D, 4, M>(g, a, w, s);
-  return hipErrorInvalidValue;
+  if (columns <= 16) return go<D, M>(attend<D, 1, M>, g, a, split_of<D>(g, a, w, columns, 16, w.n_cu * 6), s);
+  if (columns <= 64) return go<D, M>(attend<D, 2, M>, g, a, split_of<D>(g, a, w, columns, 32, w.n_cu * 4), s);
+  constexpr int C = WIDE_C, W = WIDE_W;
+  return go<D, M>(attend_wide<D, C, W, M>, g, a, split_of<D>(g, a, w, columns, 16 * C * W, w.n_cu * 2), s, 64 * W);
 }
 
 }  // namespace

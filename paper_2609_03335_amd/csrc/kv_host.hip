@@ -40,8 +40,8 @@ wf_status check_desc(const wf_kv_desc* d) {
     return fail(nullptr, WF_EUNSUPPORTED, "block_tokens=%d is not 16, 32, 64, 128 or 256", b);
   if (d->n_blocks < 1 || d->n_blocks > WF_KV_MAX_BLOCKS)
     return fail(nullptr, WF_EINVAL, "n_blocks=%d outside [1, %d]", d->n_blocks, WF_KV_MAX_BLOCKS);
-  if (d->max_blocks < 1 || d->max_blocks > WF_KV_MAX_WIDTH || (int64_t)d->max_blocks * b >= (1ll << 31))
-    return fail(nullptr, WF_EINVAL, "max_blocks=%d outside [1, %d] or rows of 2^31 tokens", d->max_blocks,
+  if (d->max_blocks < 1 || d->max_blocks > WF_KV_MAX_WIDTH || (int64_t)d->max_blocks * b > (1ll << 30))
+    return fail(nullptr, WF_EINVAL, "max_blocks=%d outside [1, %d] or rows above 2^30 tokens", d->max_blocks,
                 WF_KV_MAX_WIDTH);
   if (d->dtype != WF_KV_BF16 && d->dtype != WF_KV_F16)
     return fail(nullptr, WF_EINVAL, "dtype=%d is not WF_KV_BF16 or WF_KV_F16", d->dtype);

@@ -327,6 +327,14 @@ def test_attend_prompts(hq, hk, d, dtype):
     check_attend(hq, hk, d, 32, [(70, 70, None), (200, 33, None), (1, 1, None), (129, 2, None), (64, 64, None)], dtype, seed=d)
 
 
+@pytest.mark.parametrize("hq,hk,d,dtype", [(4, 1, 128, "bf16"), (8, 2, 64, "f16"), (6, 3, 256, "bf16"), (7, 1, 64, "bf16")])
+def test_attend_long_prompts(hq, hk, d, dtype):
+    """Several tiles of columns a row and many steps of tokens, with and without a window."""
+    rows = [(700, 700, None), (390, 130, None), (64, 64, None), (0, 5, 0), (1000, 90, None)]
+    check_attend(hq, hk, d, 32, rows, dtype, seed=d + hq)
+    check_attend(hq, hk, d, 16, rows, dtype, seed=d + hq, window=150, hints=False)
+
+
 @pytest.mark.parametrize("window", [1, 2, 16, 63, 64, 100, 5000])
 def test_attend_window(window):
     check_attend(8, 2, 64, 16, [(300, 1, None), (150, 90, None), (40, 40, None), (1, 1, None)], window=window, seed=window)
