@@ -24,6 +24,7 @@
 #include "kv.h"
 #ifndef WIDE_C
 #define WIDE_C 2
+#define WIDE_CH 4
 #define WIDE_W 8
 #define WIDE_O 2
 #endif
@@ -48,7 +49,7 @@ struct MmaBf16 : Bf16 {
   typedef __bf16 v2 __attribute__((ext_vector_type(2)));
   static constexpr float kSlack = 8.0f;
   static constexpr bool kTrack = false;
-  static constexpr float kLow = 0.0f, kHigh = 0.0f;
+  static constexpr float kAbove = 0.0f, kLow = 0.0f, kHigh = 0.0f;
   static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
@@ -67,8 +68,9 @@ struct MmaF16 : F16 {
   // where the largest score may end up against a fixed reference, in powers of two: at
   // -8 its p z is 2^-10 for values of size 1, and what f16 drops below 2^-24 is 2^-14
   // of that; 12 leaves room for z up to 16 (above that the sums overflow, and show it)
+  // The reference is put 3 above the largest score of a unit, the middle of that.
   static constexpr bool kTrack = true;
-  static constexpr float kLow = -8.0f, kHigh = 12.0f;
+  static constexpr float kAbove = 3.0f, kLow = -8.0f, kHigh = 12.0f;
   static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
@@ -399,7 +401,8 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
 // groups).  Step n's probabilities are taken while the matrix cores multiply those of
 // step n - 1 with their values and the queries with the keys of step n + 1.  LDS holds
 // four steps of keys and of values; during the two steps of unit u the waves write keys
-// 2u + 3 and 2u + 4 and values 2u + 1 and 2u + 2, whose codes they loaded a unit earlier.
+// 2u + 3 and 2u + 4 and values 2u + 2 and 2u + 3, whose codes they loaded a unit earlier.
+// A chunk of operands is read from LDS while the one before it is multiplied.
 //
 // There is no running maximum: probabilities are taken against a reference that stands
 // from the start, the largest score among the last tokens that all of a wave's columns
@@ -409,14 +412,18 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
 // the workgroup runs once more, so that the loop itself has no branch and touches the sums with
 // matrix instructions alone.
 template <int D, int C, int W, class M>
-__global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs a, Split sp) {
+__global__ __launch_bounds__(64 * W, (D == 256 ? 1 : WIDE_O)) void attend_wide(Geo g, AttendArgs a, Split sp) {
   constexpr int KS = D / 32, RB = D / 32, MT = D / 16;
   constexpr int kFrag = 64;  // 16-byte lanes of an operand
-  __shared__ u32x4 kbuf[4][2 * KS][kFrag], vbuf[4][2 * RB][kFrag];
+  // Chunks of CH operands, NC of them to a step's values or keys.  With several, the next
+  // step's values may not replace the last one's: eight steps of LDS, or where that is too
+  // much (VS = 4) a barrier between.
+  constexpr int CH = D == 256 ? 8 : WIDE_CH, NC = D / 16 / CH, VS = NC > 1 && D < 256 ? 8 : 4;
+  constexpr bool kMid = NC > 1 && VS == 4;
+  __shared__ u32x4 kbuf[4][2 * KS][kFrag], vbuf[VS][2 * RB][kFrag];
   __shared__ __attribute__((aligned(16))) float kzbuf[4][32], vzbuf[4][32];
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   unsigned id = blockIdx.x;
   const int kvh = (int)(id % (unsigned)g.hk);
   id /= (unsigned)g.hk;
@@ -433,6 +440,11 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
   __shared__ int range[2];
 
   for (int64_t tile = tile0; tile * 16 * C * W < columns; tile += sp.tiles) {
+    // (opaque, so that what follows from it is worked out here and not kept in registers
+    // across tiles)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int n = lane & 15, grp = lane >> 4;
     const int64_t col0 = (tile * W + wave) * 16 * C;
     u32x4 q[C][KS];
     int lo[C], hi[C];
@@ -541,8 +553,8 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
         const int job = wave + x * W, s = step + job / RB, r = job % RB;
         if (job >= 2 * RB) continue;
         const uint32_t w0 = w.v[x][0], w1 = w.v[x][1], mask = 0x0f0f0f0fu;
-        vbuf[s & 3][r][lane] = operand<M>((w0 & mask) | (w1 << 4 & ~mask));
-        vbuf[s & 3][r + RB][lane] = operand<M>((w0 >> 4 & mask) | (w1 & ~mask));
+        vbuf[s & (VS - 1)][r][lane] = operand<M>((w0 & mask) | (w1 << 4 & ~mask));
+        vbuf[s & (VS - 1)][r + RB][lane] = operand<M>((w0 >> 4 & mask) | (w1 & ~mask));
       }
     };
     // scales of the two steps of a unit, a token a lane: wave 0 the keys', wave 1 the values'
@@ -561,25 +573,32 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
     float ref[C], sum[C], top[C];
     u32x4 p[C];
     f32x4 s[C][2];
-    auto scores = [&](int step) __attribute__((always_inline)) {
+    // a step's operands: of the values RB of the lower, RB of the upper half of the
+    // channels; of the keys KS of each score tile
+    u32x4 op[2][CH];
+    auto read_values = [&](int step, int part, u32x4 (&to)[CH]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) s[c][e] = (f32x4){0, 0, 0, 0};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const u32x4 kk = kbuf[step & 3][e * KS + k][lane];
-#pragma unroll
-          for (int c = 0; c < C; ++c) s[c][e] = M::mma(kk, q[c][k], s[c][e]);
-        }
-      }
+      for (int x = 0; x < CH; ++x) to[x] = vbuf[step & (VS - 1)][part * CH + x][lane];
     };
-    auto outputs = [&](int step) __attribute__((always_inline)) {
+    auto read_keys = [&](int step, int part, u32x4 (&to)[CH]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int r = 0; r < 2 * RB; ++r) {
-        const u32x4 vv = vbuf[step & 3][r][lane];
+      for (int x = 0; x < CH; ++x) to[x] = kbuf[step & 3][part * CH + x][lane];
+    };
+    auto outputs = [&](int part, const u32x4 (&from)[CH]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c][r] = M::mma(vv, p[c], o[c][r]);
+      for (int x = 0; x < CH; ++x)
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c][part * CH + x] = M::mma(from[x], p[c], o[c][part * CH + x]);
+    };
+    auto scores = [&](int part, const u32x4 (&from)[CH]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < CH; ++x) {
+        const int e = (part * CH + x) / KS, k = (part * CH + x) % KS;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          if (k == 0) s[c][e] = (f32x4){0, 0, 0, 0};
+          s[c][e] = M::mma(from[x], q[c][k], s[c][e]);
+        }
       }
     };
     // the largest score of each column among the tokens of units [u0, u1) that it sees,
@@ -587,11 +606,14 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
     auto largest = [&](int u0, int u1, float (&m)[C]) {
 #pragma unroll
       for (int c = 0; c < C; ++c) m[c] = -INFINITY;
-      for (int u = u0; u < u1; ++u)
+      for (int u = u0; u < u1; ++u) {
+        const int ktoken = (u << 6) + (n >> 2) * 16, ztoken = (u << 6) + grp * 16;
+        const unsigned kid = pages.id(ktoken), zid = pages.id(ztoken);
+        const uint8_t* kat = pages.cell(kid) + ((ktoken & (g.b - 1)) + (n & 3)) * (D / 2) + grp * (D / 8);
+        const uint8_t* zat = pages.cell(zid) + g.b * D + (ztoken & (g.b - 1)) * 2;
+#pragma unroll 1
         for (int t = 0; t < 4; ++t) {
-          const int ktoken = (u << 6) + (n >> 2) * 16, ztoken = (u << 6) + grp * 16;
-          const uint32_t* at = reinterpret_cast<const uint32_t*>(
-              pages.cell(pages.id(ktoken)) + ((ktoken & (g.b - 1)) + t * 4 + (n & 3)) * (D / 2) + grp * (D / 8));
+          const uint32_t* at = reinterpret_cast<const uint32_t*>(kat + t * 4 * (D / 2));
           f32x4 x[C] = {};
 #pragma unroll
           for (int k = 0; k < KS; ++k) {
@@ -599,8 +621,8 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
 #pragma unroll
             for (int c = 0; c < C; ++c) x[c] = M::mma(kk, q[c][k], x[c]);
           }
-          const int j0 = (u << 6) + grp * 16 + t * 4;
-          const u32x2 z = *reinterpret_cast<const u32x2*>(pages.cell(pages.id(ztoken)) + g.b * D + (j0 & (g.b - 1)) * 2);
+          const int j0 = ztoken + t * 4;
+          const u32x2 z = *reinterpret_cast<const u32x2*>(zat + t * 8);
           const float kz[4] = {bf_lo(z[0]) * scale, bf_hi(z[0]) * scale, bf_lo(z[1]) * scale, bf_hi(z[1]) * scale};
 #pragma unroll
           for (int c = 0; c < C; ++c)
@@ -608,55 +630,74 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
             for (int i = 0; i < 4; ++i)
               m[c] = fmaxf(m[c], j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] * kz[i] : -INFINITY);
         }
+      }
 #pragma unroll
       for (int c = 0; c < C; ++c) m[c] = column_max(m[c]);
     };
 
-    const int near = max(hi_min - 1, 0) >> 6;
-    largest(near, near + (hi_min > 0), ref);
-#pragma unroll
-    for (int c = 0; c < C; ++c) ref[c] = fabsf(ref[c]) < INFINITY ? ref[c] : 0.0f;
-
+    auto whole = [&](int u) {
+      const int base = (begin + u) << 6;
+      return base >= lo_max && base + 64 <= hi_min;
+    };
    for (int pass = 0;; ++pass) {
+    // pass 0 takes the reference from the last unit that all of the wave's columns see
+    // whole, or at all, unless they see the first one whole (below); pass 1 from all
+    const int near = hi_min >= 64 && ((hi_min >> 6) - 1) << 6 >= lo_max ? (hi_min >> 6) - 1 : max(hi_min - 1, 0) >> 6;
+    if (pass) largest(begin, begin + count, ref);
+    else largest(near, near + (hi_min > 0 && !whole(0)), ref);
+    // keys of steps 0 to 3, values and scales of steps 0 and 1; all on their way at once
+    Codes w, w0, w2;
+    Ids d, d0, d2, d3;
+    ask(0, 0, 0, d0);
+    ask(2, 2, 2, d2);
+    ask(3, 4, 4, d3);
+    ask(5, 4, 4, d);
+    load_keys(0, d0.k, w0);
+    load_values(0, d0.v, w0);
+    w0.z = load_scales(0, d0.z);
+    load_keys(2, d2.k, w2);
+    load_values(2, d2.v, w);
+    w.z = load_scales(2, d2.z);
+    load_keys(3, d3.k, w);
+    store_keys(0, w0);
+    store_values(0, w0);
+    store_scales(0, w0.z);
+    store_keys(2, w2);  // step 3's come again in unit 0, the same
+    __syncthreads();
+#pragma unroll
+    for (int part = 0; part < NC; ++part) {
+      read_keys(0, part, op[0]);
+      scores(part, op[0]);
+    }
+    if (pass == 0 && whole(0)) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ref[c] = fmaxf(ref[c], s[c][i / 4][i % 4] * kzbuf[0][grp * 8 + i]);
+        ref[c] = column_max(ref[c]);
+      }
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      ref[c] = fabsf(ref[c]) < INFINITY ? ref[c] + (pass ? 0.0f : M::kAbove) : 0.0f;
       sum[c] = 0.0f, top[c] = -INFINITY, p[c] = (u32x4){0, 0, 0, 0};
 #pragma unroll
       for (int k = 0; k < MT; ++k) o[c][k] = (f32x4){0, 0, 0, 0};
     }
-    // keys of steps 0 to 2, values of step 0, scales of steps 0 and 1; no values before
-    Codes w;
-    Ids d;
-    ask(0, 0, 0, d);
-    load_keys(0, d.k, w);
-    load_values(0, d.v, w);
-    w.z = load_scales(0, d.z);
-    store_keys(0, w);
-    store_values(0, w);
-    store_scales(0, w.z);
-    ask(2, 1, 2, d);
-    load_keys(2, d.k, w);
-    store_keys(2, w);  // step 3's come again in unit 0, the same
-    for (int x = threadIdx.x; x < 2 * RB * kFrag; x += 64 * W) (&vbuf[3][0][0])[x] = (u32x4){0, 0, 0, 0};
-    load_values(1, d.v, w);
-    w.z = load_scales(2, d.z);
-    ask(3, 3, 4, d);
-    load_keys(3, d.k, w);
-    ask(5, 3, 4, d);
-    __syncthreads();
-    scores(0);
+    // there are no values before step 0's: any finite ones do, the probabilities are 0
+    read_values(0, 0, op[0]);
     __syncthreads();  // unit 0 writes step 4's keys over step 0's
 
     auto unit = [&](int u, auto masked) __attribute__((always_inline)) {
       constexpr bool kMask = decltype(masked)::value;
       // codes loaded a unit ago into LDS, the next ones on their way
       store_keys(2 * u + 3, w);
-      store_values(2 * u + 1, w);
+      if (!kMid) store_values(2 * u + 2, w);
       store_scales(2 * u + 2, w.z);
       load_keys(2 * u + 5, d.k, w);
-      load_values(2 * u + 3, d.v, w);
+      if (!kMid) load_values(2 * u + 4, d.v, w);
       w.z = load_scales(2 * u + 4, d.z);
-      ask(2 * u + 7, 2 * u + 5, 2 * u + 6, d);
+      if (!kMid) ask(2 * u + 7, 2 * u + 6, 2 * u + 6, d);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int step = 2 * u + h;
@@ -667,6 +708,14 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
         *reinterpret_cast<f32x4*>(vz + 4) = *reinterpret_cast<const f32x4*>(&vzbuf[step & 3][grp * 8 + 4]);
         const int j0 = ((begin + u) << 6) + grp * 16 + h * 8;
         float x[C][8];
+        // values of the step before; op[part % 2] holds chunk `part`
+#pragma unroll
+        for (int part = 0; part < NC; ++part) {
+          if (part + 1 < NC) read_values(max(step - 1, 0), part + 1, op[(part + 1) % 2]);
+          else read_keys(step + 1, 0, op[(part + 1) % 2]);
+          __builtin_amdgcn_sched_barrier(0);
+          outputs(part, op[part % 2]);
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -675,8 +724,14 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
             if (kMask) x[c][i] = j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] : -INFINITY;
             if (M::kTrack) top[c] = fmaxf(top[c], x[c][i]);
           }
-        outputs(step - 1);
-        scores(step + 1);
+        // keys of the step after
+#pragma unroll
+        for (int part = 0; part < NC; ++part) {
+          if (part + 1 < NC) read_keys(step + 1, part + 1, op[(NC + part + 1) % 2]);
+          else read_values(step, 0, op[(NC + part + 1) % 2]);
+          __builtin_amdgcn_sched_barrier(0);
+          scores(part, op[(NC + part) % 2]);
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
 #pragma unroll
@@ -690,28 +745,25 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
 #pragma unroll
           for (int b = 0; b < 4; ++b) p[c][b] = M::pair(x[c][b], x[c][4 + b]);
         }
-#if SGB
-        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-        for (int i = 0; i < 2 * C * (RB + KS); ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
-          __builtin_amdgcn_sched_group_barrier(0x002, SGV, 0);
-          if (i % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
-          if (i % C == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        if (kMid && h == 0) {
+          // step 2u read the later chunks of step 2u - 1's values, which 2u + 3's replace
+          __syncthreads();
+          store_values(2 * u + 2, w);
+          load_values(2 * u + 4, d.v, w);
+          ask(2 * u + 7, 2 * u + 6, 2 * u + 6, d);
         }
-#endif
       }
       __syncthreads();
-    };
-    auto whole = [&](int u) {
-      const int base = (begin + u) << 6;
-      return base >= lo_max && base + 64 <= hi_min;
     };
     for (int u = 0; u < count;) {
       while (u < count && !whole(u)) unit(u++, std::true_type());
       while (u < count && whole(u)) unit(u++, std::false_type());
     }
-    outputs(2 * count - 1);
+#pragma unroll
+    for (int part = 0; part < NC; ++part) {
+      if (part) read_values(max(2 * count - 1, 0), part, op[0]);
+      outputs(part, op[0]);
+    }
     // was the reference near enough?
     bool bad = false;
 #pragma unroll
@@ -731,9 +783,6 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
     }
     // (also: all have read LDS before the next tile or pass writes it)
     if (!__syncthreads_or(bad) || pass) break;
-    largest(begin, begin + count, ref);
-#pragma unroll
-    for (int c = 0; c < C; ++c) ref[c] = fabsf(ref[c]) < INFINITY ? ref[c] : 0.0f;
    }
 
 #pragma unroll
@@ -765,44 +814,52 @@ __global__ __launch_bounds__(64 * W, WIDE_O) void attend_wide(Geo g, AttendArgs 
   }
 }
 
-// The shares of one query's head, joined in a fixed order: four channels a thread,
-// every kParts-th share a group of threads, then the groups.
-template <int D, class M>
+// The shares of each query's head, joined in a fixed order: four channels a thread, P
+// groups of threads a head that take every P-th share.
+template <int D, int P, class M>
 __global__ __launch_bounds__(kThreads) void combine(Geo g, AttendArgs a, Split sp) {
-  constexpr int kParts = kThreads / (D / 4);
-  __shared__ float tops[kWaves], totals[kParts];
-  __shared__ __attribute__((aligned(16))) f32x4 sums[kParts][D / 4];
-  const int64_t head = blockIdx.x, heads = (int64_t)a.n_tokens * g.hq;
-  const int64_t t = head / g.hq;
-  if (t < a.q_off[0] || t >= a.q_off[a.n_rows]) return;
-  const int used = sp.used[head];
-  if (used <= 1) return;
-  const int ch = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
+  constexpr int L = D / 4, H = kThreads / (L * P);  // heads of a workgroup
+  __shared__ __attribute__((aligned(16))) f32x4 sums[H][P][L];
+  __shared__ float tops[kWaves], totals[H][P];
+  const int ch = threadIdx.x % L, part = threadIdx.x / L % P, slot = threadIdx.x / (L * P);
+  const int64_t head = (int64_t)blockIdx.x * H + slot, heads = (int64_t)a.n_tokens * g.hq, t = head / g.hq;
+  const bool mine = head < heads && t >= a.q_off[0] && t < a.q_off[a.n_rows];
+  const int used = mine ? sp.used[head] : 0;
   const float* from = sp.part + head * (D + 2);
   const int64_t step = heads * (D + 2);
   float m = -INFINITY;
-  for (int s = threadIdx.x; s < used; s += kThreads) m = fmaxf(m, from[s * step + D]);
+  if constexpr (P > 1) {
+    static_assert(H == 1, "all threads look for one head's maximum");
+    for (int s = threadIdx.x; s < used; s += kThreads) m = fmaxf(m, from[s * step + D]);
 #pragma unroll
-  for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = m;
-  __syncthreads();
-  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, tops[w]);
+    for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = m;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, tops[w]);
+  } else {
+    for (int s = 0; s < used; ++s) m = fmaxf(m, from[s * step + D]);
+  }
   const float r = m == -INFINITY ? 0.0f : m;
   float total = 0.0f;
   f32x4 v = {0, 0, 0, 0};
+  if (used > 1) {
 #pragma unroll 4
-  for (int s = part; s < used; s += kParts) {
-    const float* at = from + s * step;
-    const float keep = __builtin_amdgcn_exp2f(at[D] - r);
-    total += at[D + 1] * keep;
-    const f32x2 v0 = *reinterpret_cast<const f32x2*>(at + 4 * ch), v1 = *reinterpret_cast<const f32x2*>(at + 4 * ch + 2);
-    v[0] += v0[0] * keep, v[1] += v0[1] * keep, v[2] += v1[0] * keep, v[3] += v1[1] * keep;
+    for (int s = part; s < used; s += P) {
+      const float* at = from + s * step;
+      const float keep = __builtin_amdgcn_exp2f(at[D] - r);
+      total += at[D + 1] * keep;
+      const f32x2 v0 = *reinterpret_cast<const f32x2*>(at + 4 * ch), v1 = *reinterpret_cast<const f32x2*>(at + 4 * ch + 2);
+      v[0] += v0[0] * keep, v[1] += v0[1] * keep, v[2] += v1[0] * keep, v[3] += v1[1] * keep;
+    }
   }
-  sums[part][ch] = v;
-  if (ch == 0) totals[part] = total;
-  __syncthreads();
-  if (part) return;
-  for (int k = 1; k < kParts; ++k) v += sums[k][ch], total += totals[k];
+  if (P > 1) {
+    sums[slot][part][ch] = v;
+    if (ch == 0) totals[slot][part] = total;
+    __syncthreads();
+    if (part) return;
+    for (int k = 1; k < P; ++k) v += sums[slot][k][ch], total += totals[slot][k];
+  }
+  if (used <= 1) return;
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;
   const u32x2 w = {M::pair(v[0] * inv, v[1] * inv), M::pair(v[2] * inv, v[3] * inv)};
   *reinterpret_cast<u32x2*>((uint16_t*)a.out + head * D + 4 * ch) = w;
@@ -833,8 +890,15 @@ hipError_t go(K kernel, const Geo& g, const AttendArgs& a, const Split& sp, hipS
   const int64_t grid = (int64_t)a.n_rows * g.hk * sp.tiles * sp.splits;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, s, g, a, sp);
-  if (sp.splits > 1)
-    hipLaunchKernelGGL((combine<D, M>), dim3((unsigned)(a.n_tokens * g.hq)), dim3(kThreads), 0, s, g, a, sp);
+  if (sp.splits > 1) {
+    // a head to a group of threads where there are few shares, to a workgroup where many
+    constexpr int P = kThreads / (D / 4);
+    const int64_t heads = (int64_t)a.n_tokens * g.hq;
+    if (sp.splits <= 8)
+      hipLaunchKernelGGL((combine<D, 1, M>), dim3((unsigned)((heads + P - 1) / P)), dim3(kThreads), 0, s, g, a, sp);
+    else
+      hipLaunchKernelGGL((combine<D, P, M>), dim3((unsigned)heads), dim3(kThreads), 0, s, g, a, sp);
+  }
   return hipGetLastError();
 }
 
@@ -843,7 +907,7 @@ hipError_t by_columns(const Geo& g, const AttendArgs& a, const AttendWork& w, hi
   const int64_t columns = (int64_t)(a.max_q > 0 ? std::min(a.max_q, a.n_tokens) : a.n_tokens) * g.group;
   if (columns <= 16) return go<D, M>(attend<D, 1, M>, g, a, split_of<D>(g, a, w, columns, 16, w.n_cu * 6), s);
   if (columns <= 64) return go<D, M>(attend<D, 2, M>, g, a, split_of<D>(g, a, w, columns, 32, w.n_cu * 4), s);
-  constexpr int C = WIDE_C, W = WIDE_W;
+  constexpr int C = D == 256 ? 1 : WIDE_C, W = D == 256 ? 4 : WIDE_W;
   return go<D, M>(attend_wide<D, C, W, M>, g, a, split_of<D>(g, a, w, columns, 16 * C * W, w.n_cu * 2), s, 64 * W);
 }
 
