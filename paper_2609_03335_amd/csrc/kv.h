@@ -65,15 +65,15 @@ struct AttendArgs {
   void* out;
 };
 
-// The work area of launch_attend: partial sums, and for each query's head the
-// number of shares that wrote them.
-constexpr size_t kPartBytes = size_t(32) << 20, kUsedBytes = size_t(1) << 20;
+// The work area of launch_attend: partial sums, the number of shares that wrote
+// those of each query's head, and counts of shares done, 0 between launches.
+constexpr size_t kPartBytes = size_t(32) << 20, kCountBytes = size_t(1) << 20;
 struct AttendWork {
   int n_cu;
   float* part;
   size_t part_bytes;
-  int32_t* used;
-  size_t used_bytes;
+  int32_t *used, *arrived;
+  size_t count_bytes;  // of each
 };
 
 hipError_t launch_step(const Geo& g, const StepArgs& a, hipStream_t s);

@@ -115,7 +115,16 @@ wf_status wf_kv_ctx_create(int hip_device, const wf_kv_desc* desc, wf_kv_ctx** o
   g.cell = (int)cell_bytes(desc);
   wf_status made = launch(ctx, "wf_kv_ctx_create", [&] {
     hipError_t e = hipDeviceGetAttribute(&ctx->work.n_cu, hipDeviceAttributeMultiprocessorCount, hip_device);
-    if (e == hipSuccess) e = hipMalloc(&ctx->work.part, wfkv::kPartBytes + wfkv::kUsedBytes);
+    if (e == hipSuccess) e = hipMalloc(&ctx->work.part, wfkv::kPartBytes + 2 * wfkv::kCountBytes);
+    if (e != hipSuccess) return e;
+    char* counts = reinterpret_cast<char*>(ctx->work.part) + wfkv::kPartBytes;
+    ctx->work.used = reinterpret_cast<int32_t*>(counts);
+    ctx->work.arrived = reinterpret_cast<int32_t*>(counts + wfkv::kCountBytes);
+    ctx->work.part_bytes = wfkv::kPartBytes;
+    ctx->work.count_bytes = wfkv::kCountBytes;
+    e = hipMemset(counts, 0, 2 * wfkv::kCountBytes);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    if (e != hipSuccess) (void)hipFree(ctx->work.part);
     return e;
   });
   if (made != WF_OK) {
@@ -123,9 +132,6 @@ wf_status wf_kv_ctx_create(int hip_device, const wf_kv_desc* desc, wf_kv_ctx** o
     delete ctx;
     return st;
   }
-  ctx->work.part_bytes = wfkv::kPartBytes;
-  ctx->work.used = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(ctx->work.part) + wfkv::kPartBytes);
-  ctx->work.used_bytes = wfkv::kUsedBytes;
   *out = ctx;
   return WF_OK;
 }
