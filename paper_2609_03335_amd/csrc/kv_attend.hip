@@ -934,6 +934,10 @@ __global__ __launch_bounds__(kThreads) void combine(Geo g, AttendArgs a, Split s
   *reinterpret_cast<u32x2*>((uint16_t*)a.out + head * D + 4 * ch) = w;
 }
 
+// Workgroups of a launch at most (a grid has fewer than 2^32 threads, 512 a workgroup here);
+// batches of more rows take several.
+constexpr int64_t kMostGrid = 1 << 22;
+
 // Column tiles, shares and work area of a launch whose workgroups take `tile` columns;
 // `want` workgroups fill the chip.
 template <int D>
@@ -941,7 +945,8 @@ Split split_of(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t c
   const int64_t most_kv = (int64_t)g.width * g.b;
   const int64_t max_kv = a.max_kv > 0 ? std::min((int64_t)a.max_kv, most_kv) : most_kv;
   Split sp;
-  sp.tiles = (int)((columns + tile - 1) / tile);
+  // (workgroups go on to the tiles past those launched: max_q may be unknown or too low)
+  sp.tiles = (int)std::min<int64_t>((columns + tile - 1) / tile, std::max<int64_t>(1, kMostGrid / g.hk));
   const int64_t items = (int64_t)a.n_rows * g.hk * sp.tiles;
   // shares of at least a unit a wave, partial sums that fit the work area
   const int64_t heads = (int64_t)a.n_tokens * g.hq, units = (max_kv + 63) / 64;
@@ -957,10 +962,17 @@ Split split_of(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t c
 
 template <class K>
 hipError_t launch(K kernel, const Geo& g, const AttendArgs& a, const Split& sp, int threads, hipStream_t s) {
-  const int64_t grid = (int64_t)a.n_rows * g.hk * sp.tiles * sp.splits;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, s, g, a, sp);
-  return hipGetLastError();
+  const int64_t row = (int64_t)g.hk * sp.tiles * sp.splits;  // workgroups
+  const int rows = (int)std::max<int64_t>(1, std::min<int64_t>(a.n_rows, kMostGrid / row));
+  for (int r = 0; r < a.n_rows; r += rows) {
+    AttendArgs b = a;
+    b.table += (int64_t)r * g.width, b.kv_len += r, b.q_off += r;
+    b.n_rows = std::min(rows, a.n_rows - r);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(b.n_rows * row)), dim3(threads), 0, s, g, b, sp);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // Up to 128 columns a row (1 or 2 tiles of 16 a workgroup); the tokens are split so that all
@@ -971,6 +983,7 @@ hipError_t narrow(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_
   const Split sp = split_of<D>(g, a, w, columns, 16 * C, w.n_cu * kOcc<D, C>);
   const hipError_t e = launch(attend<D, C, M>, g, a, sp, kThreads, s);
   if (e != hipSuccess || sp.splits <= kFused) return e;
+  // (heads x 256 threads: shares are only taken of up to kCountBytes / 4 heads)
   hipLaunchKernelGGL((combine<D, kThreads / (D / 4), M>), dim3((unsigned)(a.n_tokens * g.hq)), dim3(kThreads), 0, s, g, a, sp);
   return hipGetLastError();
 }

@@ -32,7 +32,7 @@ def wf_kv_cache_bytes(q_heads: int, kv_heads: int, head_dim: int, block_tokens: 
 class KVContext:
     """A wf_kv_ctx on one HIP device: the geometry of a cache.  Tensor
     arguments are checked before any call reaches the library (GPU tensor, the
-    context's device, enough bytes; the 16-bit ones also for their type)."""
+    context's device, enough bytes, type or size of the elements)."""
 
     def __init__(self, device: int = 0, *, q_heads: int, kv_heads: int, head_dim: int, block_tokens: int,
                  n_blocks: int, max_blocks: int, dtype="bf16"):
@@ -55,25 +55,31 @@ class KVContext:
         if st != WF_OK:
             raise WFError(st, self.lib.wf_kv_last_error(self.handle).decode())
 
-    def _b(self, x, need: int, name: str, size: int = 4) -> Optional[int]:
-        """Address of a buffer of `size`-byte elements; an int is an address
-        the caller vouches for."""
+    def _b(self, x, need: int, name: str, size: int = 4, floating: bool = False) -> Optional[int]:
+        """Address of a buffer of `size`-byte whole numbers (or floating ones); an int is an address
+        the caller vouches for.  (A sound tensor passes in 0.4 us; an exception
+        on the way to an int would cost twice that.)"""
+        if x is None or x.__class__ is int:
+            return x
         try:
             if (x.get_device() == self.device and x.nbytes >= need and x.element_size() == size and
-                    x.is_contiguous()):
+                    x.is_contiguous() and x.is_floating_point() == floating):
                 return x.data_ptr()
         except AttributeError:
             pass
         if hasattr(x, "element_size") and x.element_size() != size:
             raise TypeError(f"{name}: elements of {x.element_size()} bytes, {size} needed")
-        return _buf(x, max(int(need), 0), self.device, name)
+        address = _buf(x, max(int(need), 0), self.device, name)
+        if hasattr(x, "is_floating_point") and x.is_floating_point() != floating:
+            raise TypeError(f"{name}: elements of type {x.dtype}")
+        return address
 
     def _wide(self, x, need: int, name: str) -> Optional[int]:
         """A buffer of the context's 16-bit type."""
         if x is None or x.__class__ is int:
             return x
         self._type(x, name)
-        return self._b(x, need, name, 2)
+        return self._b(x, need, name, 2, True)
 
     def _type(self, x, name: str) -> None:
         if getattr(x, "dtype", None) is not self.torch_dtype:
@@ -91,6 +97,8 @@ class KVContext:
             raise ValueError(f"{name}: tensor on {x.device}, context on cuda:{self.device}"
                              if x.is_cuda else f"{name}: a host tensor cannot be passed to the GPU library")
         shape, st = x.shape, x.stride()
+        if shape == (n, heads, self.head_dim) and st[1:] == (self.head_dim, 1):
+            return x.data_ptr(), st[0] if n > 1 else width
         if len(shape) == 3:
             dense = (shape[1] == heads and shape[2] == self.head_dim and st[2] == 1 and
                      (st[1] == self.head_dim or heads == 1))
@@ -125,7 +133,7 @@ class KVContext:
                                         self._tokens(k, n, self.kv_heads, "k", strides[1]),
                                         self._tokens(v, n, self.kv_heads, "v", strides[2]))
         how = wf_kv_norm_rope(self._wide(q_weight, 2 * d, "q_weight"), self._wide(k_weight, 2 * d, "k_weight"), eps,
-                              rot_dim, int(interleaved), n_pos, self._b(cos_sin, 4 * n_pos * rot_dim, "cos_sin"))
+                              rot_dim, int(interleaved), n_pos, self._b(cos_sin, 4 * n_pos * rot_dim, "cos_sin", 4, True))
         self._check(self.lib.wf_kv_store(
             self.handle, qp, kp, vp, qs, ks, vs, int(n_tokens), ctypes.byref(how), self._b(pos, 4 * n, "pos"),
             self._b(slot, 8 * n, "slot", 8), self._wide(q_out, 2 * n * self.q_heads * d, "q_out"),
@@ -183,11 +191,11 @@ def kv_step(ctx: KVContext, new_tokens, n_tokens: int, lens, pool, ring, table, 
     """Allocate the outputs of wf_kv_step and enqueue it.  table and ring are
     updated in place; returns (lens, pool, q_off, slot, pos, granted)."""
     import torch
-    r, device = new_tokens.shape[0], new_tokens.device
+    r, empty = new_tokens.shape[0], new_tokens.new_empty
     # one allocation for the int32 outputs: lens, pool, q_off, pos
-    flat = torch.empty(2 * r + 3 + n_tokens, dtype=torch.int32, device=device)
-    slot = torch.empty(n_tokens, dtype=torch.int64, device=device)
-    granted = torch.empty(r, dtype=torch.uint8, device=device)
+    flat = empty(2 * r + 3 + n_tokens, dtype=torch.int32)
+    slot = empty(n_tokens, dtype=torch.int64)
+    granted = empty(r, dtype=torch.uint8)
     at = flat.data_ptr()
     ctx.wf_kv_step(new_tokens, r, n_tokens, lens, at, pool, at + 4 * r, ring, table, at + 4 * r + 8, slot.data_ptr(),
                    at + 8 * r + 12, granted.data_ptr(), stream)
@@ -199,9 +207,8 @@ def kv_store(ctx: KVContext, q, k, v, pos, slot, cache, cos_sin=None, *, rot_dim
              q_weight=None, k_weight=None, eps: float = 1e-6, stream=None):
     """Norm, rotate and store the tokens of q [T, q_heads, D], k and v [T,
     kv_heads, D]; returns the queries [T, q_heads, D]."""
-    import torch
     n = q.shape[0]
-    out = torch.empty((n, ctx.q_heads, ctx.head_dim), dtype=q.dtype, device=q.device)
+    out = q.new_empty((n, ctx.q_heads, ctx.head_dim))
     ctx.wf_kv_store(q, k, v, n, pos, slot, out.data_ptr(), cache, cos_sin=cos_sin,
                     n_pos=0 if cos_sin is None else cos_sin.shape[0], rot_dim=rot_dim, interleaved=interleaved,
                     q_weight=q_weight, k_weight=k_weight, eps=eps, stream=stream)
@@ -210,10 +217,8 @@ def kv_store(ctx: KVContext, q, k, v, pos, slot, cache, cos_sin=None, *, rot_dim
 
 def kv_load(ctx: KVContext, cache, slot, stream=None):
     """The cached keys and values [T, kv_heads, D] at the given slots."""
-    import torch
-    n = slot.shape[0]
-    k = torch.empty((n, ctx.kv_heads, ctx.head_dim), dtype=ctx.torch_dtype, device=slot.device)
-    v = torch.empty_like(k)
+    n, shape = slot.shape[0], (slot.shape[0], ctx.kv_heads, ctx.head_dim)
+    k, v = slot.new_empty(shape, dtype=ctx.torch_dtype), slot.new_empty(shape, dtype=ctx.torch_dtype)
     ctx.wf_kv_load(cache, slot, n, k.data_ptr(), v.data_ptr(), stream)
     return k, v
 
@@ -222,9 +227,8 @@ def kv_attend(ctx: KVContext, q, cache, table, kv_len, q_off, pos, *, scale: flo
               max_kv: int = 0, stream=None):
     """Attention of the packed queries q [T, q_heads, D] over the cache:
     [T, q_heads, D].  Rows of tokens past q_off[-1] are not written."""
-    import torch
     n = q.shape[0]
-    out = torch.empty((n, ctx.q_heads, ctx.head_dim), dtype=q.dtype, device=q.device)
+    out = q.new_empty((n, ctx.q_heads, ctx.head_dim))
     ctx.wf_kv_attend(q, n, cache, table, kv_len, q_off, pos, kv_len.shape[0], scale, out.data_ptr(), window=window,
                      max_q=max_q, max_kv=max_kv, stream=stream)
     return out

@@ -212,6 +212,52 @@ def test_store_runs_of_tokens(T):
         assert np.array_equal(cache.cpu().numpy(), want.bytes)
 
 
+def runs_of_slots(rng, T, b, longest):
+    """Slots of T tokens: runs of consecutive tokens from anywhere in a block, in blocks of
+    any order; a run without slots now and then.  And the number of blocks."""
+    slot, used = [], 0
+    while len(slot) < T:
+        n, first = int(rng.integers(1, longest + 1)), int(rng.integers(0, b))
+        n = min(n, T - len(slot))
+        if rng.random() < 0.1:
+            slot += [-1] * n
+        else:
+            slot += [used * b + first + i for i in range(n)]
+            used += -(-(first + n) // b)
+    order = rng.permutation(used)
+    slot = np.array(slot)
+    return np.where(slot < 0, -1, order[np.maximum(slot, 0) // b] * b + slot % b).astype(np.int64), used
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d,b,longest", [(12, 4, 64, 16, 300), (14, 1, 128, 32, 40), (9, 3, 256, 64, 700), (16, 2, 128, 16, 3)])
+def test_store_many_tokens(hq, hk, d, b, longest, dtype):
+    """Large calls: the same bytes and queries, to the last bit, as the tokens a few at a time,
+    and values and keys as the oracle's where nothing is normed or rotated."""
+    rng = np.random.default_rng(d + b)
+    T = 40000 // (hq + 2 * hk) + 13
+    q, k, v, _, _, pos, cs = store_case(rng, hq, hk, d, b, T, dtype, d, pad=8)
+    slot, n = runs_of_slots(rng, T, b, longest)
+    w = dev((1 + 0.2 * rng.standard_normal(d)).astype(np.float32), TYPES[dtype])
+    p, sl, c = dev(pos), dev(slot), dev(cs)
+    with ctx_of(hq, hk, d, b, n, 4, dtype) as ctx:
+        for how in (dict(rot_dim=d, q_weight=w, k_weight=w), dict(rot_dim=d // 2, k_weight=w), dict(rot_dim=d // 4, interleaved=True), dict()):
+            table = (c[:, :how["rot_dim"]].contiguous(),) if how.get("rot_dim") else ()
+            one, parts = (torch.full((ctx.cache_bytes,), 170, dtype=torch.uint8, device=DEV) for _ in range(2))
+            out = pkg.kv_store(ctx, q, k, v, p, sl, one, *table, **how)
+            for t in range(0, T, 499):
+                e = min(T, t + 499)
+                got = pkg.kv_store(ctx, q[t:e], k[t:e], v[t:e], p[t:e].clone(), sl[t:e].clone(), parts, *table, **how)
+                assert torch.equal(got, out[t:e]), (how, t)
+            assert torch.equal(one, parts), how
+    want = K.Cache(n, hk, b, d)
+    want.bytes[:] = 170
+    hk_, hv_ = host(k), host(v)
+    for t in np.nonzero(slot >= 0)[0]:
+        want.put(slot[t], hk_[t], hv_[t])
+    assert np.array_equal(one.cpu().numpy(), want.bytes.reshape(-1))     # the last: as given
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_store_extremes(dtype):
     """Zeros, one large channel, ties, the type's largest and smallest values,
@@ -403,6 +449,102 @@ def test_attend_nan_in_sight_shows():
         got = host(pkg.kv_attend(ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos), scale=0.125))
     assert np.isnan(got[20:, 2:]).all()
     assert np.isfinite(got[:20]).all() and np.isfinite(got[:, :2]).all()
+
+
+def skewed_case(rng, hq, hk, d, b, n, nq, dtype, far, size=1.0):
+    """nq queries of one row over n tokens; the tokens in `far` have large keys along the queries'
+    common direction, all others small ones; value scales `size` times the usual."""
+    q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, [(n, nq, None)], dtype)
+    x = 0.1 * rng.standard_normal((n, hk, d)).astype(np.float32)
+    line = rng.standard_normal(d).astype(np.float32)
+    for j, f in far.items():
+        x[j] = f * line
+    q = dev((line + 0.1 * rng.standard_normal((nq, hq, d))).astype(np.float32), TYPES[dtype])
+    v = (size * rng.standard_normal((n, hk, d))).astype(np.float32)
+    for j in range(n):
+        cache.put(int(table[0, j // b]) * b + j % b, x[j], v[j])
+    return q, cache, table, kv, q_off, pos
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d", [(8, 1, 64), (4, 1, 128), (6, 1, 256)])
+def test_attend_prompts_of_uneven_scores(hq, hk, d, dtype):
+    """Many columns whose largest score is far above or below those of the last and the first
+    tokens: at one early token, in the middle, at the end only; large and small values."""
+    b, n, nq = 16, 450, 60
+    for i, (far, size) in enumerate([({3: 8.0}, 1.0), ({200: 20.0}, 1.0), ({449: 30.0}, 1.0), ({0: -20.0, 447: -20.0}, 1.0),
+                                     ({5: 3.0, 300: 3.0}, 400.0), ({100: 12.0}, 3000.0), ({}, 0.01)]):
+        rng = np.random.default_rng(100 * i + d)
+        q, cache, table, kv, q_off, pos = skewed_case(rng, hq, hk, d, b, n, nq, dtype, far, size)
+        want, mag, dots = K.attend(host(q), cache, table, kv, q_off, pos, d ** -0.5, 0)
+        with ctx_of(hq, hk, d, b, cache.n, table.shape[1], dtype) as ctx:
+            got = host(pkg.kv_attend(ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos), scale=d ** -0.5,
+                                     max_q=nq, max_kv=n))
+        # as bound(); for f16, a probability times its value scale is rounded to a step of 2^-25 of a
+        # total that may be as small as 2^-8 (the reference is within 8 powers of two of the largest score)
+        lim = bound(dtype, want, mag, dots, d, n) + (6 * n * 2.0 ** -17 if dtype == "f16" else 0.0)
+        assert np.isfinite(got).all(), i
+        assert (np.abs(got - want) <= lim).all(), (i, float((np.abs(got - want) / lim).max()))
+
+
+def test_floats_are_not_taken_for_integers():
+    with ctx_of(4, 2, 64, 16, 8, 4) as ctx:
+        x = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt, device=DEV)
+        cache, q, k, slot = x(ctx.cache_bytes, dt=torch.uint8), x(3, 4, 64), x(3, 2, 64), x(3, dt=torch.int64)
+        for bad in (dict(pos=x(3, dt=torch.float32)), dict(slot=slot.double()), dict(cos_sin=x(4, 64, dt=torch.int32), rot_dim=64)):
+            with pytest.raises(TypeError):
+                how = {**dict(pos=x(3, dt=torch.int32), slot=slot, cos_sin=x(4, 64, dt=torch.float32), rot_dim=64), **bad}
+                pkg.kv_store(ctx, q, k, k, how["pos"], how["slot"], cache, how["cos_sin"], rot_dim=64)
+
+
+@pytest.mark.parametrize("hq,hk,rows", [(128, 128, 40000), (8, 2, 65536)])
+def test_attend_more_rows_than_one_grid(hq, hk, rows):
+    """Batches whose workgroups do not fit one grid: each row has its own token's value."""
+    d, b = 64, 16
+    rng = np.random.default_rng(rows)
+    x = torch.from_numpy(rng.integers(-6, 7, (32, hk, d)).astype(np.float32)).to(DEV).bfloat16()
+    x[..., 0] = 6                                          # scale 1: integers up to 6 less the ones off the grid
+    slots = torch.arange(32, device=DEV) * b               # 32 blocks of one token
+    with ctx_of(hq, hk, d, b, 32, 1) as ctx:
+        cache = torch.zeros(ctx.cache_bytes, dtype=torch.uint8, device=DEV)
+        pkg.kv_store(ctx, x[:, :1].expand(32, hq, d).contiguous(), x, x, None, slots, cache)
+        _, v = pkg.kv_load(ctx, cache, slots)
+        at = torch.arange(rows, device=DEV) % 32
+        ones = torch.ones(rows, dtype=torch.int32, device=DEV)
+        q = torch.ones(1, hq, d, dtype=torch.bfloat16, device=DEV).expand(rows, hq, d).contiguous()
+        for hint in (1, 0):                                # 0: as many columns a row as there are tokens
+            out = pkg.kv_attend(ctx, q, cache, at.int()[:, None].contiguous(), ones, torch.arange(rows + 1, device=DEV).int(), ones - 1,
+                                scale=1.0, max_q=hint, max_kv=1)
+            assert torch.equal(out.view(rows, hk, hq // hk, d), v[at][:, :, None].expand(-1, -1, hq // hk, -1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d,b", [(8, 2, 64, 16), (4, 1, 128, 64), (4, 2, 256, 32)])
+def test_attend_prompts_beside_garbage(hq, hk, d, b, dtype):
+    """Many columns: NaN and infinite scales past a row's end, before its window, in other blocks."""
+    rng = np.random.default_rng(d)
+    window, rows = 90, [(333, 80, None), (70, 70, None), (0, 40, 0), (200, 45, None)]
+    q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, rows, dtype)
+    want, mag, dots = K.attend(host(q), cache, table, kv, q_off, pos, d ** -0.5, window)
+    raw = cache.bytes[..., b * d:].copy().view(np.uint16).reshape(cache.n, hk, 2, b)
+    seen = np.zeros((cache.n, b), bool)
+    for r, (n, nq, _) in enumerate(rows):
+        for j in range(max(0, n - nq - window + 1), n):
+            seen[table[r, j // b], j % b] = True
+    raw = np.where(seen[:, None, None, :], raw, rng.choice(np.array([0x7fc0, 0x7f80, 0xff80, 0x7f7f], np.uint16), raw.shape))
+    cache.bytes[..., b * d:] = np.ascontiguousarray(raw).view(np.uint8).reshape(cache.n, hk, 4 * b)
+    with ctx_of(hq, hk, d, b, cache.n, table.shape[1], dtype) as ctx:
+        for hints in (dict(max_q=80, max_kv=333), dict()):
+            got = host(pkg.kv_attend(ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos), scale=d ** -0.5,
+                                     window=window, **hints))
+            assert (np.abs(got - want) <= bound(dtype, want, mag, dots, d, window)).all()
+
+
+@pytest.mark.parametrize("hq,hk,d,nq", [(8, 1, 64, 3), (8, 1, 128, 16), (16, 1, 128, 20), (4, 1, 256, 90)])
+def test_attend_few_queries_over_many_tokens(hq, hk, d, nq):
+    """One row in many shares, joined by the last workgroup or by a launch of its own."""
+    check_attend(hq, hk, d, 64, [(9000, nq, None)], seed=nq, hints=False)
+    check_attend(hq, hk, d, 64, [(2500, nq, None), (700, 1, None)], "f16", seed=nq, hints=False)
 
 
 def test_attend_cache_past_32_bits():
