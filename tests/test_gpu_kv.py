@@ -256,6 +256,13 @@ def test_store_many_tokens(hq, hk, d, b, longest, dtype):
     for t in np.nonzero(slot >= 0)[0]:
         want.put(slot[t], hk_[t], hv_[t])
     assert np.array_equal(one.cpu().numpy(), want.bytes.reshape(-1))     # the last: as given
+    # read back at once, in any order and from its middle, as a few at a time
+    many = np.concatenate([slot, slot[7:], rng.permutation(slot)] * (1 + 65536 // (2 * hk * 3 * T)))
+    want_k, want_v = want.get(np.maximum(many, 0))
+    with ctx_of(hq, hk, d, b, n, 4, dtype) as ctx:
+        for x, y in zip(pkg.kv_load(ctx, one, dev(many)), (want_k, want_v)):
+            y[many < 0] = 0
+            assert torch.equal(x.cpu(), torch.from_numpy(y).to(TYPES[dtype]))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
