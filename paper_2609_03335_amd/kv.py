@@ -187,9 +187,24 @@ def torch_type(dtype: int):
     return torch.bfloat16 if dtype == WF_KV_BF16 else torch.float16
 
 
+def _made_current(ctx: KVContext, stream):
+    """Makes a stream (torch's, or a handle) torch's current one, so that outputs are
+    allocated for it: their memory is not given to another stream's work while this one's runs."""
+    import torch
+    if isinstance(stream, int):
+        at = torch.device("cuda", ctx.device)
+        stream = torch.cuda.ExternalStream(stream, device=at) if stream else torch.cuda.default_stream(at)
+    return torch.cuda.stream(stream)
+
+
 def kv_step(ctx: KVContext, new_tokens, n_tokens: int, lens, pool, ring, table, stream=None):
     """Allocate the outputs of wf_kv_step and enqueue it.  table and ring are
-    updated in place; returns (lens, pool, q_off, slot, pos, granted)."""
+    updated in place; returns (lens, pool, q_off, slot, pos, granted).  Here and below,
+    `stream` (a torch stream or a handle; default: the current one) takes the work and
+    owns the outputs."""
+    if stream is not None:
+        with _made_current(ctx, stream):
+            return kv_step(ctx, new_tokens, n_tokens, lens, pool, ring, table)
     import torch
     r, empty = new_tokens.shape[0], new_tokens.new_empty
     # one allocation for the int32 outputs: lens, pool, q_off, pos
@@ -198,7 +213,7 @@ def kv_step(ctx: KVContext, new_tokens, n_tokens: int, lens, pool, ring, table, 
     granted = empty(r, dtype=torch.uint8)
     at = flat.data_ptr()
     ctx.wf_kv_step(new_tokens, r, n_tokens, lens, at, pool, at + 4 * r, ring, table, at + 4 * r + 8, slot.data_ptr(),
-                   at + 8 * r + 12, granted.data_ptr(), stream)
+                   at + 8 * r + 12, granted.data_ptr())
     lens_out, pool_out, q_off, pos = flat.split((r, 2, r + 1, n_tokens))
     return lens_out, pool_out, q_off, slot, pos, granted
 
@@ -207,19 +222,26 @@ def kv_store(ctx: KVContext, q, k, v, pos, slot, cache, cos_sin=None, *, rot_dim
              q_weight=None, k_weight=None, eps: float = 1e-6, stream=None):
     """Norm, rotate and store the tokens of q [T, q_heads, D], k and v [T,
     kv_heads, D]; returns the queries [T, q_heads, D]."""
+    if stream is not None:
+        with _made_current(ctx, stream):
+            return kv_store(ctx, q, k, v, pos, slot, cache, cos_sin, rot_dim=rot_dim, interleaved=interleaved,
+                            q_weight=q_weight, k_weight=k_weight, eps=eps)
     n = q.shape[0]
     out = q.new_empty((n, ctx.q_heads, ctx.head_dim))
     ctx.wf_kv_store(q, k, v, n, pos, slot, out.data_ptr(), cache, cos_sin=cos_sin,
                     n_pos=0 if cos_sin is None else cos_sin.shape[0], rot_dim=rot_dim, interleaved=interleaved,
-                    q_weight=q_weight, k_weight=k_weight, eps=eps, stream=stream)
+                    q_weight=q_weight, k_weight=k_weight, eps=eps)
     return out
 
 
 def kv_load(ctx: KVContext, cache, slot, stream=None):
     """The cached keys and values [T, kv_heads, D] at the given slots."""
+    if stream is not None:
+        with _made_current(ctx, stream):
+            return kv_load(ctx, cache, slot)
     n, shape = slot.shape[0], (slot.shape[0], ctx.kv_heads, ctx.head_dim)
     k, v = slot.new_empty(shape, dtype=ctx.torch_dtype), slot.new_empty(shape, dtype=ctx.torch_dtype)
-    ctx.wf_kv_load(cache, slot, n, k.data_ptr(), v.data_ptr(), stream)
+    ctx.wf_kv_load(cache, slot, n, k.data_ptr(), v.data_ptr())
     return k, v
 
 
@@ -227,8 +249,11 @@ def kv_attend(ctx: KVContext, q, cache, table, kv_len, q_off, pos, *, scale: flo
               max_kv: int = 0, stream=None):
     """Attention of the packed queries q [T, q_heads, D] over the cache:
     [T, q_heads, D].  Rows of tokens past q_off[-1] are not written."""
+    if stream is not None:
+        with _made_current(ctx, stream):
+            return kv_attend(ctx, q, cache, table, kv_len, q_off, pos, scale=scale, window=window, max_q=max_q, max_kv=max_kv)
     n = q.shape[0]
     out = q.new_empty((n, ctx.q_heads, ctx.head_dim))
     ctx.wf_kv_attend(q, n, cache, table, kv_len, q_off, pos, kv_len.shape[0], scale, out.data_ptr(), window=window,
-                     max_q=max_q, max_kv=max_kv, stream=stream)
+                     max_q=max_q, max_kv=max_kv)
     return out

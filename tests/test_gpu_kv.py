@@ -610,6 +610,32 @@ def test_streams_and_replays():
             assert torch.equal(out, eager[k % 2]), k
 
 
+@pytest.mark.parametrize("handle", [False, True])
+def test_outputs_belong_to_the_stream(handle):
+    """Outputs of a call on a given stream are that stream's memory: once dropped, the current
+    stream does not get it while the other may still write it."""
+    with ctx_of(4, 2, 64, 16, 8, 4) as ctx:
+        slot = torch.arange(64, device=DEV)
+        cache = torch.zeros(ctx.cache_bytes, dtype=torch.uint8, device=DEV)
+        off, lens = torch.tensor([0, 64], dtype=torch.int32, device=DEV), torch.tensor([64], dtype=torch.int32, device=DEV)
+        table, q = torch.arange(4, dtype=torch.int32, device=DEV)[None], torch.ones(64, 4, 64, dtype=torch.bfloat16, device=DEV)
+        kv = q[:, :2].contiguous()
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        on = dict(stream=s.cuda_stream if handle else s)
+        for call in (lambda: pkg.kv_load(ctx, cache, slot, **on)[0], lambda: pkg.kv_store(ctx, q, kv, kv, None, slot, cache, **on),
+                     lambda: pkg.kv_attend(ctx, q, cache, table, lens, off, slot.int(), scale=0.125, **on),
+                     lambda: pkg.kv_step(ctx, lens, 64, lens, off[:2].clone(), torch.arange(8, dtype=torch.int32, device=DEV),
+                                         table.clone(), **on)[3]):
+            out = call()
+            shape, kind, at = out.shape, out.dtype, out.data_ptr()
+            del out
+            assert torch.empty(shape, dtype=kind, device=DEV).data_ptr() != at
+            with torch.cuda.stream(s):
+                assert abs(torch.empty(shape, dtype=kind, device=DEV).data_ptr() - at) < 2 << 20    # its segment
+        torch.cuda.synchronize()
+
+
 def test_refusals():
     hq, hk, d, b = 4, 2, 64, 16
     with ctx_of(hq, hk, d, b, 8, 4) as ctx:
