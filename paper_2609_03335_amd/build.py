@@ -12,6 +12,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libwfplan.so"
 LIB_PATH = os.path.join(PKG, LIB_NAME)
+BIND_PATH = os.path.join(PKG, "_kvbind.so")
 SOURCES = ["host.hip", "score.hip", "score_keys.hip", "argmin.hip", "prefix.hip", "lean.hip",
            "lanes.hip", "kv_host.hip", "kv_step.hip", "kv_store.hip", "kv_attend.hip"]
 ARCH = "gfx950"
@@ -38,6 +39,19 @@ def flags(src: str) -> list:
     return [f for f in HIP_FLAGS if "sched-strategy" not in f and f != "-mllvm"]
 
 
+def bind_command(out: str) -> list:
+    """Compiler call for _kvbind.so, the short way from torch tensors to the cache's calls: host
+    code only, against the headers and libraries of the installed torch."""
+    import sysconfig
+    import torch
+    at = os.path.dirname(torch.__file__)
+    lib = os.path.join(at, "lib")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+            "-I", os.path.join(at, "include"), "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+            "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "kv_bind.cpp"), "-o", out,
+            "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10"]
+
 
 def hipcc() -> str:
     for c in (os.environ.get("HIPCC"), "/opt/rocm/bin/hipcc", shutil.which("hipcc")):
@@ -48,7 +62,7 @@ def hipcc() -> str:
 
 def build(verbose: bool = False) -> str:
     """Compile every HIP source for gfx950 and link libwfplan.so next to
-    this file.  Always recompiles."""
+    this file, and _kvbind.so beside it.  Always recompiles."""
     build_dir = os.path.join(PKG, "_build")
     os.makedirs(build_dir, exist_ok=True)
     objs = []
@@ -60,6 +74,8 @@ def build(verbose: bool = False) -> str:
             print(" ".join(cmd), file=sys.stderr)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
         objs.append(obj)
+    bind = os.path.join(build_dir, "_kvbind.so")
+    procs.append(("kv_bind.cpp", subprocess.Popen(bind_command(bind), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     errors = []
     for src, p in procs:
         out, _ = p.communicate()
@@ -75,6 +91,7 @@ def build(verbose: bool = False) -> str:
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     subprocess.check_call(cmd)
     os.replace(tmp, LIB_PATH)
+    os.replace(bind, BIND_PATH)
     return LIB_PATH
 
 

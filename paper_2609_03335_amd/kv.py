@@ -1,6 +1,11 @@
 """The paged 4-bit key/value cache of a replica: binding of include/wf_kv.h
 (same names) and helpers that allocate the outputs.  Only marshalling: every
 step runs in the gfx950 kernels.
+
+The helpers take sound tensors through _kvbind (csrc/kv_bind.cpp), which checks, allocates and calls
+in one step: a step of 64 rows takes 14 us through ctypes, a call of attention 9.5.  What it
+does not take at once (addresses, other strides, wrong arguments) goes through
+KVContext's methods, which accept it or say what is wrong.
 """
 from __future__ import annotations
 
@@ -49,7 +54,11 @@ class KVContext:
         self.block_tokens, self.n_blocks, self.max_blocks = block_tokens, n_blocks, max_blocks
         self.dtype, self.torch_dtype = d.dtype, torch_type(d.dtype)
         self._current = _current_stream()
+        self._bind = _bind() if self._current is not None else None
         self.cache_bytes = n_blocks * kv_heads * block_tokens * (head_dim + 4)
+        if self._bind is not None:
+            self._geometry = self._bind.geometry(h.value, device, q_heads, kv_heads, head_dim, n_blocks, max_blocks,
+                                                 self.cache_bytes, d.dtype == WF_KV_F16)
 
     def _check(self, st):
         if st != WF_OK:
@@ -157,6 +166,7 @@ class KVContext:
             self._wide(out, 2 * n * self.q_heads * self.head_dim, "out"), self._s(stream)))
 
     def close(self):
+        self._bind = None
         if getattr(self, "handle", None):
             self.lib.wf_kv_ctx_destroy(self.handle)
             self.handle = None
@@ -172,6 +182,20 @@ class KVContext:
             self.close()
         except Exception:
             pass
+
+
+@functools.lru_cache(maxsize=None)
+def _bind():
+    """The module _kvbind with the library's calls, None where it was not built."""
+    import torch  # noqa: F401  (its libraries are _kvbind's)
+    try:
+        from . import _kvbind
+    except ImportError:
+        return None
+    lib = load()
+    _kvbind.calls(*(ctypes.cast(f, ctypes.c_void_p).value
+                    for f in (lib.wf_kv_step, lib.wf_kv_store, lib.wf_kv_load, lib.wf_kv_attend)))
+    return _kvbind
 
 
 def _current_stream():
@@ -205,6 +229,12 @@ def kv_step(ctx: KVContext, new_tokens, n_tokens: int, lens, pool, ring, table, 
     if stream is not None:
         with _made_current(ctx, stream):
             return kv_step(ctx, new_tokens, n_tokens, lens, pool, ring, table)
+    if ctx._bind is not None:
+        out = ctx._bind.step(ctx._geometry, ctx._current(ctx.device), new_tokens, n_tokens, lens, pool, ring, table)
+        if out is not None:
+            if out.__class__ is int:
+                ctx._check(out)
+            return out
     import torch
     r, empty = new_tokens.shape[0], new_tokens.new_empty
     # one allocation for the int32 outputs: lens, pool, q_off, pos
@@ -226,6 +256,13 @@ def kv_store(ctx: KVContext, q, k, v, pos, slot, cache, cos_sin=None, *, rot_dim
         with _made_current(ctx, stream):
             return kv_store(ctx, q, k, v, pos, slot, cache, cos_sin, rot_dim=rot_dim, interleaved=interleaved,
                             q_weight=q_weight, k_weight=k_weight, eps=eps)
+    if ctx._bind is not None:
+        out = ctx._bind.store(ctx._geometry, ctx._current(ctx.device), q, k, v, pos, slot, cache, cos_sin, rot_dim,
+                              interleaved, q_weight, k_weight, eps)
+        if out is not None:
+            if out.__class__ is int:
+                ctx._check(out)
+            return out
     n = q.shape[0]
     out = q.new_empty((n, ctx.q_heads, ctx.head_dim))
     ctx.wf_kv_store(q, k, v, n, pos, slot, out.data_ptr(), cache, cos_sin=cos_sin,
@@ -239,6 +276,12 @@ def kv_load(ctx: KVContext, cache, slot, stream=None):
     if stream is not None:
         with _made_current(ctx, stream):
             return kv_load(ctx, cache, slot)
+    if ctx._bind is not None:
+        out = ctx._bind.load(ctx._geometry, ctx._current(ctx.device), cache, slot)
+        if out is not None:
+            if out.__class__ is int:
+                ctx._check(out)
+            return out
     n, shape = slot.shape[0], (slot.shape[0], ctx.kv_heads, ctx.head_dim)
     k, v = slot.new_empty(shape, dtype=ctx.torch_dtype), slot.new_empty(shape, dtype=ctx.torch_dtype)
     ctx.wf_kv_load(cache, slot, n, k.data_ptr(), v.data_ptr())
@@ -252,6 +295,13 @@ def kv_attend(ctx: KVContext, q, cache, table, kv_len, q_off, pos, *, scale: flo
     if stream is not None:
         with _made_current(ctx, stream):
             return kv_attend(ctx, q, cache, table, kv_len, q_off, pos, scale=scale, window=window, max_q=max_q, max_kv=max_kv)
+    if ctx._bind is not None:
+        out = ctx._bind.attend(ctx._geometry, ctx._current(ctx.device), q, cache, table, kv_len, q_off, pos, scale, window,
+                               max_q, max_kv)
+        if out is not None:
+            if out.__class__ is int:
+                ctx._check(out)
+            return out
     n = q.shape[0]
     out = q.new_empty((n, ctx.q_heads, ctx.head_dim))
     ctx.wf_kv_attend(q, n, cache, table, kv_len, q_off, pos, kv_len.shape[0], scale, out.data_ptr(), window=window,

@@ -636,6 +636,52 @@ def test_outputs_belong_to_the_stream(handle):
         torch.cuda.synchronize()
 
 
+def test_both_ways_of_a_call_agree(monkeypatch):
+    """The helpers through _kvbind and through ctypes: the same outputs, the same refusals."""
+    rng = np.random.default_rng(31)
+    hq, hk, d, b = 8, 2, 64, 16
+    q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, [(90, 3, None), (40, 1, None), (17, 17, None)], "bf16")
+    lens, new, tb, ring, pool = random_step(rng, 70, b, table.shape[1], 0.7)
+    with ctx_of(hq, hk, d, b, cache.n, table.shape[1]) as ctx, ctx_of(hq, hk, d, b, len(ring), table.shape[1]) as sctx:
+        assert ctx._bind is not None, "_kvbind is not built"
+        c, x = dev(cache.bytes), dev(rng.standard_normal((21, hk, d)).astype(np.float32), torch.bfloat16)
+        w, cs = torch.ones(d, dtype=torch.bfloat16, device=DEV), torch.rand(99, d, device=DEV)
+        slot, p = dev(rng.permutation(cache.n * b)[:21]), dev(pos)
+        tokens = int(np.maximum(new, 0).sum())
+
+        def calls():
+            mine, r, t = c.clone(), dev(ring), dev(tb)
+            return [pkg.kv_attend(ctx, q, c, dev(table), dev(kv), dev(q_off), p, scale=0.125, window=20, max_q=17, max_kv=90),
+                    pkg.kv_store(ctx, q, x, x, p, slot, mine, cs, rot_dim=d, q_weight=w), mine, *pkg.kv_load(ctx, c, slot),
+                    *pkg.kv_step(sctx, dev(new), tokens, dev(lens), dev(pool), r, t), r, t]
+        bad = [(lambda: pkg.kv_load(ctx, c, slot.int()), TypeError), (lambda: pkg.kv_load(ctx, c.cpu(), slot), ValueError),
+               (lambda: pkg.kv_load(ctx, c.flatten()[:-1], slot), ValueError),
+               (lambda: pkg.kv_store(ctx, q, x[:-1], x, p, slot, c), ValueError),
+               (lambda: pkg.kv_store(ctx, q.half(), x, x, p, slot, c), TypeError),
+               (lambda: pkg.kv_store(ctx, q, x, x, p, slot, c, eps=-1.0), pkg.WFError),
+               (lambda: pkg.kv_attend(ctx, q, c, dev(table), dev(kv), dev(q_off), p, scale=float("nan")), pkg.WFError),
+               (lambda: pkg.kv_attend(ctx, q, c, dev(table), dev(kv), dev(q_off), p, scale=0.1, window=-1), pkg.WFError),
+               (lambda: pkg.kv_step(sctx, dev(new), -1, dev(lens), dev(pool), dev(ring), dev(tb)), (pkg.WFError, RuntimeError)),
+               (lambda: pkg.kv_step(sctx, dev(new), tokens, dev(lens)[:-1], dev(pool), dev(ring), dev(tb)), ValueError)]
+        results = []
+        for way in (ctx._bind, None):
+            monkeypatch.setattr(ctx, "_bind", way)
+            monkeypatch.setattr(sctx, "_bind", way)
+            results.append(calls())
+            for call, error in bad:
+                with pytest.raises(error):
+                    call()
+        assert len(results[0]) == len(results[1]) == 13
+        for one, two in zip(*results):
+            assert one.shape == two.shape and one.dtype == two.dtype and torch.equal(one, two)
+        # addresses, an integer scale and a 2-D view go the longer way
+        monkeypatch.undo()
+        assert torch.equal(pkg.kv_attend(ctx, q.flatten(1), c, dev(table), dev(kv), dev(q_off), p, scale=1),
+                           pkg.kv_attend(ctx, q, c, dev(table), dev(kv), dev(q_off), p, scale=1.0))
+    with pytest.raises(pkg.WFError):
+        pkg.kv_load(ctx, c, slot)                          # closed
+
+
 def test_refusals():
     hq, hk, d, b = 4, 2, 64, 16
     with ctx_of(hq, hk, d, b, 8, 4) as ctx:
