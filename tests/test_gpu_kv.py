@@ -95,6 +95,34 @@ def test_step_one_long_prompt():
     check_step(lens, new, table, ring, np.array([n - 10, 7500], np.int32), b)
 
 
+@pytest.mark.parametrize("rows", [40, 5000])
+def test_step_sums_past_32_bits(rows):
+    """Rows that ask for far more than fits: offsets stop at 2^31 - 1, later rows are placed as if
+    they were right; needs beyond 2^32 blocks in all leave nothing for the rows after."""
+    b, n = 16, 9
+    new = np.ones(rows, np.int32)
+    new[:7] = 2 ** 31 - 1
+    off = np.minimum(np.concatenate([[0], np.cumsum(new.astype(np.int64))]), 2 ** 31 - 1)
+    with ctx_of(b=b, n=n, width=4) as ctx:
+        table = torch.full((rows, 4), -1, dtype=torch.int32, device=DEV)
+        ring, pool = torch.arange(n, dtype=torch.int32, device=DEV), torch.tensor([0, n], dtype=torch.int32, device=DEV)
+        lens, pool, q_off, slot, pos, granted = pkg.kv_step(ctx, dev(new), 300, dev(np.zeros(rows, np.int32)), pool, ring, table)
+        assert np.array_equal(q_off.cpu().numpy(), off)
+        want = np.zeros(rows, np.int32)
+        want[7:7 + n] = 1
+        assert np.array_equal(granted.cpu().numpy(), want) and np.array_equal(lens.cpu().numpy(), want)
+        assert pool.tolist() == [0, 0] and (slot == -1).all() and np.array_equal(pos.cpu().numpy(), np.arange(300))
+        assert table[7:7 + n, 0].tolist() == list(range(n)) and (table[7:7 + n, 1:] == -1).all()
+    width, rows = 1 << 22, 1100 if rows == 40 else 4200
+    with ctx_of(b=b, n=n, width=width) as ctx:
+        new = dev(np.full(rows, width * b, np.int32))
+        new[-1] = 1
+        table = torch.empty(rows, width, dtype=torch.int32, device=DEV)
+        pool = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+        lens, pool, q_off, slot, pos, granted = pkg.kv_step(ctx, new, 10, torch.zeros_like(new), pool, ring, table)
+        assert not granted.any() and not lens.any() and pool.tolist() == [0, n] and (slot == -1).all()
+
+
 def test_step_invalid_device_values_stay_in_bounds():
     """Lengths, counters and ring contents outside their range: unspecified
     results, but nothing outside the arrays is written."""
