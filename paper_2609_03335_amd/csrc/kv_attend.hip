@@ -126,14 +126,20 @@ struct Pages {
 struct Split {
   int tiles, splits;  // of the launch: column tiles of a row, shares of its tokens
   float* part;        // [splits][n_tokens][hq][D + 2] sums, reference, total
-  int32_t* used;      // more than kFused shares: [n_tokens][hq] shares written; 1: the output is done
-  int32_t* arrived;   // at most kFused: [n_rows][tiles][hk] shares done; 0 before and after a launch
+  int32_t* used;      // joined by a kernel: [n_tokens][hq] shares written; 1: the output is done
+  int32_t* arrived;   // by the last workgroup: [n_rows][tiles][hk] shares done; 0 before and after a launch
 };
 
-// Up to this many shares are joined by the workgroup that is done last, more by a kernel
-// of their own, with a workgroup for each head: 4 shares of one token over 1,000 cached
-// take 10 us against 14, but 16 of 32 tokens over 6,000 49 against 20.
-constexpr int kFused = 8;
+// Up to this many shares of 16 columns are joined by the workgroup that is done last, more (or of
+// more columns, which it would take one after the other) by a kernel of their own, with a
+// workgroup for each head: one token over 1,000 cached ones (4 shares) takes 8.6 us against 9.5, over
+// 2,000 (8) 10.8 against 9.5; 24 tokens (48 columns) over 1,000 18.7 against 12.8, over 2,000 26 against 13.
+template <int C>
+constexpr int kFused = C == 1 ? 4 : 1;
+
+// Units of a row that a narrow workgroup takes without sharing: two a wave cost less than a
+// join (one token over 500: 7.2 us against 8.1 for two shares).
+constexpr int kAlone = 2 * kWaves;
 
 // Partial sums go past the caches that the dies do not share, both ways: a release and an
 // acquire that write those back and empty them for every workgroup cost more than the
@@ -268,7 +274,7 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
     const int first = lo_min >> 6, units = max(0, ((hi_max + 63) >> 6) - first);
     // (a tile past those the launch knew of is not shared: its count would be another's)
     const int splits = tile < sp.tiles ? sp.splits : 1;
-    const int share = max(kWaves, (units + splits - 1) / splits);
+    const int share = units <= kAlone ? kAlone : max(kWaves, (units + splits - 1) / splits);
     const int used = max(1, (units + share - 1) / share);
     if (split >= used) continue;
     const int end = first + min(units, (split + 1) * share);
@@ -462,11 +468,11 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
           put(to + at + 2, v[2], v[3]);
           if (at == 0) put(to + D, m, total);
         }
-        if (at == 0 && split == 0 && sp.splits > kFused) sp.used[head] = used;
+        if (at == 0 && split == 0 && sp.splits > kFused<C>) sp.used[head] = used;
       }
       __syncthreads();
     }
-    if (used > 1 && sp.splits <= kFused)
+    if (used > 1 && sp.splits <= kFused<C>)
       join_item<D, M>(g, a, sp, row, tile, kvh, q0, tile * 16 * C, columns, 16 * C, used, &last);
   }
 }
@@ -948,9 +954,10 @@ __global__ __launch_bounds__(kThreads) void combine(Geo g, AttendArgs a, Split s
 constexpr int64_t kMostGrid = 1 << 22;
 
 // Column tiles, shares and work area of a launch whose workgroups take `tile` columns;
-// `want` workgroups fill the chip.
+// `want` workgroups fill the chip; rows of up to `alone` units are not shared.
 template <int D>
-Split split_of(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, int tile, int64_t want) {
+Split split_of(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, int tile, int64_t want,
+               int alone) {
   const int64_t most_kv = (int64_t)g.width * g.b;
   const int64_t max_kv = a.max_kv > 0 ? std::min((int64_t)a.max_kv, most_kv) : most_kv;
   Split sp;
@@ -961,7 +968,7 @@ Split split_of(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t c
   const int64_t heads = (int64_t)a.n_tokens * g.hq, units = (max_kv + 63) / 64;
   int64_t splits = std::min({want / items, (units + kWaves - 1) / kWaves,
                              (int64_t)(w.part_bytes / (heads * (D + 2) * 4))});
-  if (std::max(heads, items) > (int64_t)(w.count_bytes / 4)) splits = 1;
+  if (units <= alone || std::max(heads, items) > (int64_t)(w.count_bytes / 4)) splits = 1;
   sp.splits = (int)std::max<int64_t>(1, splits);
   sp.part = w.part;
   sp.used = w.used;
@@ -989,9 +996,9 @@ hipError_t launch(K kernel, const Geo& g, const AttendArgs& a, const Split& sp, 
 // token over 200,001 cached: 53 us at 3 workgroups a CU, 61 at 6, 77 at 12).
 template <int D, int C, class M>
 hipError_t narrow(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, hipStream_t s) {
-  const Split sp = split_of<D>(g, a, w, columns, 16 * C, w.n_cu * kOcc<D, C>);
+  const Split sp = split_of<D>(g, a, w, columns, 16 * C, w.n_cu * kOcc<D, C>, kAlone);
   const hipError_t e = launch(attend<D, C, M>, g, a, sp, kThreads, s);
-  if (e != hipSuccess || sp.splits <= kFused) return e;
+  if (e != hipSuccess || sp.splits <= kFused<C>) return e;
   // (heads x 256 threads: shares are only taken of up to kCountBytes / 4 heads)
   hipLaunchKernelGGL((combine<D, kThreads / (D / 4), M>), dim3((unsigned)(a.n_tokens * g.hq)), dim3(kThreads), 0, s, g, a, sp);
   return hipGetLastError();
@@ -1000,7 +1007,7 @@ hipError_t narrow(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_
 template <int D, class M>
 hipError_t wide(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, hipStream_t s) {
   constexpr int C = D == 256 ? 1 : 2, W = D == 256 ? 4 : 8, H = kThreads / (D / 4);
-  const Split sp = split_of<D>(g, a, w, columns, 16 * C * W, w.n_cu * 2);
+  const Split sp = split_of<D>(g, a, w, columns, 16 * C * W, w.n_cu * 2, kWaves);
   const hipError_t e = launch(attend_wide<D, C, W, M>, g, a, sp, 64 * W, s);
   if (e != hipSuccess || sp.splits == 1) return e;
   const int64_t heads = (int64_t)a.n_tokens * g.hq;
