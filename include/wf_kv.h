@@ -168,8 +168,8 @@ wf_status wf_kv_load(wf_kv_ctx *ctx, const uint8_t *cache, const int64_t *slot, 
  * kv_len int32 [n_rows]; q_off int32 [n_rows + 1]; pos int32 [n_tokens].  Tokens
  * from q_off[n_rows] on are not written.
  * max_q and max_kv are hints for the launch: the most queries and the most cached
- * tokens of a row (0: not known).  Results are right whatever they are; too
- * low or too high ones cost time.
+ * tokens of a row (0: not known).  Results are right whatever they are, to the
+ * roundings of the kernel taken; unknown, too low or too high ones cost time.
  * Products are of 16-bit values with fp32 sums; the softmax is fp32, its
  * probabilities times the value scales are rounded to the 16-bit type.  Sums are
  * divided by the softmax's total at their end: with bf16, values must stay below

@@ -991,7 +991,7 @@ hipError_t launch(K kernel, const Geo& g, const AttendArgs& a, const Split& sp, 
   return hipSuccess;
 }
 
-// Up to 128 columns a row (1 or 2 tiles of 16 a workgroup); the tokens are split so that all
+// Few columns (1 or 2 tiles of 16 a workgroup); the tokens are split so that all
 // workgroups run at once.  Shares above that cost more than the balance that they bring (one
 // token over 200,001 cached: 53 us at 3 workgroups a CU, 61 at 6, 77 at 12).
 template <int D, int C, class M>
@@ -1021,7 +1021,13 @@ hipError_t by_columns(const Geo& g, const AttendArgs& a, const AttendWork& w, hi
   // 32 rows over up to 6,000 tokens: 49 us narrow against 178 wide for 5 tokens each (20
   // columns), 133 against 190 for 32 (128 columns); one such row 20 against 36
   if (columns <= 16) return narrow<D, 1, M>(g, a, w, columns, s);
-  if (columns <= 128) return narrow<D, 2, M>(g, a, w, columns, s);
+  // More columns too where narrow workgroups run all at once and their tokens are not many: a wide one's
+  // pipeline and LDS take 10 us and more to fill.  32 heads of 128 channels, narrow against wide:
+  // a prompt of 256 9.0 and 21 us, of 400 12 and 27, 128 tokens over 4,000 28 and 40, 256 over 4,000
+  // 44 and 46, over 16,000 109 and 92; 16 prompts of 400 (more than at once) 52 and 43.
+  const int64_t at_once = w.n_cu * kOcc<D, 2>, narrow_wgs = (int64_t)a.n_rows * g.hk * ((columns + 31) / 32);
+  const bool few = a.max_kv > 0 && narrow_wgs <= at_once && narrow_wgs * a.max_kv <= at_once * 3500;
+  if (columns <= 128 || few) return narrow<D, 2, M>(g, a, w, columns, s);
   return wide<D, M>(g, a, w, columns, s);
 }
 

@@ -513,13 +513,14 @@ def test_attend_prompts_of_uneven_scores(hq, hk, d, dtype):
         q, cache, table, kv, q_off, pos = skewed_case(rng, hq, hk, d, b, n, nq, dtype, far, size)
         want, mag, dots = K.attend(host(q), cache, table, kv, q_off, pos, d ** -0.5, 0)
         with ctx_of(hq, hk, d, b, cache.n, table.shape[1], dtype) as ctx:
-            got = host(pkg.kv_attend(ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos), scale=d ** -0.5,
-                                     max_q=nq, max_kv=n))
+            both = [host(pkg.kv_attend(ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos), scale=d ** -0.5,
+                                       **hints)) for hints in (dict(max_q=nq, max_kv=n), dict())]
         # as bound(); for f16, a probability times its value scale is rounded to a step of 2^-25 of a
         # total that may be as small as 2^-8 (the reference is within 8 powers of two of the largest score)
         lim = bound(dtype, want, mag, dots, d, n) + (6 * n * 2.0 ** -17 if dtype == "f16" else 0.0)
-        assert np.isfinite(got).all(), i
-        assert (np.abs(got - want) <= lim).all(), (i, float((np.abs(got - want) / lim).max()))
+        for got in both:
+            assert np.isfinite(got).all(), i
+            assert (np.abs(got - want) <= lim).all(), (i, float((np.abs(got - want) / lim).max()))
 
 
 def test_floats_are_not_taken_for_integers():
@@ -578,8 +579,9 @@ def test_attend_prompts_beside_garbage(hq, hk, d, b, dtype):
 @pytest.mark.parametrize("hq,hk,d,nq", [(8, 1, 64, 3), (8, 1, 128, 16), (16, 1, 128, 20), (4, 1, 256, 90)])
 def test_attend_few_queries_over_many_tokens(hq, hk, d, nq):
     """One row in many shares, joined by the last workgroup or by a launch of its own."""
-    check_attend(hq, hk, d, 64, [(9000, nq, None)], seed=nq, hints=False)
-    check_attend(hq, hk, d, 64, [(2500, nq, None), (700, 1, None)], "f16", seed=nq, hints=False)
+    check_attend(hq, hk, d, 64, [(9000, nq, None)], seed=nq)
+    check_attend(hq, hk, d, 64, [(2500, nq, None), (700, 1, None)], "f16", seed=nq)
+    check_attend(hq, hk, d, 64, [(600, nq, None), (400, nq, None), (1300, 3, None)], "f16", seed=nq, window=450)
 
 
 def test_attend_cache_past_32_bits():
