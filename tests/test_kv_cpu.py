@@ -114,3 +114,24 @@ def test_oracle_cache_round_trip():
     for got, x in ((gk[0], k), (gv[0], v)):
         code, bits = K.quantised(x)
         assert np.array_equal(got, K.values(code) * (bits.astype(np.uint32) << 16).view(np.float32)[..., None])
+
+
+def test_native_binding_leaves_what_it_does_not_take():
+    """_kvbind takes sound GPU tensors only: None for all else, before any call."""
+    import torch
+    from paper_2609_03335_amd import build
+    if not os.path.exists(build.BIND_PATH):
+        build.build()
+    from paper_2609_03335_amd import _kvbind as kb
+    g = kb.geometry(0, 0, 8, 2, 64, 10, 4, 10 * 2 * 16 * 68, False)
+    cache, slot, i = torch.zeros(10 * 2 * 16 * 68, dtype=torch.uint8), torch.zeros(3, dtype=torch.int64), torch.zeros(4, dtype=torch.int32)
+    q = torch.zeros(3, 8, 64, dtype=torch.bfloat16)
+    assert kb.load(g, 0, cache, slot) is None              # tensors of the host
+    assert kb.load(g, 0, 4096, 4096) is None               # addresses
+    assert kb.load(g, 0, cache) is None and kb.load() is None and kb.load(None, 0, cache, slot) is None
+    assert kb.load("geometry", 0, cache, slot) is None and kb.load(g, -1, cache, slot) is None
+    assert kb.step(g, 0, i, 3, i, i, i, i) is None and kb.step(g, 0, None, 1 << 40, i, i, i, i) is None
+    assert kb.attend(g, 0, q, cache, i, i, i, i, 1.0, 0, 0, 0) is None
+    assert kb.store(g, 0, q, q, q, i, slot, cache, None, 0, False, None, None, 1e-6) is None
+    with pytest.raises(TypeError):
+        kb.geometry(0)
