@@ -640,6 +640,51 @@ def test_streams_and_replays():
             assert torch.equal(out, eager[k % 2]), k
 
 
+@pytest.mark.parametrize("prompt", [1, 90])
+def test_a_whole_step_replays(prompt):
+    """Step, store, attention and load in one graph, replayed with other keys, values and queries: what
+    the same calls give one after the other."""
+    rng = np.random.default_rng(41)
+    hq, hk, d, b, rows, width = 8, 2, 64, 16, 12, 40
+    lens = rng.integers(0, 400, rows).astype(np.int32)
+    new = np.where(rng.random(rows) < 0.3, prompt, 1).astype(np.int32)
+    new[3] = -1
+    have = -(-lens // b)
+    n = int(have.sum()) + rows * (1 + prompt // b)
+    ids, at, table = rng.permutation(n).astype(np.int32), 0, np.full((rows, width), -1, np.int32)
+    for r in range(rows):
+        table[r, :have[r]] = ids[at:at + have[r]]
+        at += have[r]
+    ring = np.roll(np.concatenate([ids[at:], np.full(at, -1, np.int32)]), 7)
+    T = int(np.maximum(new, 0).sum())
+    raw = K.Cache(n, hk, b, d, rng).bytes
+    raw[..., b * d:] = K.bf16(rng.uniform(0.1, 0.4, (n, hk, 2 * b)).astype(np.float32))[1].view(np.uint8).reshape(n, hk, 4 * b)
+    inputs = [[dev(rng.standard_normal((T, h, d)).astype(np.float32), torch.bfloat16) for h in (hq, hk, hk)] for _ in range(2)]
+    cs = torch.rand(width * b, d, device=DEV)
+    with ctx_of(hq, hk, d, b, n, width) as ctx:
+        fresh, ln, pool = dev(new), dev(lens), dev(np.array([7, n - at], np.int32))
+
+        def step(qkv, cache, rg, tb):
+            out_lens, out_pool, q_off, slot, pos, granted = pkg.kv_step(ctx, fresh, T, ln, pool, rg, tb)
+            q = pkg.kv_store(ctx, *qkv, pos, slot, cache, cs, rot_dim=d)
+            o = pkg.kv_attend(ctx, q, cache, tb, out_lens, q_off, pos, scale=0.125, max_q=prompt, max_kv=500)
+            return [out_lens, out_pool, q_off, slot, pos, granted, q, o, *pkg.kv_load(ctx, cache, slot), cache, rg, tb]
+        eager = [[x.clone() for x in step(qkv, dev(raw), dev(ring), dev(table))] for qkv in inputs]
+        held, cache, rg, tb = [x.clone() for x in inputs[0]], dev(raw), dev(ring), dev(table)
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            out = step(held, cache, rg, tb)
+        for k in range(6):
+            for x, y in zip((*held, cache, rg, tb), (*inputs[k % 2], dev(raw), dev(ring), dev(table))):
+                x.copy_(y)
+            step(inputs[1 - k % 2], dev(raw), dev(ring), dev(table))     # eager work of the same context between
+            graph.replay()
+            torch.cuda.synchronize()
+            for i, (x, y) in enumerate(zip(out, eager[k % 2])):
+                assert torch.equal(x, y), (k, i)
+
+
 @pytest.mark.parametrize("handle", [False, True])
 def test_outputs_belong_to_the_stream(handle):
     """Outputs of a call on a given stream are that stream's memory: once dropped, the current
