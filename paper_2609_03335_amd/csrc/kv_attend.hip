@@ -30,6 +30,8 @@
 #include <type_traits>
 
 #include "kv.h"
+#include "kv_sight.h"
+
 namespace wfkv {
 namespace {
 
@@ -251,9 +253,8 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
                                                         (int64_t)(kvh * g.group + h) * D + grp * (D / 4));
 #pragma unroll
       for (int k = 0; k < KS; ++k) q[c][k] = src[k];
-      const int p = a.pos[q0 + i];
-      hi[c] = p < 0 ? 0 : min(len, p < INT32_MAX ? p + 1 : p);
-      lo[c] = a.window && p >= a.window ? p - a.window + 1 : 0;
+      const Sight see = sight_of(a.pos[q0 + i], len, a.window);
+      lo[c] = see.lo, hi[c] = see.hi;
       lo_min = min(lo_min, lo[c]);
       lo_max = max(lo_max, lo[c]);
       hi_min = min(hi_min, hi[c]);
@@ -540,9 +541,8 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
                                                         (int64_t)(kvh * g.group + h) * D + grp * (D / 4));
 #pragma unroll
       for (int k = 0; k < KS; ++k) q[c][k] = src[k];
-      const int p = a.pos[q0 + i];
-      hi[c] = p < 0 ? 0 : min(len, p < INT32_MAX ? p + 1 : p);
-      lo[c] = a.window && p >= a.window ? p - a.window + 1 : 0;
+      const Sight see = sight_of(a.pos[q0 + i], len, a.window);
+      lo[c] = see.lo, hi[c] = see.hi;
       lo_min = min(lo_min, lo[c]);
       lo_max = max(lo_max, lo[c]);
       hi_min = min(hi_min, hi[c]);

@@ -813,3 +813,27 @@ def test_refusals():
         with pytest.raises(pkg.WFError):
             ctx.wf_kv_load(cache, None, 3, k, k)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d", [(8, 2, 64), (4, 2, 128), (4, 2, 256)])
+def test_attend_positions_past_every_window(hq, hk, d, dtype):
+    """Positions as far as the largest integer, for rows of any length: nothing is seen through a window, the whole
+    row without one; by the kernel of few columns and by that of many, among sound queries of the same call."""
+    rng = np.random.default_rng(d)
+    top = 2 ** 31 - 1
+    for queries in (1, 70):
+        rows = [(90, queries, None), (300, queries, None), (0, queries, 0), (40, queries, -queries)]
+        q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, 16, rows, dtype)
+        far = pos.copy()
+        far[:q_off[2]] = top - np.arange(q_off[2]) % 3 * 300
+        mixed = np.where(np.arange(len(pos)) % 2 == 0, far, pos)
+        with ctx_of(hq, hk, d, 16, cache.n, table.shape[1], dtype) as ctx:
+            for p in (far, mixed):
+                for window in (0, 1, 64, top):
+                    want, mag, dots = K.attend(host(q), cache, table, kv, q_off, p.astype(np.int64), d ** -0.5, window)
+                    for hints in (dict(max_q=queries, max_kv=300), dict()):
+                        got = host(pkg.kv_attend(ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(p.astype(np.int32)),
+                                                 scale=d ** -0.5, window=window, **hints))
+                        assert (np.abs(got - want) <= bound(dtype, want, mag, dots, d, 300)).all(), (queries, window)
+                        assert (got[mag.sum(-1) == 0] == 0).all()

@@ -135,3 +135,41 @@ def test_native_binding_leaves_what_it_does_not_take():
     assert kb.store(g, 0, q, q, q, i, slot, cache, None, 0, False, None, None, 1e-6) is None
     with pytest.raises(TypeError):
         kb.geometry(0)
+
+
+@pytest.fixture(scope="module")
+def sight(tmp_path_factory):
+    """csrc/kv_sight.h, the kernels' own arithmetic, compiled for the host."""
+    import subprocess
+    at = tmp_path_factory.mktemp("sight")
+    (at / "sight.cpp").write_text('#include "kv_sight.h"\nextern "C" void sight(int p, int len, int window, int* to) '
+                                  '{ const wfkv::Sight s = wfkv::sight_of(p, len, window); to[0] = s.lo, to[1] = s.hi; }\n')
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2609_03335_amd", "csrc"),
+                           str(at / "sight.cpp"), "-o", str(at / "sight.so")])
+    lib = ctypes.CDLL(str(at / "sight.so"))
+
+    def call(p, length, window):
+        to = (ctypes.c_int * 2)()
+        lib.sight(p, length, window, to)
+        return to[0], to[1]
+    return call
+
+
+def test_sight_of_any_position_stays_in_the_row(sight):
+    """Positions of a device array may be anything: no token index that follows from one (units of
+    64 tokens, up to 16 units asked ahead) leaves 32 bits, and what is seen is the definition's."""
+    top = 2 ** 31 - 1
+    lengths = [0, 1, 63, 64, 65, 1000, 2 ** 30 - 1, 2 ** 30]
+    for length in lengths:
+        near = [length + x for x in (-2, -1, 0, 1, 2, 63, 64, 65)]
+        for window in (0, 1, 2, 64, 1000, 2 ** 30, top - 1, top):
+            for p in {-2 ** 31, -1, 0, 1, 50, *near, *(x + window for x in near), top - 512, top - 450, top - 300, top - 1, top}:
+                if not -2 ** 31 <= p <= top:
+                    continue
+                lo, hi = sight(p, length, window)
+                first, last = (max(0, p - window + 1) if window else 0), min(p, length - 1)
+                assert (lo < hi) == (first <= last), (p, length, window)
+                if lo < hi:
+                    assert (lo, hi - 1) == (first, last), (p, length, window)
+                assert 0 <= lo and 0 <= hi <= length, (p, length, window)
+                assert (max(lo >> 6, (hi + 63) >> 6) + 16) << 6 < 2 ** 31, (p, length, window)
