@@ -173,7 +173,9 @@ wf_status wf_kv_load(wf_kv_ctx *ctx, const uint8_t *cache, const int64_t *slot, 
  * Products are of 16-bit values with fp32 sums; the softmax is fp32, its
  * probabilities times the value scales are rounded to the 16-bit type.  Sums are
  * divided by the softmax's total at their end: with bf16, values must stay below
- * about 1e36 / (tokens seen) for them to be finite.
+ * about 1e36 / (tokens seen) for them to be finite.  With f16 the largest
+ * probability times scale is moved to the upper part of the type's range first,
+ * so that small values keep as many bits as large ones.
  */
 wf_status wf_kv_attend(wf_kv_ctx *ctx, const void *q, int64_t q_stride, int32_t n_tokens,
                        const uint8_t *cache, const int32_t *table, const int32_t *kv_len,

@@ -27,6 +27,7 @@
 // PFLOP/s (a large product reaches 1.2), with the matrix cores busy for 42% of the cycles of a
 // busy CU and vector instructions issued in 38%; at 64 channels, where a score costs half the
 // product and the same softmax, it is 26% and 52%.
+#include <cfloat>
 #include <type_traits>
 
 #include "kv.h"
@@ -44,15 +45,19 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // What depends on the 16-bit type: the product, the codes as its operand, a pair of
-// rounded values, and how far a score may pass the running maximum (in powers of
-// two) before the sums are rescaled: p z must stay below the type's largest
-// value, z of f16 values is at most 10,917.
+// rounded values, and where the reference of the probabilities stands (in powers of two: p is
+// 2^(score - reference)) and how far a score may pass it.
+//
+// bf16 has the range of fp32, so any p z keeps its bits and the reference is the largest score.
+// f16 ends at 2^16 and has whole precision from 2^-14 on, so the reference goes by p z instead (kScaled):
+// the largest is put high in that range, whatever the size of the values.  A p may then be large or small,
+// in fp32.
 struct MmaBf16 : Bf16 {
   typedef __bf16 v8 __attribute__((ext_vector_type(8)));
   typedef __bf16 v2 __attribute__((ext_vector_type(2)));
   static constexpr float kSlack = 8.0f;
-  static constexpr bool kTrack = false;
-  static constexpr float kAbove = 0.0f, kLow = 0.0f, kHigh = 0.0f;
+  static constexpr bool kScaled = false;
+  static constexpr float kAimFixed = 0.0f;
   static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
@@ -67,13 +72,13 @@ struct MmaBf16 : Bf16 {
 struct MmaF16 : F16 {
   typedef _Float16 v8 __attribute__((ext_vector_type(8)));
   typedef _Float16 v2 __attribute__((ext_vector_type(2)));
-  static constexpr float kSlack = 2.0f;
-  // where the largest score may end up against a fixed reference, in powers of two: at
-  // -8 its p z is 2^-10 for values of size 1, and what f16 drops below 2^-24 is 2^-14
-  // of that; 12 leaves room for z up to 16 (above that the sums overflow, and show it)
-  // The reference is put 3 above the largest score of a unit, the middle of that.
-  static constexpr bool kTrack = true;
-  static constexpr float kAbove = 3.0f, kLow = -8.0f, kHigh = 12.0f;
+  static constexpr float kSlack = 60.0f;
+  static constexpr bool kScaled = true;
+  // Running reference: the largest p z is from 2^12 to 2^15; one that is 2^-26 of it still has all its bits.
+  // Fixed reference: the largest p z of some tokens that the query sees is 2^2 (a half step that f16 drops,
+  // 2^-25, is 2^-27 of it), so that of all may be 14 powers of two above.  (600 normal queries over 9,000
+  // keys: up to 10; at 2^6 a sixth of the workgroups had to run twice.)
+  static constexpr float kAim = 12.0f, kAimFixed = 2.0f, kMostTerm = 0x1p15f;
   static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
@@ -94,6 +99,12 @@ __device__ __forceinline__ u32x4 operand(uint32_t w) {
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// The size of a value scale in powers of two: f16's largest at most, and so small that f16 has no place
+// for the value at least (0, and what is not a number).
+__device__ __forceinline__ float scale_log(float z) {
+  return __builtin_amdgcn_logf(fminf(fmaxf(fabsf(z), 0x1p-40f), 0x1p16f));
+}
 
 // Over the four lanes of a column.
 __device__ __forceinline__ float column_max(float x) {
@@ -217,7 +228,7 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
   constexpr int JT = C >= 4 ? 2 : 4;  // channel blocks joined at once
   constexpr int JP = JT * 16 + 4;     // and their padded row
   __shared__ __attribute__((aligned(16))) float join[kWaves][16 * C][JP];
-  __shared__ float top_of[kWaves][16 * C], sum_of[kWaves][16 * C];
+  __shared__ float ref_of[kWaves][16 * C], sum_of[kWaves][16 * C];
   __shared__ int last;
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -281,9 +292,10 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
     const int end = first + min(units, (split + 1) * share);
 
     f32x4 o[C][MT] = {};
-    float top[C], ref[C], sum[C];
+    // (the reference before the first score is below any, and not infinite: hidden scores are)
+    float ref[C], sum[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) top[c] = -INFINITY, ref[c] = 0.0f, sum[c] = 0.0f;
+    for (int c = 0; c < C; ++c) ref[c] = -FLT_MAX, sum[c] = 0.0f;
 
     const int kgrp = n >> 2;  // the group whose keys this lane loads: row n of a score tile
     // keys of a unit: token t*4 + n%4 of group n/4, this lane's quarter of the channels
@@ -368,16 +380,20 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
 #pragma unroll
           for (int i = 1; i < 8; ++i) m = fmaxf(m, s[c][i / 4][i % 4]);
           most[c] = m;
-          up |= m > top[c] + M::kSlack;
+          up |= m > ref[c] + M::kSlack;
         }
-        // the running maximum moves only when a score passes it by the slack
+        // the reference moves only when a score passes it by the slack
         if (__builtin_expect(__any(up), 0)) {
 #pragma unroll
           for (int c = 0; c < C; ++c) {
-            const float m = fmaxf(top[c], column_max(most[c]));
-            const float r = m == -INFINITY ? 0.0f : m;
-            const float keep = __builtin_amdgcn_exp2f(top[c] - r);
-            top[c] = m;
+            float r = most[c];
+            if constexpr (M::kScaled) {
+              r -= 40.0f;  // (values of next to nothing at the largest score: p stays far from fp32's end)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) r = fmaxf(r, s[c][i / 4][i % 4] + scale_log(vz[i]) - M::kAim);
+            }
+            r = fmaxf(ref[c], column_max(r));
+            const float keep = __builtin_amdgcn_exp2f(ref[c] - r);
             ref[c] = r;
             sum[c] *= keep;
 #pragma unroll
@@ -397,6 +413,22 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
             x[i] = e * vz[i];
             // a hidden token's scale may be anything
             if (!whole) x[i] = j0 + i >= lo[c] && j0 + i < hi[c] ? x[i] : 0.0f;
+          }
+          if constexpr (M::kScaled) {  // ... or when a term passes what its type holds
+            float m = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
+            if (__builtin_expect(__any(m > M::kMostTerm), 0)) {
+              m = column_max(m);
+              const float up = m > M::kMostTerm && m < INFINITY ? __builtin_amdgcn_logf(m) - M::kAim : 0.0f;
+              const float keep = __builtin_amdgcn_exp2f(-up);
+              ref[c] += up;
+              sum[c] *= keep;
+#pragma unroll
+              for (int k = 0; k < MT; ++k) o[c][k] *= keep;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[i] *= keep;
+            }
           }
 #pragma unroll
           for (int b = 0; b < 4; ++b) p[c][b] = M::pair(x[b], x[4 + b]);
@@ -422,16 +454,16 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
     for (int c = 0; c < C; ++c) {
       sum[c] = column_sum(sum[c]);
       if (grp == 0) {
-        top_of[wave][c * 16 + n] = top[c];
+        ref_of[wave][c * 16 + n] = ref[c];
         sum_of[wave][c * 16 + n] = sum[c];
       }
     }
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float m = -INFINITY;
-      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, top_of[w][c * 16 + n]);
-      const float keep = __builtin_amdgcn_exp2f(top[c] - (m == -INFINITY ? 0.0f : m));
+      float m = ref[c];
+      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ref_of[w][c * 16 + n]);
+      const float keep = __builtin_amdgcn_exp2f(ref[c] - m);
 #pragma unroll
       for (int k = 0; k < MT; ++k) o[c][k] *= keep;
     }
@@ -449,13 +481,12 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
         const int64_t col = tile * 16 * C + cc;
         if (col >= columns) continue;
         f32x4 v = {0, 0, 0, 0};
-        float m = -INFINITY, total = 0.0f;
+        float m = -FLT_MAX, total = 0.0f;
         for (int w = 0; w < kWaves; ++w) {
           v += *reinterpret_cast<const f32x4*>(&join[w][cc][ch]);
-          m = fmaxf(m, top_of[w][cc]);
+          m = fmaxf(m, ref_of[w][cc]);
         }
-        const float r = m == -INFINITY ? 0.0f : m;
-        for (int w = 0; w < kWaves; ++w) total += sum_of[w][cc] * __builtin_amdgcn_exp2f(top_of[w][cc] - r);
+        for (int w = 0; w < kWaves; ++w) total += sum_of[w][cc] * __builtin_amdgcn_exp2f(ref_of[w][cc] - m);
         const unsigned i = (unsigned)col / (unsigned)g.group, h = (unsigned)col - i * (unsigned)g.group;
         const int64_t head = (int64_t)(q0 + i) * g.hq + kvh * g.group + h;
         const int at = j0 * 16 + ch;
@@ -489,10 +520,11 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend(Geo g, AttendAr
 // A chunk of operands is read from LDS while the one before it is multiplied.
 //
 // There is no running maximum: probabilities are taken against a reference that stands
-// from the start, the largest score among the last tokens that all of a wave's columns
-// see.  A softmax does not depend on it as long as nothing overflows or vanishes.  For
-// bf16, whose range is that of fp32, the total tells at the end whether it did; f16 tracks the
-// largest score.  Where the reference was too far off, the true maximum is found and
+// from the start, the largest score (f16: with the value's scale) among the last tokens that all of a
+// wave's columns see.  A softmax does not depend on it as long as nothing overflows or vanishes.  For
+// bf16, whose range is that of fp32, the total tells at the end whether it did; f16 cannot lose
+// what matters beside those tokens, and what passes its range makes sums that are not finite.  Where the
+// reference was too far off, or those tokens are hidden from a query, the true maximum is found and
 // the workgroup runs once more, so that the loop itself has no branch and touches the sums with
 // matrix instructions alone.
 template <int D, int C, int W, class M>
@@ -653,7 +685,7 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
     };
 
     f32x4 o[C][MT];
-    float ref[C], sum[C], top[C];
+    float ref[C], sum[C];
     u32x4 p[C];
     f32x4 s[C][2];
     // a step's operands: of the values RB of the lower, RB of the upper half of the
@@ -684,8 +716,8 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
         }
       }
     };
-    // the largest score of each column among the tokens of units [u0, u1) that it sees,
-    // straight from the cache
+    // the largest score (kScaled: with the scale of its value) of each column among the tokens of units [u0, u1)
+    // that it sees, straight from the cache
     auto largest = [&](int u0, int u1, float (&m)[C]) {
 #pragma unroll
       for (int c = 0; c < C; ++c) m[c] = -INFINITY;
@@ -707,11 +739,17 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
           const int j0 = ztoken + t * 4;
           const u32x2 z = *reinterpret_cast<const u32x2*>(zat + t * 8);
           const float kz[4] = {bf_lo(z[0]) * scale, bf_hi(z[0]) * scale, bf_lo(z[1]) * scale, bf_hi(z[1]) * scale};
+          float vl[4] = {};
+          if constexpr (M::kScaled) {
+            const u32x2 v = *reinterpret_cast<const u32x2*>(zat + g.b * 2 + t * 8);
+            vl[0] = scale_log(bf_lo(v[0])), vl[1] = scale_log(bf_hi(v[0]));
+            vl[2] = scale_log(bf_lo(v[1])), vl[3] = scale_log(bf_hi(v[1]));
+          }
 #pragma unroll
           for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              m[c] = fmaxf(m[c], j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] * kz[i] : -INFINITY);
+              m[c] = fmaxf(m[c], j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] * kz[i] + vl[i] : -INFINITY);
         }
       }
 #pragma unroll
@@ -724,10 +762,11 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
     };
    for (int pass = 0;; ++pass) {
     // pass 0 takes the reference from the last unit that all of the wave's columns see
-    // whole, or at all, unless they see the first one whole (below); pass 1 from all
+    // whole, or at all, unless they see the first one whole (below); pass 1 from all.  (A window may hide
+    // that unit from the wave's last queries: they see the next one.)
     const int near = hi_min >= 64 && ((hi_min >> 6) - 1) << 6 >= lo_max ? (hi_min >> 6) - 1 : max(hi_min - 1, 0) >> 6;
     if (pass) largest(begin, begin + count, ref);
-    else largest(near, near + (hi_min > 0 && !whole(0)), ref);
+    else largest(near, near + (hi_min == 0 || whole(0) ? 0 : M::kScaled && near << 6 < lo_max && (near + 1) << 6 < hi_max ? 2 : 1), ref);
     // keys of steps 0 to 3, values and scales of steps 0 and 1; all on their way at once
     Codes w, w0, w2;
     Ids d, d0, d2, d3;
@@ -756,14 +795,17 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
 #pragma unroll
       for (int c = 0; c < C; ++c) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ref[c] = fmaxf(ref[c], s[c][i / 4][i % 4] * kzbuf[0][grp * 8 + i]);
+        for (int i = 0; i < 8; ++i) {
+          const float x = s[c][i / 4][i % 4] * kzbuf[0][grp * 8 + i];
+          ref[c] = fmaxf(ref[c], M::kScaled ? x + scale_log(vzbuf[0][grp * 8 + i]) : x);
+        }
         ref[c] = column_max(ref[c]);
       }
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      ref[c] = fabsf(ref[c]) < INFINITY ? ref[c] + (pass ? 0.0f : M::kAbove) : 0.0f;
-      sum[c] = 0.0f, top[c] = -INFINITY, p[c] = (u32x4){0, 0, 0, 0};
+      ref[c] = fabsf(ref[c]) < INFINITY ? ref[c] - M::kAimFixed : 0.0f;
+      sum[c] = 0.0f, p[c] = (u32x4){0, 0, 0, 0};
 #pragma unroll
       for (int k = 0; k < MT; ++k) o[c][k] = (f32x4){0, 0, 0, 0};
     }
@@ -805,7 +847,6 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
           for (int i = 0; i < 8; ++i) {
             x[c][i] = fmaf(s[c][i / 4][i % 4], kz[i], -ref[c]);
             if (kMask) x[c][i] = j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] : -INFINITY;
-            if (M::kTrack) top[c] = fmaxf(top[c], x[c][i]);
           }
         // keys of the step after
 #pragma unroll
@@ -854,13 +895,8 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
     for (int c = 0; c < C; ++c) {
       sum[c] = column_sum(sum[c]);
       const bool sees = max(lo[c], begin << 6) < min(hi[c], (begin + count) << 6);
-      bool fine = true;
-      if (M::kTrack) {
-        top[c] = column_max(top[c]);
-        fine = top[c] >= M::kLow && top[c] <= M::kHigh;
-      } else {
-        fine = sum[c] >= 0x1p-60f && sum[c] <= 0x1p60f;
-      }
+      // (kScaled: 0 is the reference of a query that saw none of the tokens it was to come from)
+      bool fine = M::kScaled ? ref[c] != 0.0f : sum[c] >= 0x1p-60f && sum[c] <= 0x1p60f;
 #pragma unroll
       for (int k = 0; k < MT; ++k) fine &= fabsf(o[c][k][0] + o[c][k][1] + o[c][k][2] + o[c][k][3]) < INFINITY;
       bad |= sees && !fine;

@@ -837,3 +837,81 @@ def test_attend_positions_past_every_window(hq, hk, d, dtype):
                                                  scale=d ** -0.5, window=window, **hints))
                         assert (np.abs(got - want) <= bound(dtype, want, mag, dots, d, 300)).all(), (queries, window)
                         assert (got[mag.sum(-1) == 0] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d", [(8, 1, 64), (4, 1, 128), (4, 1, 256)])
+def test_attend_is_as_accurate_for_small_and_large_values(hq, hk, d, dtype):
+    """Values of sizes 2^-13 to 2^11, one score 10 powers of two above a long tail of others or none, by the kernels
+    of 16, of 32 and of many columns: the error is bounded relative to the values."""
+    b, n, most = 16, 1500, 70
+    u = UNIT[dtype]
+    for i, at in enumerate((None, 7, n - 1)):
+        far = {} if at is None else {at: 10 / (1.4427 * d ** 0.5)}
+        q, cache, table, kv, q_off, pos = skewed_case(np.random.default_rng(10 * d + i), hq, hk, d, b, n, most, dtype, far)
+        want, mag, dots = K.attend(host(q), cache, table, kv, q_off, pos, d ** -0.5, 0)
+        with ctx_of(hq, hk, d, b, cache.n, table.shape[1], dtype) as ctx:
+            for power in (0, -7, -10, -13, 11):
+                raw, size = cache.bytes.copy(), 2.0 ** power
+                raw[..., b * d:].view(np.uint16)[..., b:] += np.uint16((power << 7) & 0xffff)      # scales of the values
+                for nq in (1, 5, most):
+                    got = host(pkg.kv_attend(ctx, q[-nq:], dev(raw), dev(table), dev(kv), dev(np.array([0, nq], np.int32)),
+                                             dev(pos[-nq:].copy()), scale=d ** -0.5, max_q=nq, max_kv=n))
+                    w, m = want[-nq:] * size, mag[-nq:] * size
+                    # as in bound(), but for f16's small steps: a probability times a value scale is rounded to half a step,
+                    # 2^-25, of a number whose largest is at least 2^-2; a scale is a sixth of some channel
+                    delta = (d + 16) * 2.0 ** -24 * dots[-nq:][..., None]
+                    lim = u * np.abs(w) + (1.01 * u + 2.2 * delta + (n + 64) * 2.0 ** -23) * m + 2.0 ** -25
+                    if dtype == "f16":
+                        lim += n * 2.0 ** -23 * m.max(-1, keepdims=True)
+                    assert (np.abs(w) > lim).any(-1).all()        # zeros would not pass
+                    assert (np.abs(got - w) <= lim).all(), (at, power, nq, float((np.abs(got - w) / lim).max()))
+
+
+@pytest.mark.parametrize("hq,hk,d", [(8, 1, 64), (4, 1, 128), (4, 1, 256)])
+def test_attend_uneven_values(hq, hk, d):
+    """f16: the token that has most of the weight with a value of zeros, and one of next to no weight with a value a
+    thousand times the others', by the kernels of 16, of 32 and of many columns."""
+    b, n, most = 16, 700, 70
+    one = 1 / (1.4427 * d ** 0.5)                                # a power of two in the score
+    for i, (sink, loud) in enumerate(((None, 400), (7, None), (690, 3), (3, 690))):
+        far = {**({} if sink is None else {sink: 20 * one}), **({} if loud is None else {loud: -12 * one})}
+        q, cache, table, kv, q_off, pos = skewed_case(np.random.default_rng(5 * d + i), hq, hk, d, b, n, most, "f16", far, 8.0)
+        for j, size in ((sink, 0.0), (loud, 8000.0)):
+            if j is not None:
+                keys, _ = cache.get([int(table[0, j // b]) * b + j % b])
+                cache.put(int(table[0, j // b]) * b + j % b, keys[0].astype(np.float32),
+                          (size * np.random.default_rng(j).uniform(0.5, 1, (hk, d))).astype(np.float32))
+        want, mag, dots = K.attend(host(q), cache, table, kv, q_off, pos, d ** -0.5, 0)
+        with ctx_of(hq, hk, d, b, cache.n, table.shape[1], "f16") as ctx:
+            for nq in (1, 5, most):
+                got = host(pkg.kv_attend(ctx, q[-nq:], dev(cache.bytes), dev(table), dev(kv), dev(np.array([0, nq], np.int32)),
+                                         dev(pos[-nq:].copy()), scale=d ** -0.5, max_q=nq, max_kv=n))
+                w, m, u = want[-nq:], mag[-nq:], UNIT["f16"]
+                # as in the test before
+                lim = u * np.abs(w) + (1.01 * u + 2.2 * (d + 16) * 2.0 ** -24 * dots[-nq:][..., None] + (n + 64) * 2.0 ** -23) * m
+                lim += 2.0 ** -25 + n * 2.0 ** -23 * m.max(-1, keepdims=True)
+                assert (np.abs(w) > lim).any(-1).all()
+                assert (np.abs(got - w) <= lim).all(), (sink, loud, nq, float((np.abs(got - w) / lim).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("window", [1, 2, 16, 63, 100])
+def test_attend_prompts_through_small_windows(window, dtype):
+    """Many columns whose windows share no tokens, some or all."""
+    check_attend(8, 2, 64, 16, [(300, 200, None), (150, 90, None), (40, 40, None)], dtype, window=window, seed=window)
+    check_attend(3, 3, 128, 32, [(400, 300, None)], dtype, window=window, seed=window)
+
+
+def test_attend_over_zeros():
+    """A cache of zeros, as it may be before its first use."""
+    for hq, hk, d in ((8, 1, 64), (4, 1, 128), (4, 1, 256)):
+        for dtype in ("bf16", "f16"):
+            with ctx_of(hq, hk, d, 16, 32, 32, dtype) as ctx:
+                q = torch.randn(60, hq, d, device=DEV).to(TYPES[dtype])
+                table, pos = torch.arange(32, dtype=torch.int32, device=DEV)[None], torch.arange(440, 500, dtype=torch.int32, device=DEV)
+                cache = torch.zeros(ctx.cache_bytes, dtype=torch.uint8, device=DEV)
+                for nq in (1, 5, 60):
+                    off, kv = dev(np.array([0, nq], np.int32)), dev(np.array([500], np.int32))
+                    out = pkg.kv_attend(ctx, q[:nq], cache, table, kv, off, pos[:nq].clone(), scale=0.1, max_q=nq, max_kv=500)
+                    assert (out == 0).all()
