@@ -90,6 +90,10 @@ struct Args {
   void holds(const at::Tensor* t, int64_t numel) {
     if (ok && t && t->numel() < numel) ok = false;
   }
+  // ... whose rows, where it has several axes, are `pitch` elements apart.
+  void rows(const at::Tensor* t, int64_t pitch) {
+    if (ok && t && t->dim() > 1 && t->numel() != t->size(0) * pitch) ok = false;
+  }
   // [n, heads, D] with dense heads; its token stride.
   int64_t tokens(const at::Tensor* t, int64_t n, int64_t heads) {
     if (!ok) return 0;
@@ -125,6 +129,7 @@ PyObject* step(PyObject*, PyObject* const* args, Py_ssize_t n) {
   a.holds(pool, 2);
   a.holds(ring, a.g->n_blocks);
   a.holds(table, r * a.g->max_blocks);
+  a.rows(table, a.g->max_blocks);
   if (!a.ok) return none();
   at::AutoDispatchBelowADInplaceOrView plain;
   const at::Tensor flat = fresh(*new_tokens, {2 * r + 3 + tokens}, at::kInt);
@@ -172,6 +177,7 @@ PyObject* store(PyObject*, PyObject* const* args, Py_ssize_t n) {
   a.holds(slot, t);
   a.holds(cache, a.g->cache_bytes);
   a.holds(cos_sin, n_pos * rot);
+  if (rot) a.rows(cos_sin, rot);
   a.holds(qw, a.g->d);
   a.holds(kw, a.g->d);
   if (!a.ok) return none();
@@ -221,6 +227,7 @@ PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const int64_t t = q->size(0), r = kv_len->size(0), qs = a.tokens(q, t, a.g->q_heads);
   a.holds(cache, a.g->cache_bytes);
   a.holds(table, r * a.g->max_blocks);
+  a.rows(table, a.g->max_blocks);
   a.holds(q_off, r + 1);
   a.holds(pos, t);
   if (!a.ok) return none();

@@ -37,7 +37,8 @@ def wf_kv_cache_bytes(q_heads: int, kv_heads: int, head_dim: int, block_tokens: 
 class KVContext:
     """A wf_kv_ctx on one HIP device: the geometry of a cache.  Tensor
     arguments are checked before any call reaches the library (GPU tensor, the
-    context's device, enough bytes, type or size of the elements)."""
+    context's device, enough bytes, type or size of the elements, length of the rows
+    of block tables and rotations)."""
 
     def __init__(self, device: int = 0, *, q_heads: int, kv_heads: int, head_dim: int, block_tokens: int,
                  n_blocks: int, max_blocks: int, dtype="bf16"):
@@ -82,6 +83,12 @@ class KVContext:
         if hasattr(x, "is_floating_point") and x.is_floating_point() != floating:
             raise TypeError(f"{name}: elements of type {x.dtype}")
         return address
+
+    def _rows(self, x, pitch: int, need: int, name: str, floating: bool = False) -> Optional[int]:
+        """A buffer of 4-byte elements whose rows, where it has several axes, are `pitch` elements apart."""
+        if getattr(x, "ndim", 0) > 1 and x.numel() != x.shape[0] * pitch:
+            raise ValueError(f"{name}: shape {tuple(x.shape)}, rows of {pitch} elements needed")
+        return self._b(x, need, name, 4, floating)
 
     def _wide(self, x, need: int, name: str) -> Optional[int]:
         """A buffer of the context's 16-bit type."""
@@ -130,7 +137,7 @@ class KVContext:
         self._check(self.lib.wf_kv_step(
             self.handle, b(new_tokens, 4 * r, "new_tokens"), int(n_rows), int(n_tokens), b(len_in, 4 * r, "len_in"),
             b(len_out, 4 * r, "len_out"), b(pool_in, 8, "pool_in"), b(pool_out, 8, "pool_out"),
-            b(ring, 4 * self.n_blocks, "ring"), b(table, 4 * r * self.max_blocks, "table"),
+            b(ring, 4 * self.n_blocks, "ring"), self._rows(table, self.max_blocks, 4 * r * self.max_blocks, "table"),
             b(q_off, 4 * r + 4, "q_off"), b(slot, 8 * t, "slot", 8), b(pos, 4 * t, "pos"), b(granted, r, "granted", 1),
             self._s(stream)))
 
@@ -141,8 +148,13 @@ class KVContext:
         (qp, qs), (kp, ks), (vp, vs) = (self._tokens(q, n, self.q_heads, "q", strides[0]),
                                         self._tokens(k, n, self.kv_heads, "k", strides[1]),
                                         self._tokens(v, n, self.kv_heads, "v", strides[2]))
+        need = 4 * n_pos * rot_dim
+        if 0 < rot_dim <= d and rot_dim % 16 == 0 and n_pos > 0 and pos is not None:
+            angles = self._rows(cos_sin, rot_dim, need, "cos_sin", True)
+        else:                                   # not read, or the library says what is wrong
+            angles = self._b(cos_sin, need, "cos_sin", 4, True)
         how = wf_kv_norm_rope(self._wide(q_weight, 2 * d, "q_weight"), self._wide(k_weight, 2 * d, "k_weight"), eps,
-                              rot_dim, int(interleaved), n_pos, self._b(cos_sin, 4 * n_pos * rot_dim, "cos_sin", 4, True))
+                              rot_dim, int(interleaved), n_pos, angles)
         self._check(self.lib.wf_kv_store(
             self.handle, qp, kp, vp, qs, ks, vs, int(n_tokens), ctypes.byref(how), self._b(pos, 4 * n, "pos"),
             self._b(slot, 8 * n, "slot", 8), self._wide(q_out, 2 * n * self.q_heads * d, "q_out"),
@@ -161,7 +173,7 @@ class KVContext:
         qp, qs = self._tokens(q, n, self.q_heads, "q", q_stride)
         self._check(self.lib.wf_kv_attend(
             self.handle, qp, qs, int(n_tokens), b(cache, self.cache_bytes, "cache", 1),
-            b(table, 4 * r * self.max_blocks, "table"), b(kv_len, 4 * r, "kv_len"), b(q_off, 4 * r + 4, "q_off"),
+            self._rows(table, self.max_blocks, 4 * r * self.max_blocks, "table"), b(kv_len, 4 * r, "kv_len"), b(q_off, 4 * r + 4, "q_off"),
             b(pos, 4 * n, "pos"), int(n_rows), float(scale), int(window), int(max_q), int(max_kv),
             self._wide(out, 2 * n * self.q_heads * self.head_dim, "out"), self._s(stream)))
 

@@ -915,3 +915,42 @@ def test_attend_over_zeros():
                     off, kv = dev(np.array([0, nq], np.int32)), dev(np.array([500], np.int32))
                     out = pkg.kv_attend(ctx, q[:nq], cache, table, kv, off, pos[:nq].clone(), scale=0.1, max_q=nq, max_kv=500)
                     assert (out == 0).all()
+
+
+def test_rows_of_another_length_are_refused(monkeypatch):
+    """Block tables wider or narrower than the context's and rotations of other channels, with as many elements
+    as are needed or more: refused by both ways of a call, before anything is written."""
+    hq, hk, d, b, width, rows = 4, 2, 64, 16, 4, 3
+    i32 = torch.int32
+    with ctx_of(hq, hk, d, b, 32, width) as ctx:
+        cache = torch.zeros(ctx.cache_bytes, dtype=torch.uint8, device=DEV)
+        q, k = torch.ones(rows, hq, d, dtype=torch.bfloat16, device=DEV), torch.ones(rows, hk, d, dtype=torch.bfloat16, device=DEV)
+        ones, off, pos = torch.ones(rows, dtype=i32, device=DEV), torch.arange(rows + 1, dtype=i32, device=DEV), torch.zeros(rows, dtype=i32, device=DEV)
+        ring, pool, slot = torch.arange(32, dtype=i32, device=DEV), torch.tensor([0, 32], dtype=i32, device=DEV), torch.arange(rows, device=DEV)
+        table = lambda *s: torch.zeros(*s, dtype=i32, device=DEV)
+        angles = lambda *s: torch.ones(*s, device=DEV)
+        step = lambda t: pkg.kv_step(ctx, ones, rows, pos, pool, ring, t)
+        attend = lambda t: pkg.kv_attend(ctx, q, cache, t, ones, off, pos, scale=1.0, max_q=1, max_kv=1)
+        store = lambda c, rot: pkg.kv_store(ctx, q, k, k, pos, slot, cache, c, rot_dim=rot)
+        for way in (ctx._bind, None):
+            monkeypatch.setattr(ctx, "_bind", way)
+            for call in (step, attend):
+                for bad in (table(rows, width + 1), table(2 * rows, width - 1), table(rows, 2 * width), table(1, rows * width), table(rows, width, 2)):
+                    with pytest.raises(ValueError):
+                        call(bad)
+                    assert not bad.any()
+                for good in (table(rows, width), table(rows + 2, width), table(rows * width), table(rows, 2, width // 2)):
+                    call(good)
+            for bad, rot in ((angles(9, d), d // 2), (angles(9, d // 2), d), (angles(9, 2, d), d), (angles(40, 16), 32)):
+                cache.fill_(7)
+                with pytest.raises(ValueError):
+                    store(bad, rot)
+                assert (cache == 7).all()
+            for good, rot in ((angles(9, d), d), (angles(9, d // 2), d // 2), (angles(9, 2, d // 2), d), (angles(9, d), 0), (None, 0)):
+                store(good, rot)
+        for bad in (table(rows, width + 1), table(2 * rows, width - 1)):
+            with pytest.raises(ValueError):
+                ctx.wf_kv_attend(q, rows, cache, bad, ones, off, pos, rows, 1.0, torch.empty_like(q))
+        with pytest.raises(ValueError):
+            ctx.wf_kv_store(q, k, k, rows, pos, slot, torch.empty_like(q), cache, cos_sin=angles(9, d), n_pos=9, rot_dim=d // 2)
+        torch.cuda.synchronize()
