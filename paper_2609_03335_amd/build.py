@@ -60,9 +60,19 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found: the gfx950 library cannot be built")
 
 
+def start_bind(out: str):
+    """The compiler of _kvbind.so as a process, or why there is none: it needs torch and a host compiler,
+    which the library does not."""
+    try:
+        return subprocess.Popen(bind_command(out), stdout=subprocess.PIPE, stderr=subprocess.STDOUT), None
+    except (ImportError, OSError) as e:
+        return None, str(e)
+
+
 def build(verbose: bool = False) -> str:
     """Compile every HIP source for gfx950 and link libwfplan.so next to
-    this file, and _kvbind.so beside it.  Always recompiles."""
+    this file.  Always recompiles.  _kvbind.so is built beside it where that is possible; where it
+    is not, the Python calls take the longer way."""
     build_dir = os.path.join(PKG, "_build")
     os.makedirs(build_dir, exist_ok=True)
     objs = []
@@ -75,7 +85,7 @@ def build(verbose: bool = False) -> str:
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
         objs.append(obj)
     bind = os.path.join(build_dir, "_kvbind.so")
-    procs.append(("kv_bind.cpp", subprocess.Popen(bind_command(bind), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+    bind_proc, why = start_bind(bind)
     errors = []
     for src, p in procs:
         out, _ = p.communicate()
@@ -91,7 +101,16 @@ def build(verbose: bool = False) -> str:
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     subprocess.check_call(cmd)
     os.replace(tmp, LIB_PATH)
-    os.replace(bind, BIND_PATH)
+    if bind_proc is not None:
+        out, _ = bind_proc.communicate()
+        if bind_proc.returncode != 0:
+            why = out.decode(errors="replace").strip() or f"exit status {bind_proc.returncode}"
+    if why is None:
+        os.replace(bind, BIND_PATH)
+    else:
+        print(f"_kvbind.so is not built: {why}", file=sys.stderr)
+        if os.path.exists(BIND_PATH):    # an earlier build's may not fit this one's header
+            os.remove(BIND_PATH)
     return LIB_PATH
 
 

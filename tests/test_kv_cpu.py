@@ -173,3 +173,29 @@ def test_sight_of_any_position_stays_in_the_row(sight):
                     assert (lo, hi - 1) == (first, last), (p, length, window)
                 assert 0 <= lo and 0 <= hi <= length, (p, length, window)
                 assert (max(lo >> 6, (hi + 63) >> 6) + 16) << 6 < 2 ** 31, (p, length, window)
+
+
+@pytest.mark.parametrize("case", ["whole", "no torch", "binding does not compile", "no host compiler"])
+def test_the_library_is_built_without_the_binding(monkeypatch, tmp_path, capfd, case):
+    """The C library needs hipcc alone: where torch or a host compiler for _kvbind is missing, it is built all the same,
+    and a binding of an earlier build does not stay.  (Compilers that only make their output file.)"""
+    import sys
+    from paper_2609_03335_amd import build
+    tool = tmp_path / "compiler"
+    tool.write_text('#!/bin/sh\nwhile [ "$1" != -o ]; do shift; done\necho built > "$2"\n')
+    tool.chmod(0o755)
+    lib, bind = tmp_path / "lib.so", tmp_path / "_kvbind.so"
+    monkeypatch.setattr(build, "PKG", str(tmp_path))
+    monkeypatch.setattr(build, "LIB_PATH", str(lib))
+    monkeypatch.setattr(build, "BIND_PATH", str(bind))
+    monkeypatch.setenv("HIPCC", str(tool))
+    monkeypatch.setenv("CXX", {"binding does not compile": "false", "no host compiler": str(tmp_path / "none")}.get(case, str(tool)))
+    if case == "no torch":
+        monkeypatch.setitem(sys.modules, "torch", None)
+    bind.write_text("of an earlier build")
+    assert build.build() == str(lib)
+    assert lib.read_text() == "built\n"
+    if case == "whole":
+        assert bind.read_text() == "built\n"
+    else:
+        assert not bind.exists() and "_kvbind" in capfd.readouterr().err
