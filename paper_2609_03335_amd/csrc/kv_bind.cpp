@@ -111,6 +111,16 @@ PyObject* none() {
   Py_RETURN_NONE;
 }
 
+// A call of the library, which may wait for a place in a full queue: other threads of the
+// interpreter go on meanwhile.
+template <class F, class... A>
+wf_status queued(F call, A... args) {
+  PyThreadState* thread = PyEval_SaveThread();
+  const wf_status st = call(args...);
+  PyEval_RestoreThread(thread);
+  return st;
+}
+
 at::Tensor fresh(const at::Tensor& like, at::IntArrayRef shape, at::ScalarType type) {
   return at::empty(shape, like.options().dtype(type));
 }
@@ -138,7 +148,7 @@ PyObject* step(PyObject*, PyObject* const* args, Py_ssize_t n) {
                              fresh(*new_tokens, {r}, at::kByte)};
   int32_t* base = static_cast<int32_t*>(flat.data_ptr());
   const wf_status st =
-      g_step(a.g->ctx, (const int32_t*)data(new_tokens), (int32_t)r, tokens, (const int32_t*)data(lens), base,
+      queued(g_step, a.g->ctx, (const int32_t*)data(new_tokens), (int32_t)r, tokens, (const int32_t*)data(lens), base,
              (const int32_t*)data(pool), base + r, (int32_t*)data(ring), (int32_t*)data(table), base + r + 2,
              (int64_t*)data(&out[3]), base + 2 * r + 3, (uint8_t*)data(&out[5]), stream);
   if (st != WF_OK) return PyLong_FromLong(st);
@@ -184,7 +194,7 @@ PyObject* store(PyObject*, PyObject* const* args, Py_ssize_t n) {
   at::AutoDispatchBelowADInplaceOrView plain;
   const at::Tensor out = fresh(*q, {t, a.g->q_heads, a.g->d}, a.g->type);
   const wf_kv_norm_rope how = {data(qw), data(kw), eps, rot, interleaved, (int32_t)n_pos, (const float*)data(cos_sin)};
-  const wf_status st = g_store(a.g->ctx, data(q), data(k), data(v), qs, ks, vs, (int32_t)t, &how, (const int32_t*)data(pos),
+  const wf_status st = queued(g_store, a.g->ctx, data(q), data(k), data(v), qs, ks, vs, (int32_t)t, &how, (const int32_t*)data(pos),
                                (const int64_t*)data(slot), data(&out), (uint8_t*)data(cache), stream);
   if (st != WF_OK) return PyLong_FromLong(st);
   return THPVariable_Wrap(out);
@@ -203,7 +213,7 @@ PyObject* load(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const int64_t t = slot->size(0);
   at::AutoDispatchBelowADInplaceOrView plain;
   const at::Tensor k = fresh(*slot, {t, a.g->kv_heads, a.g->d}, a.g->type), v = fresh(*slot, {t, a.g->kv_heads, a.g->d}, a.g->type);
-  const wf_status st = g_load(a.g->ctx, (const uint8_t*)data(cache), (const int64_t*)data(slot), (int32_t)t, data(&k), data(&v), stream);
+  const wf_status st = queued(g_load, a.g->ctx, (const uint8_t*)data(cache), (const int64_t*)data(slot), (int32_t)t, data(&k), data(&v), stream);
   if (st != WF_OK) return PyLong_FromLong(st);
   PyObject *x = THPVariable_Wrap(k), *y = THPVariable_Wrap(v);
   PyObject* pair = x && y ? PyTuple_Pack(2, x, y) : nullptr;
@@ -233,7 +243,7 @@ PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!a.ok) return none();
   at::AutoDispatchBelowADInplaceOrView plain;
   const at::Tensor out = fresh(*q, {t, a.g->q_heads, a.g->d}, a.g->type);
-  const wf_status st = g_attend(a.g->ctx, data(q), qs, (int32_t)t, (const uint8_t*)data(cache), (const int32_t*)data(table),
+  const wf_status st = queued(g_attend, a.g->ctx, data(q), qs, (int32_t)t, (const uint8_t*)data(cache), (const int32_t*)data(table),
                                 (const int32_t*)data(kv_len), (const int32_t*)data(q_off), (const int32_t*)data(pos), (int32_t)r,
                                 scale, window, max_q, max_kv, data(&out), stream);
   if (st != WF_OK) return PyLong_FromLong(st);

@@ -954,3 +954,34 @@ def test_rows_of_another_length_are_refused(monkeypatch):
         with pytest.raises(ValueError):
             ctx.wf_kv_store(q, k, k, rows, pos, slot, torch.empty_like(q), cache, cos_sin=angles(9, d), n_pos=9, rot_dim=d // 2)
         torch.cuda.synchronize()
+
+
+def test_other_threads_run_during_a_call():
+    """A call that waits in the library (here: one that only sleeps) does not stop the interpreter's other threads."""
+    import ctypes
+    import threading
+    with ctx_of(4, 2, 64, 16, 8, 4) as ctx:
+        assert ctx._bind is not None, "_kvbind is not built"
+        address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+        lib = ctx.lib
+        calls = [address(f) for f in (lib.wf_kv_step, lib.wf_kv_store, lib.wf_kv_load, lib.wf_kv_attend)]
+        microseconds = 300000                                   # usleep's argument, in the context's place
+        asleep = ctx._bind.geometry(microseconds, 0, 4, 2, 64, 8, 4, ctx.cache_bytes, False)
+        cache, slot = torch.zeros(ctx.cache_bytes, dtype=torch.uint8, device=DEV), torch.arange(3, device=DEV)
+        ticks, done = [], threading.Event()
+
+        def other():
+            while not done.wait(0.01):
+                ticks.append(1)
+        thread = threading.Thread(target=other)
+        thread.start()
+        try:
+            ctx._bind.calls(calls[0], calls[1], address(ctypes.CDLL(None).usleep), calls[3])
+            before = len(ticks)
+            out = ctx._bind.load(asleep, 0, cache, slot)
+            during = len(ticks) - before
+        finally:
+            ctx._bind.calls(*calls)
+            done.set()
+            thread.join()
+        assert isinstance(out, tuple) and during >= 5, during
