@@ -44,9 +44,13 @@
  * captured in a HIP graph.  What lies in device arrays cannot be checked by
  * the host: block ids, slots, positions, lengths or offsets outside their
  * range give unspecified results without touching memory outside the arrays.
- * A context is not thread-safe, and wf_kv_attend calls on one context must not
- * run concurrently on different streams (they share its work area, allocated
- * at create).
+ * A context is not thread-safe.  Calls of one context on different streams may
+ * run at the same time (on data of their own): each of the first
+ * WF_KV_ATTEND_STREAMS streams that wf_kv_attend is called on has a work area of
+ * the context for good (allocated at create); on further streams long rows of few
+ * queries take longer, as their tokens are not shared out.  A captured call keeps the area of
+ * the stream that it was captured on: replays of such graphs must not run at the same
+ * time as each other or as calls on that stream.
  */
 #ifndef WF_KV_H
 #define WF_KV_H
@@ -61,6 +65,7 @@ extern "C" {
 #define WF_KV_MAX_TOKENS (1 << 24)  /* packed tokens of a step                 */
 #define WF_KV_MAX_HEADS 1024        /* query heads                             */
 #define WF_KV_MAX_BLOCKS (1 << 30)  /* blocks of a cache                       */
+#define WF_KV_ATTEND_STREAMS 8      /* streams with a work area of their own   */
 #define WF_KV_MAX_WIDTH (1 << 22)   /* blocks of a row, of at most 2^30 tokens     */
 
 enum { WF_KV_BF16 = 0, WF_KV_F16 = 1 };
@@ -84,7 +89,7 @@ typedef struct wf_kv_ctx wf_kv_ctx; /* opaque; geometry and work area */
 wf_status wf_kv_cache_bytes(const wf_kv_desc *desc, int64_t *bytes);
 
 /* Create a context on HIP device `hip_device`; it copies *desc and allocates
- * the work area of wf_kv_attend.  On failure *out is NULL and
+ * the work areas of wf_kv_attend (272 MiB).  On failure *out is NULL and
  * wf_kv_last_error(NULL) describes the error. */
 wf_status wf_kv_ctx_create(int hip_device, const wf_kv_desc *desc, wf_kv_ctx **out);
 

@@ -66,8 +66,11 @@ struct AttendArgs {
 };
 
 // The work area of launch_attend: partial sums, the number of shares that wrote
-// those of each query's head, and counts of shares done, 0 between launches.
+// those of each query's head, and counts of shares done, 0 between launches.  A context has one for each of
+// the first kAreas streams that attend; without one (all sizes 0) no tokens are shared out.
 constexpr size_t kPartBytes = size_t(32) << 20, kCountBytes = size_t(1) << 20;
+constexpr size_t kAreaBytes = kPartBytes + 2 * kCountBytes;
+constexpr int kAreas = WF_KV_ATTEND_STREAMS;
 struct AttendWork {
   int n_cu;
   float* part;

@@ -141,6 +141,7 @@ struct Split {
   float* part;        // [splits][n_tokens][hq][D + 2] sums, reference, total
   int32_t* used;      // joined by a kernel: [n_tokens][hq] shares written; 1: the output is done
   int32_t* arrived;   // by the last workgroup: [n_rows][tiles][hk] shares done; 0 before and after a launch
+                      // (all of a launch on one stream: another stream has other ones)
 };
 
 // Up to this many shares of 16 columns are joined by the workgroup that is done last, more (or of
@@ -166,15 +167,17 @@ __device__ __forceinline__ f32x2 get(const float* from) {
   return (f32x2){__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32))};
 }
 
-// Whether this workgroup is the last of an item's `used` to get here.
+// Whether this workgroup is the last of an item's `used` to get here.  The count goes back to 0 by the
+// same operation that counts the last one.
 __device__ __forceinline__ bool last_to_arrive(int32_t* arrived, int used, int* flag) {
-  // every wave's stores have reached the memory that all dies see before any of them counts
+  // Every wave's stores have reached the memory that all dies see before any of them counts, and the
+  // sums are read after the last has counted: the clobber and the barriers keep the compiler to this order, and
+  // the accesses are atomic, so that none of them is served from a cache of one die.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
-    const int before = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *flag = before == used - 1;
-    if (before == used - 1) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const unsigned most = (unsigned)used - 1u;
+    *flag = atomicInc(reinterpret_cast<unsigned*>(arrived), most) == most;
   }
   __syncthreads();
   return *flag;

@@ -11,7 +11,10 @@ struct wf_kv_ctx {
   int device = 0;
   int dtype = 0;
   wfkv::Geo g{};
-  wfkv::AttendWork work{};
+  int n_cu = 0;
+  char* areas = nullptr;             // kAreas work areas: sums, then the two arrays of counts
+  void* owner[wfkv::kAreas] = {};    // the streams that have them
+  int owners = 0;
   char err[256] = "";
 };
 
@@ -76,6 +79,18 @@ wf_status launch(wf_kv_ctx* ctx, const char* what, F&& f) {
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// The work area of a stream, for good; none for those that come when all are given.
+wfkv::AttendWork area_of(wf_kv_ctx* ctx, void* stream) {
+  int i = 0;
+  while (i < ctx->owners && ctx->owner[i] != stream) ++i;
+  if (i == wfkv::kAreas) return wfkv::AttendWork{ctx->n_cu, nullptr, 0, nullptr, nullptr, 0};
+  if (i == ctx->owners) ctx->owner[ctx->owners++] = stream;
+  char* at = ctx->areas + i * wfkv::kAreaBytes;
+  char* counts = at + wfkv::kPartBytes;
+  return wfkv::AttendWork{ctx->n_cu, reinterpret_cast<float*>(at), wfkv::kPartBytes, reinterpret_cast<int32_t*>(counts),
+                          reinterpret_cast<int32_t*>(counts + wfkv::kCountBytes), wfkv::kCountBytes};
+}
+
 wf_status null_ctx() { return fail(nullptr, WF_EINVAL, "ctx is NULL"); }
 
 }  // namespace
@@ -114,17 +129,12 @@ wf_status wf_kv_ctx_create(int hip_device, const wf_kv_desc* desc, wf_kv_ctx** o
   g.width = desc->max_blocks;
   g.cell = (int)cell_bytes(desc);
   wf_status made = launch(ctx, "wf_kv_ctx_create", [&] {
-    hipError_t e = hipDeviceGetAttribute(&ctx->work.n_cu, hipDeviceAttributeMultiprocessorCount, hip_device);
-    if (e == hipSuccess) e = hipMalloc(&ctx->work.part, wfkv::kPartBytes + 2 * wfkv::kCountBytes);
+    hipError_t e = hipDeviceGetAttribute(&ctx->n_cu, hipDeviceAttributeMultiprocessorCount, hip_device);
+    if (e == hipSuccess) e = hipMalloc(&ctx->areas, wfkv::kAreas * wfkv::kAreaBytes);
     if (e != hipSuccess) return e;
-    char* counts = reinterpret_cast<char*>(ctx->work.part) + wfkv::kPartBytes;
-    ctx->work.used = reinterpret_cast<int32_t*>(counts);
-    ctx->work.arrived = reinterpret_cast<int32_t*>(counts + wfkv::kCountBytes);
-    ctx->work.part_bytes = wfkv::kPartBytes;
-    ctx->work.count_bytes = wfkv::kCountBytes;
-    e = hipMemset(counts, 0, 2 * wfkv::kCountBytes);
+    e = hipMemset2D(ctx->areas + wfkv::kPartBytes, wfkv::kAreaBytes, 0, 2 * wfkv::kCountBytes, wfkv::kAreas);
     if (e == hipSuccess) e = hipDeviceSynchronize();
-    if (e != hipSuccess) (void)hipFree(ctx->work.part);
+    if (e != hipSuccess) (void)hipFree(ctx->areas);
     return e;
   });
   if (made != WF_OK) {
@@ -140,7 +150,7 @@ void wf_kv_ctx_destroy(wf_kv_ctx* ctx) {
   if (!ctx) return;
   {
     OnDevice on(ctx->device);
-    (void)hipFree(ctx->work.part);
+    (void)hipFree(ctx->areas);
   }
   delete ctx;
 }
@@ -229,7 +239,8 @@ wf_status wf_kv_attend(wf_kv_ctx* ctx, const void* q, int64_t q_stride, int32_t 
     return fail(ctx, WF_EINVAL, "q, out and cache must be aligned to 16 bytes");
   const wfkv::AttendArgs a{q, q_stride, n_tokens, cache, table, kv_len, q_off, pos, n_rows, scale,
                            window, max_q, max_kv, out};
-  return launch(ctx, "wf_kv_attend", [&] { return wfkv::launch_attend(g, ctx->dtype, a, ctx->work, (hipStream_t)hip_stream); });
+  const wfkv::AttendWork work = area_of(ctx, hip_stream);
+  return launch(ctx, "wf_kv_attend", [&] { return wfkv::launch_attend(g, ctx->dtype, a, work, (hipStream_t)hip_stream); });
 }
 
 }  // extern "C"

@@ -38,7 +38,12 @@ class KVContext:
     """A wf_kv_ctx on one HIP device: the geometry of a cache.  Tensor
     arguments are checked before any call reaches the library (GPU tensor, the
     context's device, enough bytes, type or size of the elements, length of the rows
-    of block tables and rotations)."""
+    of block tables and rotations).
+
+    Calls on several streams may overlap, on tensors of their own: kv_attend has a work area for each of the
+    first 8 streams it is called on, and does without on others (long rows of few queries then take
+    longer).  A captured call keeps the area of the stream of its capture, so replays of graphs captured on one
+    stream must not overlap.  One thread at a time may use a context."""
 
     def __init__(self, device: int = 0, *, q_heads: int, kv_heads: int, head_dim: int, block_tokens: int,
                  n_blocks: int, max_blocks: int, dtype="bf16"):

@@ -985,3 +985,34 @@ def test_other_threads_run_during_a_call():
             done.set()
             thread.join()
         assert isinstance(out, tuple) and during >= 5, during
+
+
+@pytest.mark.parametrize("n", [1000, 9000])
+def test_attend_on_several_streams_at_once(n):
+    """Rows in shares, joined by the last workgroup (1,000 tokens) or by a launch of their own, on two streams whose
+    calls overlap: the results of each alone.  Streams past those with a work area: right too."""
+    hq, hk, d, b = 8, 2, 128, 16
+    rng = np.random.default_rng(n)
+    q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, [(n, 1, None), (n // 2 + 3, 1, None)], "bf16")
+    want, mag, dots = K.attend(host(q), cache, table, kv, q_off, pos, d ** -0.5, 0)
+    with ctx_of(hq, hk, d, b, cache.n, table.shape[1]) as ctx:
+        c, tb, ln, qo, ps = dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos)
+        run = lambda x, **kw: pkg.kv_attend(ctx, x, c, tb, ln, qo, ps, scale=d ** -0.5, max_q=1, max_kv=n, **kw)
+        inputs = [q, torch.roll(q, 1, 1)]
+        alone = [run(x) for x in inputs]
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in range(12)]
+        outs = [[], []]
+        for _ in range(300):
+            for x, s, out in zip(inputs, streams, outs):
+                out.append(run(x, stream=s))
+        torch.cuda.synchronize()
+        for out, w in zip(outs, alone):
+            for o in out:
+                assert torch.equal(o, w)
+        every = [run(q, stream=s) for s in streams]
+        torch.cuda.synchronize()
+        lim = bound("bf16", want, mag, dots, d, n)
+        for o in every:
+            assert (np.abs(host(o) - want) <= lim).all()
+        assert torch.equal(every[0], alone[0]) and torch.equal(run(q), alone[0])
