@@ -77,6 +77,8 @@ class Replica:
 def serve(replica, requests, chunk=64):
     """Run (prompt, tokens to answer) requests to their end, `chunk` prompt tokens a
     step at most; returns the answers."""
+    if not all(len(prompt) for prompt, _ in requests):
+        raise ValueError("a prompt is empty")
     waiting, batch = list(enumerate(requests)), [None] * replica.rows
     answers = [[] for _ in requests]
     while waiting or any(batch):

@@ -199,3 +199,27 @@ def test_the_library_is_built_without_the_binding(monkeypatch, tmp_path, capfd, 
         assert bind.read_text() == "built\n"
     else:
         assert not bind.exists() and "_kvbind" in capfd.readouterr().err
+
+
+def test_serving_refuses_an_empty_prompt():
+    """The serving example: a request without a first token has nothing to be answered from."""
+    import importlib.util
+    spec = importlib.util.spec_from_file_location("serve_activations", os.path.join(ROOT, "examples", "serve_activations.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+
+    class Replica:
+        """Answers every row with the number of its step; grants all."""
+        rows, steps = 2, 0
+
+        def step(self, new, tokens, most=0):
+            import torch
+            self.steps += 1
+            return torch.full((len(new),), self.steps), torch.tensor([int(n >= 0) for n in new])
+
+    assert example.serve(Replica(), [([5, 6], 2), ([7], 1), ([8], 0)]) == [[1, 2], [1], []]
+    replica = Replica()
+    for requests in ([([], 1)], [([5], 1), ([], 2)]):
+        with pytest.raises(ValueError):
+            example.serve(replica, requests)
+    assert replica.steps == 0
