@@ -729,9 +729,13 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
         const unsigned kid = pages.id(ktoken), zid = pages.id(ztoken);
         const uint8_t* kat = pages.cell(kid) + ((ktoken & (g.b - 1)) + (n & 3)) * (D / 2) + grp * (D / 8);
         const uint8_t* zat = pages.cell(zid) + g.b * D + (ztoken & (g.b - 1)) * 2;
-#pragma unroll 1
+        // (all loads on their way at once: 256 f16 prompts of 64 tokens 179 -> 161 us)
+#pragma unroll
         for (int t = 0; t < 4; ++t) {
           const uint32_t* at = reinterpret_cast<const uint32_t*>(kat + t * 4 * (D / 2));
+          const u32x2 z = *reinterpret_cast<const u32x2*>(zat + t * 8);
+          u32x2 v = {};
+          if constexpr (M::kScaled) v = *reinterpret_cast<const u32x2*>(zat + g.b * 2 + t * 8);
           f32x4 x[C] = {};
 #pragma unroll
           for (int k = 0; k < KS; ++k) {
@@ -740,11 +744,9 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend_wide(Geo g,
             for (int c = 0; c < C; ++c) x[c] = M::mma(kk, q[c][k], x[c]);
           }
           const int j0 = ztoken + t * 4;
-          const u32x2 z = *reinterpret_cast<const u32x2*>(zat + t * 8);
           const float kz[4] = {bf_lo(z[0]) * scale, bf_hi(z[0]) * scale, bf_lo(z[1]) * scale, bf_hi(z[1]) * scale};
           float vl[4] = {};
           if constexpr (M::kScaled) {
-            const u32x2 v = *reinterpret_cast<const u32x2*>(zat + g.b * 2 + t * 8);
             vl[0] = scale_log(bf_lo(v[0])), vl[1] = scale_log(bf_hi(v[0]));
             vl[2] = scale_log(bf_lo(v[1])), vl[3] = scale_log(bf_hi(v[1]));
           }
