@@ -175,6 +175,8 @@ wf_status wf_kv_load(wf_kv_ctx *ctx, const uint8_t *cache, const int64_t *slot, 
  * max_q and max_kv are hints for the launch: the most queries and the most cached
  * tokens of a row (0: not known).  Results are right whatever they are, to the
  * roundings of the kernel taken; unknown, too low or too high ones cost time.
+ * The kernel is chosen for the whole call, by its longest row: single tokens beside a
+ * long prompt take less time in a call of their own.
  * Products are of 16-bit values with fp32 sums; the softmax is fp32, its
  * probabilities times the value scales are rounded to the 16-bit type.  Sums are
  * divided by the softmax's total at their end: with bf16, values must stay below

@@ -20,13 +20,14 @@
 // join their sums through LDS; with few columns the tokens are also split over
 // workgroups, whose partial sums are joined in order, by the last workgroup or a second kernel.
 //
-// Single tokens are bound by the reading of the cache: 64 rows of up to 24,000 tokens, 1.03 GB,
-// 208 us (5.0 TB/s; a large copy reaches 5.1), one row of 200,001 49 us (4.3 TB/s), one of 1,000
-// by its launch and latency, 9.5 us.  Prompts are bound by the matrix cores and the vector
-// instructions of the softmax together: 8,191 tokens of 32 heads of 128 channels take 551 us, 1.0
+// Single tokens are bound by the reading of the cache: 64 f16 rows of up to 24,000 tokens, 1.03 GB,
+// 214 us (4.8 TB/s; a streaming kernel reaches 6.2, torch's copy 5.1) with vector instructions issued in
+// 55% of the cycles of a busy CU, one row of 200,001 50 us (4.2 TB/s), one of 1,000
+// by its launch and latency, 8.4 us.  Prompts are bound by the matrix cores and the vector
+// instructions of the softmax together: 8,191 tokens of 32 heads of 128 channels take 553 us, 1.0
 // PFLOP/s (a large product reaches 1.2), with the matrix cores busy for 42% of the cycles of a
 // busy CU and vector instructions issued in 38%; at 64 channels, where a score costs half the
-// product and the same softmax, it is 26% and 52%.
+// product and the same softmax, it is 27% and 50%.
 #include <cfloat>
 #include <type_traits>
 
@@ -146,7 +147,7 @@ struct Split {
 
 // Up to this many shares of 16 columns are joined by the workgroup that is done last, more (or of
 // more columns, which it would take one after the other) by a kernel of their own, with a
-// workgroup for each head: one token over 1,000 cached ones (4 shares) takes 8.6 us against 9.5, over
+// workgroup for each head: one token over 1,000 cached ones (4 shares) takes 8.4 us against 9.5, over
 // 2,000 (8) 10.8 against 9.5; 24 tokens (48 columns) over 1,000 18.7 against 12.8, over 2,000 26 against 13.
 template <int C>
 constexpr int kFused = C == 1 ? 4 : 1;

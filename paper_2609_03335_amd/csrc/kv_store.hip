@@ -9,8 +9,8 @@
 // stored codes are reproducible to the last bit by elementary operations.
 //
 // Bound by memory for prompts (q in and out is four fifths of the bytes): 16,384 tokens of
-// 40 + 8 heads of 128 channels take 93 us, 4.5 TB/s of their 420 MB (a large copy reaches
-// 5.1); by the launch for single tokens (3.7 us).
+// 40 + 8 heads of 128 channels take 88 to 98 us, 4.3 to 4.8 TB/s of their 420 MB (a streaming
+// kernel reaches 6.2); by the launch for single tokens (3.8 us).
 #include "kv.h"
 
 namespace wfkv {
