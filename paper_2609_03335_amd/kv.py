@@ -91,9 +91,10 @@ class KVContext:
 
     def _rows(self, x, pitch: int, need: int, name: str, floating: bool = False) -> Optional[int]:
         """A buffer of 4-byte elements whose rows, where it has several axes, are `pitch` elements apart."""
+        address = self._b(x, need, name, 4, floating)
         if getattr(x, "ndim", 0) > 1 and x.numel() != x.shape[0] * pitch:
             raise ValueError(f"{name}: shape {tuple(x.shape)}, rows of {pitch} elements needed")
-        return self._b(x, need, name, 4, floating)
+        return address
 
     def _wide(self, x, need: int, name: str) -> Optional[int]:
         """A buffer of the context's 16-bit type."""

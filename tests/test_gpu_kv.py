@@ -1016,3 +1016,19 @@ def test_attend_on_several_streams_at_once(n):
         for o in every:
             assert (np.abs(host(o) - want) <= lim).all()
         assert torch.equal(every[0], alone[0]) and torch.equal(run(q), alone[0])
+
+
+def test_arrays_of_the_host_are_a_type_error():
+    """numpy arrays where device tensors belong, those with rows too."""
+    with ctx_of(4, 2, 64, 16, 32, 4) as ctx:
+        i32 = torch.int32
+        q, k = torch.ones(3, 4, 64, dtype=torch.bfloat16, device=DEV), torch.ones(3, 2, 64, dtype=torch.bfloat16, device=DEV)
+        cache = torch.zeros(ctx.cache_bytes, dtype=torch.uint8, device=DEV)
+        ones, off, slot = torch.ones(3, dtype=i32, device=DEV), torch.arange(4, dtype=i32, device=DEV), torch.arange(3, device=DEV)
+        table = torch.zeros(3, 4, dtype=i32, device=DEV)
+        for bad in (dict(table=np.zeros((3, 4), np.int32)), dict(lens=np.ones(3, np.int32))):
+            a = {**dict(table=table, lens=ones), **bad}
+            with pytest.raises(TypeError):
+                pkg.kv_attend(ctx, q, cache, a["table"], a["lens"], off, ones - 1, scale=1.0)
+        with pytest.raises(TypeError):
+            pkg.kv_store(ctx, q, k, k, ones, slot, cache, np.ones((9, 64), np.float32), rot_dim=64)
