@@ -1,5 +1,5 @@
 /*
- * wf_kv.h -- C ABI of the paged 4-bit key/value cache of one replica.
+ * wf_kv.h -- C ABI of the paged key/value cache of one replica, in 4 or 8 bits.
  *
  * The scheduler (wf_plan.h) decides which activations a replica serves next;
  * serving them means giving their requests cache blocks, storing the keys and
@@ -13,7 +13,13 @@
  *   wf_kv_store   per layer: norm and rotation of queries and keys, queries
  *                 out, keys and values into the cache;
  *   wf_kv_attend  per layer: attention of the step's queries over the cache;
- *   wf_kv_load    cached tokens back as values.
+ *   wf_kv_load    cached tokens back as values;
+ * and between steps, for requests that begin alike (the activations of a workflow
+ * share what led to them) and for a replica that gives memory back:
+ *   wf_kv_fork     rows that begin with the first tokens of other rows share their blocks;
+ *   wf_kv_release  rows give up blocks that other rows may hold as well;
+ *   wf_kv_compact  all blocks in use move to the front of the cache;
+ *   wf_kv_copy     the contents of the blocks that a fork or a compaction moves.
  *
  * Rows and tokens.  A batch has n_rows rows, one per request; row r brings
  * new_tokens[r] tokens.  The tokens of all rows are packed in row order, row
@@ -34,6 +40,19 @@
  * a code is the nearest one to value / scale, ties to the even code, above 6
  * taken as 6.  A vector with an infinity or a NaN gets a NaN scale: it stands
  * for NaN in every channel.
+ *
+ * With WF_KV_E4M3 the cache holds 8-bit codes, and one cell is 2 * B * D + 16 bytes:
+ *   key codes    [B][D]
+ *   value codes  [B/4][D][4]  tokens 4i .. 4i+3 of a channel side by side
+ *   scales       fp32, of the keys and of the values; then 8 bytes that are not used
+ * A code is E4M3: a sign, 4 bits of exponent (bias 7), 3 of mantissa, no infinity, 0x7f and 0xff
+ * not a number.  A scale is a power of two, 2^e: e is the least for which no finite magnitude that the
+ * block's keys (values) of this head were stored with passes 448 * 2^e, -100 at least and 119 at most.  A code is
+ * the nearest one to value / scale, ties to the even code, above 448 taken as 448.  The scale
+ * grows with the block: storing at a block's first token begins it anew; storing behind it leaves the scale or
+ * raises it, and where it rises all other codes of the block and head are rounded to the new one (exactly,
+ * except those that come below 2^-6).  A token whose key or value holds an infinity or a NaN stands for
+ * NaN in every channel of both: all its key codes are 0x7f, its value codes 0.  Value codes are never NaN.
  *
  * Conventions are those of wf_plan.h: C functions that never throw and return
  * a wf_status; caller-owned DEVICE buffers of the context's GPU, contiguous
@@ -67,8 +86,11 @@ extern "C" {
 #define WF_KV_MAX_BLOCKS (1 << 30)  /* blocks of a cache                       */
 #define WF_KV_ATTEND_STREAMS 8      /* streams with a work area of their own   */
 #define WF_KV_MAX_WIDTH (1 << 22)   /* blocks of a row, of at most 2^30 tokens     */
+#define WF_KV_MAX_FORKS 65536       /* forks of a call                             */
+#define WF_KV_MAX_LAYERS 4096       /* caches that a call copies in                */
 
 enum { WF_KV_BF16 = 0, WF_KV_F16 = 1 };
+enum { WF_KV_E4M3 = 16 }; /* added to the type: a cache of 8-bit codes */
 
 /* Geometry of a cache and the heads that use it. */
 typedef struct {
@@ -79,7 +101,8 @@ typedef struct {
   int32_t n_blocks;      /* 1..WF_KV_MAX_BLOCKS                                 */
   int32_t max_blocks;    /* width of the block table: most blocks of a row      */
   int32_t dtype;         /* WF_KV_BF16 or WF_KV_F16: queries, keys, values and
-                            norm weights in, queries, values and outputs out    */
+                            norm weights in, queries, values and outputs out;
+                            with WF_KV_E4M3 added, codes of 8 bits instead of 4 */
 } wf_kv_desc;
 
 typedef struct wf_kv_ctx wf_kv_ctx; /* opaque; geometry and work area */
@@ -152,6 +175,9 @@ typedef struct {
  * that slices of one projection can be passed.  pos int32 [n_tokens] (may be
  * NULL when rot_dim is 0), slot int64 [n_tokens].  Two tokens must not have
  * the same slot.  All arithmetic is in fp32.
+ * With 8-bit codes the call's tokens of one block must follow each other, as wf_kv_step places them (they share
+ * a scale): what a block holds whose tokens come in several parts is unspecified.  Where a row's
+ * first token of the call is not the first of its block, the block's earlier tokens may be rounded anew (see above).
  */
 wf_status wf_kv_store(wf_kv_ctx *ctx, const void *q, const void *k, const void *v,
                       int64_t q_stride, int64_t k_stride, int64_t v_stride, int32_t n_tokens,
@@ -188,6 +214,75 @@ wf_status wf_kv_attend(wf_kv_ctx *ctx, const void *q, int64_t q_stride, int32_t 
                        const uint8_t *cache, const int32_t *table, const int32_t *kv_len,
                        const int32_t *q_off, const int32_t *pos, int32_t n_rows, float scale,
                        int32_t window, int32_t max_q, int32_t max_kv, void *out, void *hip_stream);
+
+/*
+ * Blocks that several rows hold.  shared[b] is the number of rows that hold block b beyond the first: 0
+ * for a block that one row holds and for a free one, so that wf_kv_step needs no change for blocks it takes.  The
+ * calls below read shared_in and write shared_out, int32 [n_blocks] each, as wf_kv_step does with lengths and
+ * pool: the old arrays stay as they were, a caller keeps two of each and swaps them.  table, ring, len_* and pool_* are
+ * those of wf_kv_step.  A batch that shares blocks ends its rows with wf_kv_release, not with
+ * new_tokens[r] < 0.  work int32 [WF_KV_PAGES_WORK] is overwritten.
+ */
+#define WF_KV_PAGES_WORK 1024
+
+/*
+ * Fork i makes row dst[i], which holds nothing, begin with the first k = min(tokens[i], len_in[src[i]])
+ * tokens of row src[i].  The floor(k / B) whole blocks are entered in both tables and counted in shared_out;
+ * the rest, if k is not a multiple of B, needs one block of the ring, and from[i] and to[i] are the block it is
+ * in and the new one, for wf_kv_copy (else -1 both): a block that more rows hold is always full and not
+ * written any more.
+ *   - A fork is granted in the order of the list, as rows are by wf_kv_step: when it needs no block, or when its need
+ *     and that of all forks before it (granted or not) fit in the free blocks.  granted[i] is 1 or 0.
+ *   - Refused, and their need not counted: src[i] or dst[i] outside the rows or the same, tokens[i] < 0, a row dst[i]
+ *     that holds tokens.
+ *   - All forks see the rows as they are before the call.  No row may be dst of two forks.
+ *   - len_out[dst[i]] = k (granted), other rows keep their length; pool_out and the entries of table follow.
+ * Arrays: src, dst, tokens, from, to int32 [n_forks]; granted uint8 [n_forks].  len_out, pool_out and shared_out
+ * must not be len_in, pool_in and shared_in.
+ */
+wf_status wf_kv_fork(wf_kv_ctx *ctx, const int32_t *src, const int32_t *dst, const int32_t *tokens, int32_t n_forks,
+                     int32_t n_rows, const int32_t *len_in, int32_t *len_out, const int32_t *pool_in,
+                     int32_t *pool_out, const int32_t *ring, int32_t *table, const int32_t *shared_in,
+                     int32_t *shared_out, int32_t *from, int32_t *to, uint8_t *granted, int32_t *work,
+                     void *hip_stream);
+
+/*
+ * Rows r with release[r] != 0 give up their blocks: each block counts one holder less for each of them.
+ * Blocks that nobody holds any more go to the end of the ring in ascending order of their ids.  len_out[r] = 0
+ * (released) or len_in[r]; table entries stay as they are.  release uint8 [n_rows].
+ */
+wf_status wf_kv_release(wf_kv_ctx *ctx, const uint8_t *release, int32_t n_rows, const int32_t *len_in,
+                        int32_t *len_out, const int32_t *pool_in, int32_t *pool_out, int32_t *ring,
+                        const int32_t *table, const int32_t *shared_in, int32_t *shared_out, int32_t *work,
+                        void *hip_stream);
+
+/*
+ * Moves the blocks in use to ids below `keep` (1 .. n_blocks - 1), so that the cache can go on with n_blocks =
+ * keep: a context of that geometry takes the front of the same buffers (block b keeps its place), the new
+ * ring, pool and shared counts and the same table.
+ *   - In use is every block that is not in the ring.  The k-th block in use from `keep` on, in ascending order, moves to the
+ *     k-th free one below: from[k], to[k], for wf_kv_copy; the other entries of from and to are -1.
+ *   - Table entries of blocks that rows hold (len of them) are rewritten; shared_out [keep] has the counts by new id.
+ *   - ring_out [keep] holds the free ids below `keep` that are left, ascending, from index 0 on, then -1;
+ *     pool_out = {0, their number}.
+ *   - done[0] is 1, or 0 when more than `keep` blocks are in use: then from and to are -1, the table
+ *     stays as it is and ring_out, pool_out and shared_out hold nothing of use.
+ * Arrays: len int32 [n_rows]; from, to int32 [min(keep, n_blocks - keep)]; done int32 [1]; ids int32
+ * [n_blocks] is overwritten.  pool_out, ring_out and shared_out must not be pool_in, ring_in and shared_in.
+ */
+wf_status wf_kv_compact(wf_kv_ctx *ctx, int32_t keep, int32_t n_rows, const int32_t *len, const int32_t *pool_in,
+                        int32_t *pool_out, const int32_t *ring_in, int32_t *ring_out, int32_t *table,
+                        const int32_t *shared_in, int32_t *shared_out, int32_t *from, int32_t *to, int32_t *done,
+                        int32_t *ids, int32_t *work, void *hip_stream);
+
+/*
+ * Copies block from[i] to block to[i], all heads, in n_layers caches `layer_stride` bytes apart (a multiple of 16, at
+ * least the bytes of one; any where n_layers is 1).  Pairs with an id outside the cache (as -1) or
+ * with the same one twice are left out.  No block may be `to` of two pairs, or `to` of one and `from` of another.  Codes of either
+ * kind.  from, to int32 [n].
+ */
+wf_status wf_kv_copy(wf_kv_ctx *ctx, uint8_t *cache, int64_t layer_stride, int32_t n_layers, const int32_t *from,
+                     const int32_t *to, int32_t n, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -11,7 +11,8 @@ from ._lib import (EXPORTS, KEY_DTYPE, SCORE_DTYPE, WF_EHIP, WF_EINVAL, WF_ENOME
                    WF_ST_REPLICA, Context, WFError, load, wf_plan_argmin_noalloc, wf_plan_validate_window,
                    wf_plan_version)
 from ._lib import KV_EXPORTS
-from .kv import (WF_KV_BF16, WF_KV_F16, KVContext, kv_attend, kv_load, kv_step, kv_store, wf_kv_cache_bytes)
+from .kv import (WF_KV_BF16, WF_KV_E4M3, WF_KV_F16, KVContext, kv_attend, kv_compact, kv_copy, kv_fork, kv_load, kv_release, kv_step,
+                 kv_store, wf_kv_cache_bytes)
 
 __all__ = [
     "Context", "WFError", "wf_plan_argmin_noalloc", "SCORE_DTYPE", "KEY_DTYPE", "EXPORTS", "load", "wf_plan_validate_window",
@@ -19,8 +20,8 @@ __all__ = [
     "keys_to_numpy",
     "WF_OK", "WF_EINVAL", "WF_ENOWINDOW", "WF_ENOMEM", "WF_EHIP", "WF_EUNSUPPORTED",
     "WF_ST_INELIGIBLE", "WF_ST_CAPACITY", "WF_ST_REPLICA", "WF_SEARCH_UNIFORM", "WF_SEARCH_RULES",
-    "KVContext", "KV_EXPORTS", "WF_KV_BF16", "WF_KV_F16", "kv_step", "kv_store", "kv_load", "kv_attend",
-    "wf_kv_cache_bytes",
+    "KVContext", "KV_EXPORTS", "WF_KV_BF16", "WF_KV_F16", "WF_KV_E4M3", "kv_step", "kv_store", "kv_load", "kv_attend",
+    "kv_fork", "kv_release", "kv_compact", "kv_copy", "wf_kv_cache_bytes",
 ]
 
 

@@ -51,7 +51,8 @@ EXPORTS = ("wf_plan_ctx_create", "wf_plan_ctx_destroy", "wf_plan_last_error",
 
 # every symbol declared in include/wf_kv.h
 KV_EXPORTS = ("wf_kv_cache_bytes", "wf_kv_ctx_create", "wf_kv_ctx_destroy", "wf_kv_last_error",
-              "wf_kv_step", "wf_kv_store", "wf_kv_load", "wf_kv_attend")
+              "wf_kv_step", "wf_kv_store", "wf_kv_load", "wf_kv_attend", "wf_kv_fork", "wf_kv_release", "wf_kv_compact",
+              "wf_kv_copy")
 
 
 class WFError(RuntimeError):
@@ -160,6 +161,10 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.wf_kv_store.argtypes = [vp, vp, vp, vp, i64, i64, i64, i32] + [vp] * 6
     lib.wf_kv_load.argtypes = [vp, vp, vp, i32, vp, vp, vp]
     lib.wf_kv_attend.argtypes = [vp, vp, i64, i32, vp, vp, vp, vp, vp, i32, f32, i32, i32, i32, vp, vp]
+    lib.wf_kv_fork.argtypes = [vp, vp, vp, vp, i32, i32] + [vp] * 13
+    lib.wf_kv_release.argtypes = [vp, vp, i32] + [vp] * 10
+    lib.wf_kv_compact.argtypes = [vp, i32, i32] + [vp] * 14
+    lib.wf_kv_copy.argtypes = [vp, vp, i64, i32, vp, vp, i32, vp]
     for name in KV_EXPORTS:
         if name not in ("wf_kv_ctx_destroy", "wf_kv_last_error"):
             getattr(lib, name).restype = i32

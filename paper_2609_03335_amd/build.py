@@ -14,7 +14,8 @@ LIB_NAME = "libwfplan.so"
 LIB_PATH = os.path.join(PKG, LIB_NAME)
 BIND_PATH = os.path.join(PKG, "_kvbind.so")
 SOURCES = ["host.hip", "score.hip", "score_keys.hip", "argmin.hip", "prefix.hip", "lean.hip",
-           "lanes.hip", "kv_host.hip", "kv_step.hip", "kv_store.hip", "kv_attend.hip"]
+           "lanes.hip", "kv_host.hip", "kv_step.hip", "kv_store.hip", "kv_attend.hip",
+           "kv8_store.hip", "kv8_attend.hip", "kv_pages.hip"]
 ARCH = "gfx950"
 
 HIP_FLAGS = [
@@ -34,7 +35,7 @@ HIP_FLAGS = [
 def flags(src: str) -> list:
     """Compiler flags of a source.  The cache kernels (kv_*) take the default
     schedule: the compiler fails on attention with the other."""
-    if not src.startswith("kv_"):
+    if not src.startswith(("kv_", "kv8_")):
         return HIP_FLAGS
     return [f for f in HIP_FLAGS if "sched-strategy" not in f and f != "-mllvm"]
 

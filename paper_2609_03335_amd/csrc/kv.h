@@ -18,6 +18,7 @@ struct Geo {
   int b, b_log2;        // tokens per block
   int n_blocks, width;  // blocks of the cache, of a row
   int cell;             // bytes of a cell
+  bool e4m3;            // 8-bit codes
 };
 
 struct StepArgs {
@@ -65,6 +66,49 @@ struct AttendArgs {
   void* out;
 };
 
+struct ForkArgs {
+  const int32_t *src, *dst, *tokens;
+  int n_forks, n_rows;
+  const int32_t* len_in;
+  int32_t* len_out;
+  const int32_t* pool_in;
+  int32_t* pool_out;
+  const int32_t* ring;
+  int32_t* table;
+  const int32_t* shared_in;
+  int32_t *shared_out, *from, *to;
+  uint8_t* granted;
+};
+
+struct ReleaseArgs {
+  const uint8_t* release;
+  int n_rows;
+  const int32_t* len_in;
+  int32_t* len_out;
+  const int32_t* pool_in;
+  int32_t *pool_out, *ring;
+  const int32_t *table, *shared_in;
+  int32_t *shared_out, *work;
+};
+
+struct CompactArgs {
+  int keep, n_rows;
+  const int32_t *len, *pool_in;
+  int32_t* pool_out;
+  const int32_t* ring_in;
+  int32_t *ring_out, *table;
+  const int32_t* shared_in;
+  int32_t *shared_out, *from, *to, *done, *ids, *work;
+};
+
+struct CopyArgs {
+  uint8_t* cache;
+  int64_t layer_stride;
+  int n_layers;
+  const int32_t *from, *to;
+  int n;
+};
+
 // The work area of launch_attend: partial sums, the number of shares that wrote
 // those of each query's head, and counts of shares done, 0 between launches.  A context has one for each of
 // the first kAreas streams that attend; without one (all sizes 0) no tokens are shared out.
@@ -83,6 +127,16 @@ hipError_t launch_step(const Geo& g, const StepArgs& a, hipStream_t s);
 hipError_t launch_store(const Geo& g, int dtype, const StoreArgs& a, hipStream_t s);
 hipError_t launch_load(const Geo& g, int dtype, const LoadArgs& a, hipStream_t s);
 hipError_t launch_attend(const Geo& g, int dtype, const AttendArgs& a, const AttendWork& w, hipStream_t s);
+
+// The same for a cache of 8-bit codes.
+hipError_t launch_store8(const Geo& g, int dtype, const StoreArgs& a, hipStream_t s);
+hipError_t launch_load8(const Geo& g, int dtype, const LoadArgs& a, hipStream_t s);
+hipError_t launch_attend8(const Geo& g, int dtype, const AttendArgs& a, const AttendWork& w, hipStream_t s);
+
+hipError_t launch_fork(const Geo& g, const ForkArgs& a, hipStream_t s);
+hipError_t launch_release(const Geo& g, const ReleaseArgs& a, hipStream_t s);
+hipError_t launch_compact(const Geo& g, const CompactArgs& a, hipStream_t s);
+hipError_t launch_copy(const Geo& g, const CopyArgs& a, int n_cu, hipStream_t s);
 
 // A 16-bit type of the queries and values: to and from fp32 (nearest even).
 struct Bf16 {

@@ -1,4 +1,4 @@
-// Host part of the paged 4-bit cache: argument checks, contexts, launches.
+// Host part of the paged cache: argument checks, contexts, launches.
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -46,12 +46,15 @@ wf_status check_desc(const wf_kv_desc* d) {
   if (d->max_blocks < 1 || d->max_blocks > WF_KV_MAX_WIDTH || (int64_t)d->max_blocks * b > (1ll << 30))
     return fail(nullptr, WF_EINVAL, "max_blocks=%d outside [1, %d] or rows above 2^30 tokens", d->max_blocks,
                 WF_KV_MAX_WIDTH);
-  if (d->dtype != WF_KV_BF16 && d->dtype != WF_KV_F16)
-    return fail(nullptr, WF_EINVAL, "dtype=%d is not WF_KV_BF16 or WF_KV_F16", d->dtype);
+  const int type = d->dtype & ~WF_KV_E4M3;
+  if (type != WF_KV_BF16 && type != WF_KV_F16)
+    return fail(nullptr, WF_EINVAL, "dtype=%d is not WF_KV_BF16 or WF_KV_F16, with or without WF_KV_E4M3", d->dtype);
   return WF_OK;
 }
 
-int64_t cell_bytes(const wf_kv_desc* d) { return (int64_t)d->block_tokens * (d->head_dim + 4); }
+int64_t cell_bytes(const wf_kv_desc* d) {
+  return d->dtype & WF_KV_E4M3 ? 2ll * d->block_tokens * d->head_dim + 16 : (int64_t)d->block_tokens * (d->head_dim + 4);
+}
 
 // Makes the context's device the current one for a scope.
 struct OnDevice {
@@ -117,7 +120,7 @@ wf_status wf_kv_ctx_create(int hip_device, const wf_kv_desc* desc, wf_kv_ctx** o
   wf_kv_ctx* ctx = new (std::nothrow) wf_kv_ctx();
   if (!ctx) return fail(nullptr, WF_ENOMEM, "out of host memory");
   ctx->device = hip_device;
-  ctx->dtype = desc->dtype;
+  ctx->dtype = desc->dtype & ~WF_KV_E4M3;
   wfkv::Geo& g = ctx->g;
   g.hq = desc->q_heads;
   g.hk = desc->kv_heads;
@@ -128,6 +131,7 @@ wf_status wf_kv_ctx_create(int hip_device, const wf_kv_desc* desc, wf_kv_ctx** o
   g.n_blocks = desc->n_blocks;
   g.width = desc->max_blocks;
   g.cell = (int)cell_bytes(desc);
+  g.e4m3 = (desc->dtype & WF_KV_E4M3) != 0;
   wf_status made = launch(ctx, "wf_kv_ctx_create", [&] {
     hipError_t e = hipDeviceGetAttribute(&ctx->n_cu, hipDeviceAttributeMultiprocessorCount, hip_device);
     if (e == hipSuccess) e = hipMalloc(&ctx->areas, wfkv::kAreas * wfkv::kAreaBytes);
@@ -202,7 +206,7 @@ wf_status wf_kv_store(wf_kv_ctx* ctx, const void* q, const void* k, const void* 
       !aligned(how->q_weight, 16) || !aligned(how->k_weight, 16) || !aligned(how->cos_sin, 16))
     return fail(ctx, WF_EINVAL, "q, k, v, q_out, cache, weights and cos_sin must be aligned to 16 bytes");
   const wfkv::StoreArgs a{q, k, v, q_stride, k_stride, v_stride, n_tokens, *how, pos, slot, q_out, cache};
-  return launch(ctx, "wf_kv_store", [&] { return wfkv::launch_store(g, ctx->dtype, a, (hipStream_t)hip_stream); });
+  return launch(ctx, "wf_kv_store", [&] { return (ctx->g.e4m3 ? wfkv::launch_store8 : wfkv::launch_store)(g, ctx->dtype, a, (hipStream_t)hip_stream); });
 }
 
 wf_status wf_kv_load(wf_kv_ctx* ctx, const uint8_t* cache, const int64_t* slot, int32_t n_tokens, void* k_out,
@@ -215,7 +219,7 @@ wf_status wf_kv_load(wf_kv_ctx* ctx, const uint8_t* cache, const int64_t* slot, 
   if (!aligned(cache, 16) || !aligned(k_out, 16) || !aligned(v_out, 16))
     return fail(ctx, WF_EINVAL, "cache, k_out and v_out must be aligned to 16 bytes");
   const wfkv::LoadArgs a{cache, slot, n_tokens, k_out, v_out};
-  return launch(ctx, "wf_kv_load", [&] { return wfkv::launch_load(ctx->g, ctx->dtype, a, (hipStream_t)hip_stream); });
+  return launch(ctx, "wf_kv_load", [&] { return (ctx->g.e4m3 ? wfkv::launch_load8 : wfkv::launch_load)(ctx->g, ctx->dtype, a, (hipStream_t)hip_stream); });
 }
 
 wf_status wf_kv_attend(wf_kv_ctx* ctx, const void* q, int64_t q_stride, int32_t n_tokens, const uint8_t* cache,
@@ -240,7 +244,76 @@ wf_status wf_kv_attend(wf_kv_ctx* ctx, const void* q, int64_t q_stride, int32_t 
   const wfkv::AttendArgs a{q, q_stride, n_tokens, cache, table, kv_len, q_off, pos, n_rows, scale,
                            window, max_q, max_kv, out};
   const wfkv::AttendWork work = area_of(ctx, hip_stream);
-  return launch(ctx, "wf_kv_attend", [&] { return wfkv::launch_attend(g, ctx->dtype, a, work, (hipStream_t)hip_stream); });
+  return launch(ctx, "wf_kv_attend", [&] { return (g.e4m3 ? wfkv::launch_attend8 : wfkv::launch_attend)(g, ctx->dtype, a, work, (hipStream_t)hip_stream); });
+}
+
+wf_status wf_kv_fork(wf_kv_ctx* ctx, const int32_t* src, const int32_t* dst, const int32_t* tokens, int32_t n_forks,
+                     int32_t n_rows, const int32_t* len_in, int32_t* len_out, const int32_t* pool_in,
+                     int32_t* pool_out, const int32_t* ring, int32_t* table, const int32_t* shared_in,
+                     int32_t* shared_out, int32_t* from, int32_t* to, uint8_t* granted, int32_t* work,
+                     void* hip_stream) {
+  if (!ctx) return null_ctx();
+  if (n_forks < 0 || n_forks > WF_KV_MAX_FORKS) return fail(ctx, WF_EINVAL, "n_forks=%d outside [0, %d]", n_forks, WF_KV_MAX_FORKS);
+  if (n_rows < 0 || n_rows > WF_KV_MAX_ROWS) return fail(ctx, WF_EINVAL, "n_rows=%d outside [0, %d]", n_rows, WF_KV_MAX_ROWS);
+  if (!pool_in || !pool_out || !ring || !shared_in || !shared_out || !work)
+    return fail(ctx, WF_EINVAL, "pool_in, pool_out, ring, shared_in, shared_out or work is NULL");
+  if (n_rows && (!len_in || !len_out || !table)) return fail(ctx, WF_EINVAL, "a row array (len_in, len_out, table) is NULL");
+  if (n_forks && (!src || !dst || !tokens || !from || !to || !granted))
+    return fail(ctx, WF_EINVAL, "an array of forks (src, dst, tokens, from, to, granted) is NULL");
+  if ((n_rows && len_in == len_out) || pool_in == pool_out || shared_in == shared_out)
+    return fail(ctx, WF_EINVAL, "len_out, pool_out and shared_out must not be len_in, pool_in and shared_in");
+  const wfkv::ForkArgs a{src, dst, tokens, n_forks, n_rows, len_in, len_out, pool_in, pool_out,
+                         ring, table, shared_in, shared_out, from, to, granted};
+  return launch(ctx, "wf_kv_fork", [&] { return wfkv::launch_fork(ctx->g, a, (hipStream_t)hip_stream); });
+}
+
+wf_status wf_kv_release(wf_kv_ctx* ctx, const uint8_t* release, int32_t n_rows, const int32_t* len_in,
+                        int32_t* len_out, const int32_t* pool_in, int32_t* pool_out, int32_t* ring,
+                        const int32_t* table, const int32_t* shared_in, int32_t* shared_out, int32_t* work,
+                        void* hip_stream) {
+  if (!ctx) return null_ctx();
+  if (n_rows < 0 || n_rows > WF_KV_MAX_ROWS) return fail(ctx, WF_EINVAL, "n_rows=%d outside [0, %d]", n_rows, WF_KV_MAX_ROWS);
+  if (!pool_in || !pool_out || !ring || !shared_in || !shared_out || !work)
+    return fail(ctx, WF_EINVAL, "pool_in, pool_out, ring, shared_in, shared_out or work is NULL");
+  if (n_rows && (!release || !len_in || !len_out || !table))
+    return fail(ctx, WF_EINVAL, "a row array (release, len_in, len_out, table) is NULL");
+  if ((n_rows && len_in == len_out) || pool_in == pool_out || shared_in == shared_out)
+    return fail(ctx, WF_EINVAL, "len_out, pool_out and shared_out must not be len_in, pool_in and shared_in");
+  const wfkv::ReleaseArgs a{release, n_rows, len_in, len_out, pool_in, pool_out, ring, table, shared_in, shared_out, work};
+  return launch(ctx, "wf_kv_release", [&] { return wfkv::launch_release(ctx->g, a, (hipStream_t)hip_stream); });
+}
+
+wf_status wf_kv_compact(wf_kv_ctx* ctx, int32_t keep, int32_t n_rows, const int32_t* len, const int32_t* pool_in,
+                        int32_t* pool_out, const int32_t* ring_in, int32_t* ring_out, int32_t* table,
+                        const int32_t* shared_in, int32_t* shared_out, int32_t* from, int32_t* to, int32_t* done,
+                        int32_t* ids, int32_t* work, void* hip_stream) {
+  if (!ctx) return null_ctx();
+  if (keep < 1 || keep >= ctx->g.n_blocks) return fail(ctx, WF_EINVAL, "keep=%d outside [1, %d]", keep, ctx->g.n_blocks - 1);
+  if (n_rows < 0 || n_rows > WF_KV_MAX_ROWS) return fail(ctx, WF_EINVAL, "n_rows=%d outside [0, %d]", n_rows, WF_KV_MAX_ROWS);
+  if (!pool_in || !pool_out || !ring_in || !ring_out || !shared_in || !shared_out)
+    return fail(ctx, WF_EINVAL, "pool_in, pool_out, ring_in, ring_out, shared_in or shared_out is NULL");
+  if (!from || !to || !done || !ids || !work) return fail(ctx, WF_EINVAL, "from, to, done, ids or work is NULL");
+  if (n_rows && (!len || !table)) return fail(ctx, WF_EINVAL, "a row array (len, table) is NULL");
+  if (pool_in == pool_out || ring_in == ring_out || shared_in == shared_out)
+    return fail(ctx, WF_EINVAL, "pool_out, ring_out and shared_out must not be pool_in, ring_in and shared_in");
+  const wfkv::CompactArgs a{keep, n_rows, len, pool_in, pool_out, ring_in, ring_out, table,
+                            shared_in, shared_out, from, to, done, ids, work};
+  return launch(ctx, "wf_kv_compact", [&] { return wfkv::launch_compact(ctx->g, a, (hipStream_t)hip_stream); });
+}
+
+wf_status wf_kv_copy(wf_kv_ctx* ctx, uint8_t* cache, int64_t layer_stride, int32_t n_layers, const int32_t* from,
+                     const int32_t* to, int32_t n, void* hip_stream) {
+  if (!ctx) return null_ctx();
+  const wfkv::Geo& g = ctx->g;
+  if (n < 0 || n > WF_KV_MAX_BLOCKS) return fail(ctx, WF_EINVAL, "n=%d outside [0, %d]", n, WF_KV_MAX_BLOCKS);
+  if (n_layers < 0 || n_layers > WF_KV_MAX_LAYERS) return fail(ctx, WF_EINVAL, "n_layers=%d outside [0, %d]", n_layers, WF_KV_MAX_LAYERS);
+  if (n_layers > 1 && (layer_stride % 16 || layer_stride < (int64_t)g.n_blocks * g.hk * g.cell))
+    return fail(ctx, WF_EINVAL, "layer_stride is below the bytes of a cache or not a multiple of 16");
+  if (n == 0 || n_layers == 0) return WF_OK;
+  if (!cache || !from || !to) return fail(ctx, WF_EINVAL, "cache, from or to is NULL");
+  if (!aligned(cache, 16)) return fail(ctx, WF_EINVAL, "cache must be aligned to 16 bytes");
+  const wfkv::CopyArgs a{cache, n_layers > 1 ? layer_stride : 0, n_layers, from, to, n};
+  return launch(ctx, "wf_kv_copy", [&] { return wfkv::launch_copy(g, a, ctx->n_cu, (hipStream_t)hip_stream); });
 }
 
 }  // extern "C"

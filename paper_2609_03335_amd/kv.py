@@ -1,4 +1,4 @@
-"""The paged 4-bit key/value cache of a replica: binding of include/wf_kv.h
+"""The paged key/value cache of a replica, in 4 or 8 bits: binding of include/wf_kv.h
 (same names) and helpers that allocate the outputs.  Only marshalling: every
 step runs in the gfx950 kernels.
 
@@ -16,18 +16,23 @@ from typing import Optional
 from ._lib import WF_OK, WFError, _buf, _stream, load, wf_kv_desc, wf_kv_norm_rope
 
 WF_KV_BF16, WF_KV_F16 = 0, 1
+WF_KV_E4M3 = 16
+WF_KV_PAGES_WORK = 1024
 _TYPES = {"bf16": WF_KV_BF16, "f16": WF_KV_F16}
+_CODES = {"e2m1": 0, "e4m3": WF_KV_E4M3}
 
 
-def _desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, dtype) -> wf_kv_desc:
-    return wf_kv_desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, _TYPES.get(dtype, dtype))
+def _desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, dtype, codes) -> wf_kv_desc:
+    if codes not in _CODES:
+        raise ValueError(f"codes: {codes!r} is not one of {', '.join(_CODES)}")
+    return wf_kv_desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, _TYPES.get(dtype, dtype) | _CODES[codes])
 
 
 def wf_kv_cache_bytes(q_heads: int, kv_heads: int, head_dim: int, block_tokens: int, n_blocks: int,
-                      max_blocks: int = 1, dtype="bf16") -> int:
+                      max_blocks: int = 1, dtype="bf16", codes="e2m1") -> int:
     """Bytes of one layer's cache (host only)."""
     lib, out = load(), ctypes.c_int64()
-    d = _desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, dtype)
+    d = _desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, dtype, codes)
     st = lib.wf_kv_cache_bytes(ctypes.byref(d), ctypes.byref(out))
     if st != WF_OK:
         raise WFError(st, lib.wf_kv_last_error(None).decode())
@@ -35,7 +40,8 @@ def wf_kv_cache_bytes(q_heads: int, kv_heads: int, head_dim: int, block_tokens: 
 
 
 class KVContext:
-    """A wf_kv_ctx on one HIP device: the geometry of a cache.  Tensor
+    """A wf_kv_ctx on one HIP device: the geometry of a cache, of 4-bit codes with a scale for each token and head
+    (codes="e2m1") or of 8-bit ones with a scale for each block and head ("e4m3").  Tensor
     arguments are checked before any call reaches the library (GPU tensor, the
     context's device, enough bytes, type or size of the elements, length of the rows
     of block tables and rotations).
@@ -46,10 +52,10 @@ class KVContext:
     stream must not overlap.  One thread at a time may use a context."""
 
     def __init__(self, device: int = 0, *, q_heads: int, kv_heads: int, head_dim: int, block_tokens: int,
-                 n_blocks: int, max_blocks: int, dtype="bf16"):
+                 n_blocks: int, max_blocks: int, dtype="bf16", codes="e2m1"):
         self.lib = load()
         self.handle = None
-        d = _desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, dtype)
+        d = _desc(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, dtype, codes)
         h = ctypes.c_void_p()
         st = self.lib.wf_kv_ctx_create(device, ctypes.byref(d), ctypes.byref(h))
         if st != WF_OK:
@@ -58,13 +64,15 @@ class KVContext:
         self.device = device
         self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
         self.block_tokens, self.n_blocks, self.max_blocks = block_tokens, n_blocks, max_blocks
-        self.dtype, self.torch_dtype = d.dtype, torch_type(d.dtype)
+        self.codes = "e4m3" if d.dtype & WF_KV_E4M3 else "e2m1"
+        self.dtype = d.dtype & ~WF_KV_E4M3
+        self.torch_dtype = torch_type(self.dtype)
         self._current = _current_stream()
         self._bind = _bind() if self._current is not None else None
-        self.cache_bytes = n_blocks * kv_heads * block_tokens * (head_dim + 4)
+        self.cache_bytes = wf_kv_cache_bytes(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, d.dtype)
         if self._bind is not None:
             self._geometry = self._bind.geometry(h.value, device, q_heads, kv_heads, head_dim, n_blocks, max_blocks,
-                                                 self.cache_bytes, d.dtype == WF_KV_F16)
+                                                 self.cache_bytes, self.dtype == WF_KV_F16)
 
     def _check(self, st):
         if st != WF_OK:
@@ -182,6 +190,42 @@ class KVContext:
             self._rows(table, self.max_blocks, 4 * r * self.max_blocks, "table"), b(kv_len, 4 * r, "kv_len"), b(q_off, 4 * r + 4, "q_off"),
             b(pos, 4 * n, "pos"), int(n_rows), float(scale), int(window), int(max_q), int(max_kv),
             self._wide(out, 2 * n * self.q_heads * self.head_dim, "out"), self._s(stream)))
+
+    def wf_kv_fork(self, src, dst, tokens, n_forks: int, n_rows: int, len_in, len_out, pool_in, pool_out, ring, table, shared_in,
+                   shared_out, from_, to, granted, work, stream=None) -> None:
+        b, f, r, n = self._b, max(int(n_forks), 0), max(int(n_rows), 0), self.n_blocks
+        self._check(self.lib.wf_kv_fork(
+            self.handle, b(src, 4 * f, "src"), b(dst, 4 * f, "dst"), b(tokens, 4 * f, "tokens"), int(n_forks), int(n_rows),
+            b(len_in, 4 * r, "len_in"), b(len_out, 4 * r, "len_out"), b(pool_in, 8, "pool_in"), b(pool_out, 8, "pool_out"),
+            b(ring, 4 * n, "ring"), self._rows(table, self.max_blocks, 4 * r * self.max_blocks, "table"),
+            b(shared_in, 4 * n, "shared_in"), b(shared_out, 4 * n, "shared_out"), b(from_, 4 * f, "from"), b(to, 4 * f, "to"),
+            b(granted, f, "granted", 1), b(work, 4 * WF_KV_PAGES_WORK, "work"), self._s(stream)))
+
+    def wf_kv_release(self, release, n_rows: int, len_in, len_out, pool_in, pool_out, ring, table, shared_in, shared_out, work,
+                      stream=None) -> None:
+        b, r, n = self._b, max(int(n_rows), 0), self.n_blocks
+        self._check(self.lib.wf_kv_release(
+            self.handle, b(release, r, "release", 1), int(n_rows), b(len_in, 4 * r, "len_in"), b(len_out, 4 * r, "len_out"),
+            b(pool_in, 8, "pool_in"), b(pool_out, 8, "pool_out"), b(ring, 4 * n, "ring"),
+            self._rows(table, self.max_blocks, 4 * r * self.max_blocks, "table"), b(shared_in, 4 * n, "shared_in"),
+            b(shared_out, 4 * n, "shared_out"), b(work, 4 * WF_KV_PAGES_WORK, "work"), self._s(stream)))
+
+    def wf_kv_compact(self, keep: int, n_rows: int, len_, pool_in, pool_out, ring_in, ring_out, table, shared_in, shared_out, from_, to,
+                      done, ids, work, stream=None) -> None:
+        b, r, n, k = self._b, max(int(n_rows), 0), self.n_blocks, max(int(keep), 0)
+        moves = max(min(k, n - k), 0)
+        self._check(self.lib.wf_kv_compact(
+            self.handle, int(keep), int(n_rows), b(len_, 4 * r, "len"), b(pool_in, 8, "pool_in"), b(pool_out, 8, "pool_out"),
+            b(ring_in, 4 * n, "ring_in"), b(ring_out, 4 * k, "ring_out"),
+            self._rows(table, self.max_blocks, 4 * r * self.max_blocks, "table"), b(shared_in, 4 * n, "shared_in"),
+            b(shared_out, 4 * k, "shared_out"), b(from_, 4 * moves, "from"), b(to, 4 * moves, "to"), b(done, 4, "done"),
+            b(ids, 4 * n, "ids"), b(work, 4 * WF_KV_PAGES_WORK, "work"), self._s(stream)))
+
+    def wf_kv_copy(self, cache, from_, to, n: int, *, layers: int = 1, layer_stride: Optional[int] = None, stream=None) -> None:
+        m, step = max(int(n), 0), self.cache_bytes if layer_stride is None else int(layer_stride)
+        need = self.cache_bytes + max(int(layers) - 1, 0) * max(step, 0)
+        self._check(self.lib.wf_kv_copy(self.handle, self._b(cache, need, "cache", 1), step, int(layers), self._b(from_, 4 * m, "from"),
+                                        self._b(to, 4 * m, "to"), int(n), self._s(stream)))
 
     def close(self):
         self._bind = None
@@ -326,3 +370,69 @@ def kv_attend(ctx: KVContext, q, cache, table, kv_len, q_off, pos, *, scale: flo
     ctx.wf_kv_attend(q, n, cache, table, kv_len, q_off, pos, kv_len.shape[0], scale, out.data_ptr(), window=window,
                      max_q=max_q, max_kv=max_kv)
     return out
+
+
+def kv_fork(ctx: KVContext, src, dst, tokens, lens, pool, ring, table, shared, stream=None):
+    """Rows dst[i] begin with the first tokens[i] tokens of rows src[i] and share their whole blocks.  table is
+    updated in place; returns (lens, pool, shared, granted, moves): moves [2, n] are the blocks that kv_copy has to
+    copy in every layer's cache, -1 where there is none.  `shared` is zeros(n_blocks) before the first fork; a batch that has
+    forks ends its rows with kv_release."""
+    if stream is not None:
+        with _made_current(ctx, stream):
+            return kv_fork(ctx, src, dst, tokens, lens, pool, ring, table, shared)
+    import torch
+    n, r, b = src.shape[0], lens.shape[0], ctx.n_blocks
+    if not n == dst.shape[0] == tokens.shape[0]:
+        raise ValueError(f"src, dst and tokens: {n}, {dst.shape[0]} and {tokens.shape[0]} entries")
+    flat = lens.new_empty(r + 2 + b + 2 * n + WF_KV_PAGES_WORK, dtype=torch.int32)
+    granted = lens.new_empty(n, dtype=torch.uint8)
+    lens_out, pool_out, shared_out, moves, work = flat.split((r, 2, b, 2 * n, WF_KV_PAGES_WORK))
+    at = moves.data_ptr()
+    ctx.wf_kv_fork(src, dst, tokens, n, r, lens, lens_out.data_ptr(), pool, pool_out.data_ptr(), ring, table, shared,
+                   shared_out.data_ptr(), at, at + 4 * n, granted.data_ptr(), work.data_ptr())
+    return lens_out, pool_out, shared_out, granted, moves.view(2, n)
+
+
+def kv_release(ctx: KVContext, release, lens, pool, ring, table, shared, stream=None):
+    """Rows with release[r] != 0 (uint8) give up their blocks; those that no other row holds are free.  ring is
+    updated in place; returns (lens, pool, shared)."""
+    if stream is not None:
+        with _made_current(ctx, stream):
+            return kv_release(ctx, release, lens, pool, ring, table, shared)
+    import torch
+    r, b = lens.shape[0], ctx.n_blocks
+    flat = lens.new_empty(r + 2 + b + WF_KV_PAGES_WORK, dtype=torch.int32)
+    lens_out, pool_out, shared_out, work = flat.split((r, 2, b, WF_KV_PAGES_WORK))
+    ctx.wf_kv_release(release, r, lens, lens_out.data_ptr(), pool, pool_out.data_ptr(), ring, table, shared, shared_out.data_ptr(),
+                      work.data_ptr())
+    return lens_out, pool_out, shared_out
+
+
+def kv_compact(ctx: KVContext, keep: int, lens, pool, ring, table, shared, stream=None):
+    """All blocks in use move below `keep`.  table is updated in place; returns (pool, ring, shared, done, moves): moves for
+    kv_copy, the others for a context with n_blocks=keep over the front of the same caches.  done is 0 where more blocks are in
+    use: nothing has moved then."""
+    if stream is not None:
+        with _made_current(ctx, stream):
+            return kv_compact(ctx, keep, lens, pool, ring, table, shared)
+    import torch
+    r, b, k = lens.shape[0], ctx.n_blocks, max(int(keep), 0)
+    m = max(min(k, b - k), 0)
+    flat = lens.new_empty(2 + 2 * k + 2 * m + 1 + b + WF_KV_PAGES_WORK, dtype=torch.int32)
+    pool_out, ring_out, shared_out, moves, done, ids, work = flat.split((2, k, k, 2 * m, 1, b, WF_KV_PAGES_WORK))
+    at = moves.data_ptr()
+    ctx.wf_kv_compact(keep, r, lens, pool, pool_out.data_ptr(), ring, ring_out.data_ptr(), table, shared, shared_out.data_ptr(), at,
+                      at + 4 * m, done.data_ptr(), ids.data_ptr(), work.data_ptr())
+    return pool_out, ring_out, shared_out, done, moves.view(2, m)
+
+
+def kv_copy(ctx: KVContext, cache, moves, layers: int = 1, stream=None) -> None:
+    """Copies blocks moves[0] to moves[1] (those of kv_fork or kv_compact) in `layers` caches that lie one after the other in `cache`."""
+    if stream is not None:
+        with _made_current(ctx, stream):
+            return kv_copy(ctx, cache, moves, layers)
+    if moves.ndim != 2 or moves.shape[0] != 2:
+        raise ValueError(f"moves: shape {tuple(moves.shape)}, [2, n] needed")
+    n = moves.shape[1]
+    at = ctx._b(moves, 8 * n, "moves")
+    ctx.wf_kv_copy(cache, at, at + 4 * n, n, layers=layers)

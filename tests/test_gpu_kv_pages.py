@@ -1,0 +1,399 @@
+"""Blocks that rows share, on the GPU against the oracle of kv8_oracle.py: fork, release, compact, copy, and all of
+them in a batch that is served."""
+import numpy as np
+import pytest
+import torch
+
+import kv8_oracle as E
+import paper_2609_03335_amd as pkg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    assert torch.cuda.is_available(), "GPU tests need a HIP device"
+
+
+def ctx_of(n, width, b=16, codes="e2m1", hq=4, hk=2, d=64):
+    return pkg.KVContext(0, q_heads=hq, kv_heads=hk, head_dim=d, block_tokens=b, n_blocks=n, max_blocks=width, codes=codes)
+
+
+def dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+
+
+def i32(x):
+    return np.asarray(x, np.int32)
+
+
+def state_of(rng, rows, b, width, spare=3, group=3, empty=0.4):
+    """Rows in groups that share what they begin with, some of them empty; a ring that starts anywhere."""
+    lens = rng.integers(0, width * b + 1, rows) * (rng.random(rows) > empty)
+    have = -(-lens // b)
+    table, used, counts = np.full((rows, width), -1), 0, []
+    for r in range(rows):
+        lead = r // group * group
+        common = min(int(lens[lead] // b), int(lens[r] // b), int(rng.integers(0, width + 1))) if r != lead else 0
+        for j in range(have[r]):
+            if j < common:
+                table[r, j] = table[lead, j]
+                counts[table[r, j]] += 1
+            else:
+                table[r, j] = used
+                counts.append(0)
+                used += 1
+    n = max(used + spare, 1)
+    ids = rng.permutation(n)
+    table = np.where(table >= 0, ids[np.maximum(table, 0)], -1)
+    shared = np.zeros(n, int)
+    shared[ids[:used]] = counts
+    head = int(rng.integers(0, n))
+    ring = np.full(n, -7)
+    ring[(head + np.arange(n - used)) % n] = ids[used:]
+    return i32(lens), i32([head, n - used]), i32(ring), i32(table), i32(shared)
+
+
+def same(got, want):
+    for name, x in want.items():
+        assert np.array_equal(got[name].cpu().numpy(), x), name
+
+
+@pytest.mark.parametrize("b", [16, 64])
+@pytest.mark.parametrize("rows,width", [(2, 1), (5, 3), (64, 40), (300, 5), (1500, 9), (40, 3000)])
+def test_fork(rows, width, b):
+    rng = np.random.default_rng(rows + b)
+    lens, pool, ring, table, shared = state_of(rng, rows, b, width, spare=max(1, rows // 4))
+    # rows outside, the same, negative tokens, sources that hold nothing, full targets; no target twice
+    order = rng.permutation(rows)
+    forks = [(int(rng.integers(0, rows)), int(d), int(rng.integers(0, width * b + 30))) for d in order]
+    for k, (s, d, n) in enumerate(((-1, 0, 5), (0, rows, 5), (2 ** 31 - 1, -2 ** 31, 7), (1, 1, 9), (0, 0, -3))):
+        forks.insert(int(rng.integers(0, len(forks) + 1)), (s, d, n))
+    seen, list_ = set(), []
+    for f in forks:                              # (a target of a refused fork may come again)
+        ok = 0 <= f[1] < rows
+        if ok and f[1] in seen:
+            continue
+        seen.add(f[1])
+        list_.append(f)
+    f = i32(list_)
+    with ctx_of(len(ring), width, b) as ctx:
+        for take in (len(list_), 1, 0):
+            want = E.fork([tuple(x) for x in f[:take].tolist()], lens, pool, ring, table, shared, b)
+            t, rg, sh = dev(table), dev(ring), dev(shared)
+            for _ in range(2):   # inputs stay as they were: a second call gives the same
+                out = pkg.kv_fork(ctx, *(dev(f[:take, i]) for i in range(3)), dev(lens), dev(pool), rg, t, sh)
+            if take == 0:
+                want["moves"] = np.zeros((2, 0))
+            same(dict(zip(("lens", "pool", "shared", "granted", "moves"), out), table=t), want)
+            assert np.array_equal(sh.cpu().numpy(), shared) and np.array_equal(rg.cpu().numpy(), ring)
+
+
+@pytest.mark.parametrize("b", [16, 128])
+@pytest.mark.parametrize("rows,width", [(1, 1), (5, 3), (64, 40), (300, 5), (5000, 3), (30, 3000)])
+def test_release(rows, width, b):
+    rng = np.random.default_rng(rows + b)
+    lens, pool, ring, table, shared = state_of(rng, rows, b, width)
+    with ctx_of(len(ring), width, b) as ctx:
+        for share in (0.0, 0.1, 0.6, 1.0):
+            ends = (rng.random(rows) < share).astype(np.uint8) * rng.integers(1, 256, rows).astype(np.uint8)
+            want = E.release(ends, lens, pool, ring, table, shared, b)
+            rg, sh = dev(ring), dev(shared)
+            for _ in range(2):
+                out = pkg.kv_release(ctx, dev(ends), dev(lens), dev(pool), rg, dev(table), sh)
+            same(dict(zip(("lens", "pool", "shared"), out), ring=rg), want)
+            assert np.array_equal(sh.cpu().numpy(), shared)
+
+
+@pytest.mark.parametrize("b", [16, 256])
+@pytest.mark.parametrize("rows,width", [(1, 1), (5, 3), (64, 40), (300, 5), (3000, 3), (30, 3000)])
+def test_compact(rows, width, b):
+    rng = np.random.default_rng(rows + b)
+    lens, pool, ring, table, shared = state_of(rng, rows, b, width, spare=2 + rows // 2)
+    n, used = len(ring), len(ring) - int(pool[1])
+    with ctx_of(n, width, b) as ctx:
+        for keep in {1, max(used - 1, 1), max(used, 1), min(used + 1, n - 1), (max(used, 1) + n) // 2, n - 1}:
+            if not 1 <= keep < n:
+                continue
+            want = E.compact(keep, lens, pool, ring, table, shared, b)
+            t, sh = dev(table), dev(shared)
+            for _ in range(2):   # entries already rewritten stay
+                out = pkg.kv_compact(ctx, keep, dev(lens), dev(pool), dev(ring), t, sh)
+            same(dict(zip(("pool", "ring", "shared", "done", "moves"), out), table=t), want)
+
+
+def test_many_blocks():
+    """A million blocks and a few rows: every part of the ids is counted."""
+    n, b, width, rows = 1_000_003, 16, 40000, 20
+    rng = np.random.default_rng(3)
+    ids = rng.permutation(n)
+    lens = rng.integers(300000, 480000, rows)
+    have = -(-lens // b)
+    table = np.full((rows, width), -1)
+    at = 0
+    for r in range(rows):
+        table[r, :have[r]] = ids[at:at + have[r]]
+        at += have[r]
+    ring = np.full(n, -1)
+    ring[(n - 50 + np.arange(n - at)) % n] = ids[at:]
+    lens, pool, ring, table, shared = i32(lens), i32([n - 50, n - at]), i32(ring), i32(table), np.zeros(n, np.int32)
+    with ctx_of(n, width, b) as ctx:
+        ends = (np.arange(rows) % 3 == 0).astype(np.uint8)
+        rg = dev(ring)
+        out = pkg.kv_release(ctx, dev(ends), dev(lens), dev(pool), rg, dev(table), dev(shared))
+        same(dict(zip(("lens", "pool", "shared"), out), ring=rg), E.release(ends, lens, pool, ring, table, shared, b))
+        t = dev(table)
+        out = pkg.kv_compact(ctx, at + 5, dev(lens), dev(pool), dev(ring), t, dev(shared))
+        same(dict(zip(("pool", "ring", "shared", "done", "moves"), out), table=t), E.compact(at + 5, lens, pool, ring, table, shared, b))
+
+
+@pytest.mark.parametrize("codes", ["e2m1", "e4m3"])
+@pytest.mark.parametrize("hk,d,b,layers", [(1, 64, 16, 1), (2, 64, 16, 3), (3, 128, 64, 2), (2, 256, 256, 1)])
+def test_copy(hk, d, b, layers, codes):
+    rng = np.random.default_rng(d)
+    n = 23
+    with ctx_of(n, 2, b, codes, hq=hk, hk=hk, d=d) as ctx:
+        data = rng.integers(0, 256, (layers, n, ctx.cache_bytes // n), dtype=np.uint8)
+        order = rng.permutation(n)
+        moves = np.stack([order[:9], order[9:18]])
+        moves[:, 3], moves[0, 5], moves[1, 6] = -1, n, -2 ** 31
+        moves[0, 7] = moves[1, 7]
+        guard = torch.full((data.size + 512,), 77, dtype=torch.uint8, device=DEV)
+        cache = guard[256:-256]
+        cache.copy_(dev(data).view(-1))
+        pkg.kv_copy(ctx, cache, dev(i32(moves)), layers=layers)
+        for i, (f, t) in enumerate(moves.T):
+            if i not in (3, 5, 6, 7):
+                data[:, t] = data[:, f]
+        assert np.array_equal(cache.cpu().numpy(), data.reshape(-1))
+        assert (guard[:256] == 77).all() and (guard[-256:] == 77).all()
+        # layers further apart than their bytes; none; no pairs
+        wide = torch.full((layers, ctx.cache_bytes + 48), 9, dtype=torch.uint8, device=DEV)
+        wide[:, :-48] = dev(data).view(layers, -1)
+        m = dev(i32([[order[0]], [order[20]]]))
+        ctx.wf_kv_copy(wide, m[0], m[1], 1, layers=layers, layer_stride=ctx.cache_bytes + 48)
+        data[:, order[20]] = data[:, order[0]]
+        assert np.array_equal(wide[:, :-48].cpu().numpy(), data.reshape(layers, -1)) and (wide[:, -48:] == 9).all()
+        before = wide.clone()
+        ctx.wf_kv_copy(wide, m[0], m[1], 1, layers=0)
+        pkg.kv_copy(ctx, wide, m[:, :0].contiguous(), layers=1)
+        assert torch.equal(wide, before)
+
+
+def test_copy_past_32_bits():
+    with ctx_of(1100, 2, 256, "e4m3", hq=32, hk=32, d=256) as ctx:
+        cache = torch.zeros(ctx.cache_bytes, dtype=torch.uint8, device=DEV)
+        assert ctx.cache_bytes > 1 << 32
+        block = cache.view(1100, -1)
+        block[1098] = torch.arange(block.shape[1], device=DEV).to(torch.uint8)
+        pkg.kv_copy(ctx, cache, dev(i32([[1098, 1098], [3, 1099]])))
+        assert torch.equal(block[3], block[1098]) and torch.equal(block[1099], block[1098]) and not block[1097].any()
+
+
+def test_invalid_device_values_stay_in_bounds():
+    """Anything in the arrays: unspecified results, but nothing outside the arrays is written."""
+    rows, b, width, n = 70, 16, 5, 50
+    rng = np.random.default_rng(5)
+    wild = lambda k: dev(rng.integers(-2 ** 31, 2 ** 31 - 1, k).astype(np.int32))
+    with ctx_of(n, width, b) as ctx:
+        for pool in ([-5, 10 ** 9], [10 ** 9, -3], [7, 50]):
+            guards = []
+
+            def guarded(k):
+                g = torch.full((64 + k + 64,), 77, dtype=torch.int32, device=DEV)
+                g[64:-64] = wild(k)
+                guards.append(g)
+                return g[64:-64]
+            p = dev(i32(pool))
+            table, ring, work = guarded(rows * width), guarded(n), guarded(1024)
+            flags = torch.full((rows,), 1, dtype=torch.uint8, device=DEV)
+            for lens in (wild(rows), dev(i32(rng.integers(0, width * b + 1, rows)))):
+                ctx.wf_kv_fork(dev(i32(rng.integers(-2, rows + 2, rows))), dev(i32(rng.integers(-2, rows + 2, rows))), wild(rows).abs(), rows, rows,
+                               lens, guarded(rows), p, guarded(2), ring, table, guarded(n), guarded(n), guarded(rows), guarded(rows), flags, work)
+                ctx.wf_kv_release(flags, rows, lens, guarded(rows), p, guarded(2), ring, table, guarded(n), guarded(n), work)
+                ctx.wf_kv_compact(20, rows, lens, p, guarded(2), ring, guarded(20), table, guarded(n), guarded(20), guarded(20), guarded(20),
+                                  guarded(1), guarded(n), work)
+            cache = torch.full((64 + ctx.cache_bytes + 64,), 3, dtype=torch.uint8, device=DEV)
+            ctx.wf_kv_copy(cache[64:-64], wild(rows), wild(rows), rows)
+            torch.cuda.synchronize()
+            for g in guards:
+                assert (g[:64] == 77).all() and (g[-64:] == 77).all()
+            assert (cache == 3).all()
+
+
+def test_refusals():
+    n, width, rows = 10, 4, 3
+    z = lambda k, t=torch.int32: torch.zeros(k, dtype=t, device=DEV)
+    with ctx_of(n, width) as ctx:
+        lens, pool, ring, table, shared = z(rows), z(2), z(n), z((rows, width)), z(n)
+        f = z(2)
+        ok = (ctx, f, f, f, lens, pool, ring, table, shared)
+        pkg.kv_fork(*ok)
+        for i, bad in ((1, z(2, torch.int64)), (2, f.cpu()), (3, z(1)), (4, lens.float()), (6, ring[:-1]), (7, z((rows, width + 1))), (8, shared[:-1])):
+            with pytest.raises((ValueError, TypeError)):
+                pkg.kv_fork(*ok[:i], bad, *ok[i + 1:])
+        ok = (ctx, z(rows, torch.uint8), lens, pool, ring, table, shared)
+        pkg.kv_release(*ok)
+        for i, bad in ((1, z(rows)), (1, z(rows - 1, torch.uint8)), (5, table[:2]), (6, shared.long())):
+            with pytest.raises((ValueError, TypeError)):
+                pkg.kv_release(*ok[:i], bad, *ok[i + 1:])
+        for keep in (0, -1, n, n + 1):
+            with pytest.raises(pkg.WFError) as e:
+                pkg.kv_compact(ctx, keep, lens, pool, ring, table, shared)
+            assert e.value.status == pkg.WF_EINVAL
+        cache = z(2 * ctx.cache_bytes, torch.uint8)
+        moves = z((2, 3))
+        pkg.kv_copy(ctx, cache, moves, layers=2)
+        for bad in (lambda: pkg.kv_copy(ctx, cache, moves, layers=3), lambda: pkg.kv_copy(ctx, cache, moves.view(3, 2)),
+                    lambda: pkg.kv_copy(ctx, cache.view(torch.int32), moves), lambda: pkg.kv_copy(ctx, cache.cpu(), moves),
+                    lambda: pkg.kv_copy(ctx, cache, moves.long())):
+            with pytest.raises((ValueError, TypeError)):
+                bad()
+        for bad in (lambda: pkg.kv_copy(ctx, cache, moves, layers=-1), lambda: pkg.kv_copy(ctx, cache[1:], moves),
+                    lambda: ctx.wf_kv_copy(cache.data_ptr(), moves[0], moves[1], 3, layers=2, layer_stride=16),
+                    lambda: ctx.wf_kv_copy(cache.data_ptr(), moves[0], moves[1], 3, layers=2, layer_stride=ctx.cache_bytes + 8),
+                    lambda: ctx.wf_kv_copy(None, moves[0], moves[1], 3),
+                    lambda: ctx.wf_kv_fork(f, f, f, 2, rows, lens, lens, pool, z(2), ring, table, shared, z(n), f, f, z(2, torch.uint8), z(1024)),
+                    lambda: ctx.wf_kv_release(z(rows, torch.uint8), rows, lens, z(rows), pool, z(2), ring, table, shared, shared, z(1024)),
+                    lambda: ctx.wf_kv_fork(f.data_ptr(), 0, 0, 70000, rows, *[0] * 13)):
+            with pytest.raises(pkg.WFError) as e:
+                bad()
+            assert e.value.status == pkg.WF_EINVAL
+
+
+def test_replays():
+    """Fork, copy and release from one graph on changing states: as eager calls."""
+    rng = np.random.default_rng(8)
+    rows, width, b = 20, 6, 16
+    lens, pool, ring, table, shared = (dev(x) for x in state_of(rng, rows, b, width, spare=30))
+    n = ring.numel()
+    src = torch.zeros(4, dtype=torch.int32, device=DEV)
+    dst, tokens, ends = torch.zeros_like(src), torch.zeros_like(src), torch.zeros(rows, dtype=torch.uint8, device=DEV)
+    with ctx_of(n, width, b, "e4m3") as ctx:
+        cache = torch.randint(0, 256, (2 * ctx.cache_bytes,), device=DEV).to(torch.uint8)
+
+        def both(lens, pool, ring, table, shared, cache):
+            lens, pool, shared, granted, moves = pkg.kv_fork(ctx, src, dst, tokens, lens, pool, ring, table, shared)
+            pkg.kv_copy(ctx, cache, moves, layers=2)
+            lens, pool, shared = pkg.kv_release(ctx, ends, lens, pool, ring, table, shared)
+            return lens, pool, shared, granted, moves
+
+        mine = [x.clone() for x in (lens, pool, ring, table, shared, cache)]
+        theirs = [x.clone() for x in mine]
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            both(*[x.clone() for x in mine])
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                out = both(*mine)
+                for x, y in zip((mine[0], mine[1], mine[4]), out):
+                    x.copy_(y)
+        for i in range(6):
+            held = theirs[0].cpu().numpy()
+            free = np.nonzero(held == 0)[0]
+            full = np.nonzero(held > 0)[0]
+            d = np.resize(rng.permutation(free)[:4], 4) if len(free) >= 4 else np.arange(rows, rows + 4)
+            for x, y in ((src, rng.choice(full, 4)), (dst, d), (tokens, rng.integers(1, 90, 4))):
+                x.copy_(dev(i32(y)))
+            ends.copy_(dev((rng.random(rows) < 0.15).astype(np.uint8)))
+            graph.replay()
+            torch.cuda.synchronize()
+            want = both(*theirs)
+            for x, y in zip(out, want):
+                assert torch.equal(x, y), i
+            theirs[0], theirs[1], theirs[4] = want[:3]
+            assert torch.equal(mine[3], theirs[3]) and torch.equal(mine[5], theirs[5]) and torch.equal(mine[2], theirs[2])
+
+
+@pytest.mark.parametrize("codes", ["e2m1", "e4m3"])
+def test_rows_that_share_are_served_as_if_they_did_not(codes):
+    """A prompt, forks of it (whole and from earlier points), steps of all rows, a release, a compaction onto the front of the same
+    caches and more steps: what each row holds and attends to is what a row of its own, with the same tokens, does."""
+    hq, hk, d, b, n, rows, width, layers = 4, 2, 64, 16, 80, 6, 10, 2
+    rng = np.random.default_rng(9)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    draw = lambda t: torch.randn(layers, t, hq + 2 * hk, d, generator=g, device=DEV).to(torch.bfloat16)
+    zero = lambda k, t=torch.int32: torch.zeros(k, dtype=t, device=DEV)
+
+    class Batch:
+        def __init__(self, blocks):
+            self.ctx = ctx_of(blocks, width, b, codes, hq, hk, d)
+            self.lens, self.pool, self.ring = zero(rows), dev(i32([0, blocks])), torch.randperm(blocks, generator=g, device=DEV).int()
+            self.table, self.shared = torch.full((rows, width), -1, dtype=torch.int32, device=DEV), zero(blocks)
+            self.cache = torch.full((layers, self.ctx.cache_bytes), 255, dtype=torch.uint8, device=DEV)
+
+        def step(self, new, x):
+            T = sum(max(k, 0) for k in new)
+            self.lens, self.pool, off, slot, pos, ok = pkg.kv_step(self.ctx, dev(i32(new)), T, self.lens, self.pool, self.ring, self.table)
+            assert ok.tolist() == [int(k >= 0) for k in new]
+            outs = []
+            for i in range(layers):
+                q = pkg.kv_store(self.ctx, x[i, :, :hq], x[i, :, hq:hq + hk], x[i, :, hq + hk:], pos, slot, self.cache[i])
+                outs.append(pkg.kv_attend(self.ctx, q, self.cache[i], self.table, self.lens, off, pos, scale=0.1))
+            return outs
+
+        def held(self, r):
+            k = int(self.lens[r])
+            j = torch.arange(k, device=DEV)
+            slot = self.table[r].long()[j // b] * b + j % b
+            return [pkg.kv_load(self.ctx, self.cache[i], slot) for i in range(layers)]
+
+    one, own = Batch(n), Batch(n)
+    x = draw(53)
+    one.step([53, 0, 0, 0, 0, 0], x)
+    own.step([53, 0, 0, 0, 0, 0], x)
+    # rows 1 to 3: as long as row 0, and from 48 and 20 tokens on; a fork of a fork in the next call
+    for forks in ([(0, 1, 99), (0, 2, 48), (0, 3, 20)], [(3, 4, 17), (1, 5, 53)]):
+        f = i32(forks)
+        one.lens, one.pool, one.shared, ok, moves = pkg.kv_fork(one.ctx, *(dev(f[:, i]) for i in range(3)), one.lens, one.pool, one.ring, one.table,
+                                                                one.shared)
+        pkg.kv_copy(one.ctx, one.cache, moves, layers=layers)
+        assert ok.all()
+    # rows of their own hold the same: the block that a fork copies is copied, whole blocks too
+    for src, dst, k in ((0, 1, 53), (0, 2, 48), (0, 3, 20), (3, 4, 17), (1, 5, 53)):
+        blocks = -(-k // b)
+        ids = own.ring[int(own.pool[0]):][:blocks].clone()
+        pkg.kv_copy(own.ctx, own.cache, torch.stack([own.table[src, :blocks], ids]).contiguous(), layers=layers)
+        own.table[dst, :blocks] = ids
+        own.lens = own.lens.clone()
+        own.lens[dst] = k
+        own.pool = own.pool + dev(i32([blocks, -blocks]))
+    free = one.pool[1].item()
+    assert free == n - 4 - 4 and own.pool[1].item() == n - 4 - 4 - 3 - 2 - 2 - 4   # (one copy each, none for 48 tokens)
+
+    def more(times):
+        for _ in range(times):
+            live = one.lens.tolist()
+            new = [int(rng.integers(0, 9)) if k else 0 for k in live]
+            y = draw(sum(new))
+            for a, c in zip(one.step(new, y), own.step(new, y)):
+                assert torch.equal(a, c)
+        for r in range(rows):
+            for a, c in zip(one.held(r), own.held(r)):
+                assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+
+    more(4)
+    ends = dev(np.array([1, 0, 0, 1, 0, 0], np.uint8))
+    for s in (one, own):
+        s.lens, s.pool, s.shared = pkg.kv_release(s.ctx, ends, s.lens, s.pool, s.ring, s.table, s.shared)
+    more(3)
+    used = n - one.pool[1].item()
+    keep = used + 18
+    assert keep < n
+    one.pool, one.ring, one.shared, done, moves = pkg.kv_compact(one.ctx, keep, one.lens, one.pool, one.ring, one.table, one.shared)
+    pkg.kv_copy(one.ctx, one.cache, moves, layers=layers)
+    assert done.item() == 1 and (moves >= 0).any()
+    one.ctx.close()
+    one.ctx = ctx_of(keep, width, b, codes, hq, hk, d)
+    one.cache = one.cache[:, :one.ctx.cache_bytes]
+    one.cache = [x.contiguous() for x in one.cache]
+    more(4)
+    # all end: every block is free, once
+    one.lens, one.pool, one.shared = pkg.kv_release(one.ctx, torch.ones(rows, dtype=torch.uint8, device=DEV), one.lens, one.pool, one.ring, one.table,
+                                                    one.shared)
+    assert one.pool[1].item() == keep and sorted(one.ring.tolist()) == list(range(keep)) and not one.shared.any()
+    one.ctx.close()
+    own.ctx.close()
