@@ -97,7 +97,7 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
   const int kvh = (int)(item % (unsigned)g.hk), t0 = (int)(item / (unsigned)g.hk) * tile;
   const int span = min(tile + g.b, a.n_tokens - t0);
   const int lane = threadIdx.x % L, group = threadIdx.x / L;
-  if (threadIdx.x == 0) sp.ups = 0, sp.first = INT32_MAX, sp.end = 0;
+  if (threadIdx.x == 0) sp.ups = 0, sp.first = kSpan, sp.end = 0;
   // events: tokens that begin a run, or are not stored
   const int64_t none = -1;
   auto slot_at = [&](int i) {
