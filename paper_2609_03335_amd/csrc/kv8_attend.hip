@@ -317,6 +317,472 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
   }
 }
 
+// Many columns (prompts): the W waves of a workgroup take different columns, 16 C
+// each, and the same tokens, whose codes they turn into operands once, in LDS.
+//
+// The tokens go by in steps of 32 (half h of a unit: tokens g*16 + h*8 .. +7 of its four
+// groups).  Step n's probabilities are taken while the matrix cores multiply those of
+// step n - 1 with their values and the queries with the keys of step n + 1.  LDS holds
+// four steps of keys and of values; during the two steps of unit u the waves write keys
+// 2u + 3 and 2u + 4 and values 2u + 2 and 2u + 3, whose codes they loaded a unit earlier.
+// A chunk of operands is read from LDS while the one before it is multiplied.
+//
+// There is no running maximum: probabilities are taken against a reference that stands
+// from the start, the largest score (f16: with the value's scale) among the last tokens that all of a
+// wave's columns see.  A softmax does not depend on it as long as nothing overflows or vanishes.  For
+// bf16, whose range is that of fp32, the total tells at the end whether it did: then the true maximum is found and
+// the workgroup runs once more, so that the loop itself has no branch and touches the sums with
+// matrix instructions alone.  f16 has 13 powers of two above the reference, which scales that differ from block
+// to block pass often (8,000 tokens with scales of two powers either way: most workgroups), so there the
+// loop looks at each step's largest term and moves the reference where it has to.
+template <int D, int C, int W, class M>
+__global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend8_wide(Geo g, AttendArgs a, Split sp) {
+  constexpr int KS = D / 32, MT = D / 16;
+  constexpr int kFrag = 64;  // 16-byte lanes of an operand
+  // Chunks of CH operands, NC of them to a step's values or keys.  With several, the next
+  // step's values may not replace the last one's: eight steps of LDS, or where that is too
+  // much (VS = 4) a barrier between.
+  constexpr int CH = D == 256 ? 8 : D == 128 ? 2 : 4, NC = D / 16 / CH, VS = NC > 1 && D < 256 ? 8 : 4;
+  constexpr bool kMid = NC > 1 && VS == 4;
+  __shared__ u32x4 kbuf[4][2 * KS][kFrag], vbuf[VS][MT][kFrag];
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  unsigned id = blockIdx.x;
+  const int kvh = (int)(id % (unsigned)g.hk);
+  id /= (unsigned)g.hk;
+  const int split = (int)(id % (unsigned)sp.splits);
+  id /= (unsigned)sp.splits;
+  const int tile0 = sp.tiles - 1 - (int)(id % (unsigned)sp.tiles);
+  const int row = (int)(id / (unsigned)sp.tiles);
+
+  const int q0 = min(max(a.q_off[row], 0), a.n_tokens), q1 = min(max(a.q_off[row + 1], q0), a.n_tokens);
+  const int64_t columns = (int64_t)(q1 - q0) * g.group;
+  const int len = min(max(a.kv_len[row], 0), g.width << g.b_log2);
+  const Pages pages(g, a, row, kvh, len);
+  const float scale = a.scale * kLog2e;
+  __shared__ int range[2];
+
+  for (int64_t tile = tile0; tile * 16 * C * W < columns; tile += sp.tiles) {
+    // (opaque, so that what follows from it is worked out here and not kept in registers
+    // across tiles)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int n = lane & 15, grp = lane >> 4;
+    const int64_t col0 = (tile * W + wave) * 16 * C;
+    u32x4 q[C][KS];
+    int lo[C], hi[C];
+    int lo_min = len, lo_max = 0, hi_min = INT32_MAX, hi_max = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const unsigned col = (unsigned)min(col0 + c * 16 + n, columns - 1);
+      const unsigned i = col / (unsigned)g.group, h = col - i * (unsigned)g.group;
+      const u32x4* src = reinterpret_cast<const u32x4*>((const uint16_t*)a.q + (int64_t)(q0 + i) * a.q_stride +
+                                                        (int64_t)(kvh * g.group + h) * D + grp * 16);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) q[c][k] = src[k / 2 * 8 + k % 2];
+      const Sight see = sight_of(a.pos[q0 + i], len, a.window);
+      lo[c] = see.lo, hi[c] = see.hi;
+      // (what is seen at all: queries that see nothing do not count)
+      lo_min = min(lo_min, lo[c] < hi[c] ? lo[c] : len);
+      lo_max = max(lo_max, lo[c]);
+      hi_min = min(hi_min, hi[c]);
+      hi_max = max(hi_max, lo[c] < hi[c] ? hi[c] : 0);
+    }
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) {
+      lo_min = min(lo_min, __shfl_xor(lo_min, off, 64));
+      lo_max = max(lo_max, __shfl_xor(lo_max, off, 64));
+      hi_min = min(hi_min, __shfl_xor(hi_min, off, 64));
+      hi_max = max(hi_max, __shfl_xor(hi_max, off, 64));
+    }
+    lo_min = __builtin_amdgcn_readfirstlane(lo_min);
+    lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+    hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+    hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+    // the tokens that any column of the workgroup sees
+    if (threadIdx.x == 0) range[0] = len, range[1] = 0;
+    __syncthreads();
+    if (lane == 0) {
+      atomicMin(&range[0], lo_min);
+      atomicMax(&range[1], hi_max);
+    }
+    __syncthreads();
+    const int seen_lo = __builtin_amdgcn_readfirstlane(range[0]), seen_hi = __builtin_amdgcn_readfirstlane(range[1]);
+    const int first = seen_lo >> 6, units = max(0, ((seen_hi + 63) >> 6) - first);
+    const int share = max(kWaves, (units + sp.splits - 1) / sp.splits);
+    const int used = max(1, (units + share - 1) / share);
+    if (split >= used) {
+      __syncthreads();  // range is read by all before it is set again
+      continue;
+    }
+    const int begin = first + split * share, count = min(units - split * share, share);
+
+    // What a wave turns into operands in a unit: of the keys, KP of the KS operands of one
+    // score tile of one of two steps; of the values, VP times VC of the 2 MT operands of two
+    // steps, VC channels side by side: row n of operand r is channel 16 VC (r / VC) + VC n + r % VC.
+    constexpr int KP = KS * 4 / W, KG = KS / KP, VT = 2 * MT / W, VC = VT < 4 ? VT : 4, VP = VT / VC, VJ = MT / VC;
+    static_assert(KP >= 1 && KG * KP == KS && KG * 4 == W && VC * VP * W == 2 * MT, "waves divide the operands");
+    const int kstep = wave / (2 * KG), ktile = wave / KG % 2, kpart = wave % KG;
+    struct Codes {
+      u32x2 k[KP];
+      uint32_t v[VP][2][VC];
+      float ks, vs[VP];  // scales of the keys' and the values' blocks (not kScaled)
+      f32x2 z;           // those of this lane's own tokens (kScaled)
+    };
+    // ... and the blocks they are in, asked for a unit earlier still
+    struct Ids {
+      unsigned k, v[VP], z;
+    };
+    auto ask = [&](int kat, int vat, int zat, Ids& d) __attribute__((always_inline)) {
+      d.k = pages.id(((begin + ((kat + kstep) >> 1)) << 6) + (n >> 2) * 16);
+#pragma unroll
+      for (int x = 0; x < VP; ++x) d.v[x] = pages.id(((begin + ((vat + (wave + x * W) / VJ) >> 1)) << 6) + grp * 16);
+      if constexpr (M::kScaled) d.z = pages.id(((begin + (zat >> 1)) << 6) + grp * 16);
+    };
+    auto load_keys = [&](int step, unsigned id, Codes& w) __attribute__((always_inline)) {
+      const int s = step + kstep, t = (s & 1) * 2 + ktile;
+      const int off = (((begin + (s >> 1)) << 6) + (n >> 2) * 16) & (g.b - 1);
+      const uint8_t* cell = pages.cell(id);
+      const uint8_t* at = cell + (off + t * 4 + (n & 3)) * D + grp * 16;
+      if constexpr (KP == 1) {
+        w.k[0] = *reinterpret_cast<const u32x2*>(at + kpart / 2 * 64 + kpart % 2 * 8);
+      } else {
+#pragma unroll
+        for (int k = 0; k < KP / 2; ++k) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(at + (kpart * KP / 2 + k) * 64);
+          w.k[2 * k] = (u32x2){x[0], x[1]}, w.k[2 * k + 1] = (u32x2){x[2], x[3]};
+        }
+      }
+      if constexpr (!M::kScaled) w.ks = *reinterpret_cast<const float*>(cell + 2 * g.b * D);
+    };
+    auto store_keys = [&](int step, const Codes& w) {
+      const int s = step + kstep;
+#pragma unroll
+      for (int k = 0; k < KP; ++k)
+        kbuf[s & 3][ktile * KS + kpart * KP + k][lane] = operand8<M>(w.k[k][0], w.k[k][1], M::kScaled ? 1.0f : w.ks);
+    };
+    auto load_values = [&](int step, const unsigned (&id)[VP], Codes& w) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < VP; ++x) {
+        const int job = wave + x * W, s = step + job / VJ, r = job % VJ;
+        const int off = ((((begin + (s >> 1)) << 6) + grp * 16) & (g.b - 1)) + (s & 1) * 8;
+        const uint8_t* cell = pages.cell(id[x]);
+        const uint8_t* at = cell + g.b * D + off * D + (r * 16 + n) * (4 * VC);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) __builtin_memcpy(w.v[x][t], __builtin_assume_aligned(at + t * 4 * D, 4 * VC), 4 * VC);
+        if constexpr (!M::kScaled) w.vs[x] = reinterpret_cast<const float*>(cell + 2 * g.b * D)[1];
+      }
+    };
+    auto store_values = [&](int step, Codes& w) {
+#pragma unroll
+      for (int x = 0; x < VP; ++x) {
+        const int job = wave + x * W, s = step + job / VJ, r = job % VJ;
+        // what no query of the workgroup sees may be anything, no number too, which a probability of 0 would not hide
+        const int base = (begin + (s >> 1)) << 6, j0 = base + grp * 16;
+        if (base < seen_lo || base + 64 > seen_hi) {
+          if (j0 + 16 <= seen_lo || j0 >= seen_hi) w.vs[x] = 1.0f;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const uint32_t mask = seen_bytes(j0 + (s & 1) * 8 + t * 4, seen_lo, seen_hi);
+#pragma unroll
+            for (int c = 0; c < VC; ++c) w.v[x][t][c] &= mask;
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < VC; ++c)
+          vbuf[s & (VS - 1)][r * VC + c][lane] = operand8<M>(w.v[x][0][c], w.v[x][1][c], M::kScaled ? 1.0f : w.vs[x]);
+      }
+    };
+    // scales of this lane's tokens in the unit of a step
+    auto load_scales = [&](unsigned id) __attribute__((always_inline)) -> f32x2 {
+      if constexpr (M::kScaled) return *reinterpret_cast<const f32x2*>(pages.cell(id) + 2 * g.b * D);
+      return (f32x2){1.0f, 1.0f};
+    };
+    // ... the keys' times that of the scores, the values' only of what is seen
+    auto scales_of = [&](int u, f32x2 z) __attribute__((always_inline)) -> f32x2 {
+      const int j0 = ((begin + u) << 6) + grp * 16;
+      return (f32x2){z[0] * scale, j0 + 16 <= seen_lo || j0 >= seen_hi ? 1.0f : z[1]};
+    };
+
+    f32x4 o[C][MT];
+    float ref[C], sum[C];
+    u32x4 p[C];
+    f32x4 s[C][2];
+    // a step's operands: of the values RB of the lower, RB of the upper half of the
+    // channels; of the keys KS of each score tile
+    u32x4 op[2][CH];
+    auto read_values = [&](int step, int part, u32x4 (&to)[CH]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < CH; ++x) to[x] = vbuf[step & (VS - 1)][part * CH + x][lane];
+    };
+    auto read_keys = [&](int step, int part, u32x4 (&to)[CH]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < CH; ++x) to[x] = kbuf[step & 3][part * CH + x][lane];
+    };
+    auto outputs = [&](int part, const u32x4 (&from)[CH]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < CH; ++x)
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c][part * CH + x] = M::mma(from[x], p[c], o[c][part * CH + x]);
+    };
+    auto scores = [&](int part, const u32x4 (&from)[CH]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < CH; ++x) {
+        const int e = (part * CH + x) / KS, k = (part * CH + x) % KS;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          if (k == 0) s[c][e] = (f32x4){0, 0, 0, 0};
+          s[c][e] = M::mma(from[x], q[c][k], s[c][e]);
+        }
+      }
+    };
+    // the largest score (kScaled: with the scale of its value) of each column among the tokens of units [u0, u1)
+    // that it sees, straight from the cache
+    auto largest = [&](int u0, int u1, float (&m)[C]) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) m[c] = -INFINITY;
+      for (int u = u0; u < u1; ++u) {
+        const int ktoken = (u << 6) + (n >> 2) * 16, ztoken = (u << 6) + grp * 16;
+        const unsigned kid = pages.id(ktoken), zid = pages.id(ztoken);
+        const uint8_t* kcell = pages.cell(kid);
+        const uint8_t* kat = kcell + ((ktoken & (g.b - 1)) + (n & 3)) * D + grp * 16;
+        const f32x2 z = *reinterpret_cast<const f32x2*>(pages.cell(zid) + 2 * g.b * D);
+        const float kz = z[0] * scale;
+        float vl = 0.0f;
+        if constexpr (M::kScaled) vl = scale_log(z[1]);
+        // (all loads on their way at once)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          f32x4 x[C] = {};
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(kat + t * 4 * D + k / 2 * 64 + k % 2 * 8);
+            const u32x4 kk = operand8<M>(w[0], w[1], 1.0f);
+#pragma unroll
+            for (int c = 0; c < C; ++c) x[c] = M::mma(kk, q[c][k], x[c]);
+          }
+          const int j0 = ztoken + t * 4;
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m[c] = fmaxf(m[c], j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] * kz + vl : -INFINITY);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c) m[c] = column_max(m[c]);
+    };
+
+    auto whole = [&](int u) {
+      const int base = (begin + u) << 6;
+      return base >= lo_max && base + 64 <= hi_min;
+    };
+   for (int pass = 0;; ++pass) {
+    // pass 0 takes the reference from the last unit that all of the wave's columns see
+    // whole, or at all, unless they see the first one whole (below); pass 1 from all.  (A window may hide
+    // that unit from the wave's last queries: they see the next one.)
+    const int near = hi_min >= 64 && ((hi_min >> 6) - 1) << 6 >= lo_max ? (hi_min >> 6) - 1 : max(hi_min - 1, 0) >> 6;
+    if (pass) largest(begin, begin + count, ref);
+    else largest(near, near + (hi_min == 0 || whole(0) ? 0 : M::kScaled && near << 6 < lo_max && (near + 1) << 6 < hi_max ? 2 : 1), ref);
+    // keys of steps 0 to 3, values and scales of steps 0 and 1; all on their way at once
+    Codes w, w0, w2;
+    Ids d, d0, d2, d3;
+    ask(0, 0, 0, d0);
+    ask(2, 2, 2, d2);
+    ask(3, 4, 4, d3);
+    ask(5, 4, 4, d);
+    load_keys(0, d0.k, w0);
+    load_values(0, d0.v, w0);
+    w0.z = load_scales(d0.z);
+    load_keys(2, d2.k, w2);
+    load_values(2, d2.v, w);
+    w.z = load_scales(d2.z);
+    load_keys(3, d3.k, w);
+    store_keys(0, w0);
+    store_values(0, w0);
+    f32x2 now = scales_of(0, w0.z);  // of the unit worked on
+    store_keys(2, w2);  // step 3's come again in unit 0, the same
+    __syncthreads();
+#pragma unroll
+    for (int part = 0; part < NC; ++part) {
+      read_keys(0, part, op[0]);
+      scores(part, op[0]);
+    }
+    if (pass == 0 && whole(0)) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x = s[c][i / 4][i % 4] * (M::kScaled ? now[0] : scale);
+          ref[c] = fmaxf(ref[c], M::kScaled ? x + scale_log(now[1]) : x);
+        }
+        ref[c] = column_max(ref[c]);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      // (f16, none of those tokens in sight: below any score, so that the first one in sight sets it)
+      ref[c] = fabsf(ref[c]) < INFINITY ? ref[c] - M::kAimFixed : M::kScaled ? -FLT_MAX : 0.0f;
+      sum[c] = 0.0f, p[c] = (u32x4){0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < MT; ++k) o[c][k] = (f32x4){0, 0, 0, 0};
+    }
+    // there are no values before step 0's: any finite ones do, the probabilities are 0
+    read_values(0, 0, op[0]);
+    __syncthreads();  // unit 0 writes step 4's keys over step 0's
+
+    auto unit = [&](int u, auto masked) __attribute__((always_inline)) {
+      constexpr bool kMask = decltype(masked)::value;
+      // codes loaded a unit ago into LDS, the next ones on their way
+      store_keys(2 * u + 3, w);
+      if (!kMid) store_values(2 * u + 2, w);
+      const f32x2 next = scales_of(u + 1, w.z);
+      float vlog = 0.0f;
+      if constexpr (M::kScaled) vlog = scale_log(now[1]);
+      load_keys(2 * u + 5, d.k, w);
+      if (!kMid) load_values(2 * u + 4, d.v, w);
+      w.z = load_scales(d.z);
+      if (!kMid) ask(2 * u + 7, 2 * u + 6, 2 * u + 6, d);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int step = 2 * u + h;
+        const int j0 = ((begin + u) << 6) + grp * 16 + h * 8;
+        float x[C][8];
+        // values of the step before; op[part % 2] holds chunk `part`
+#pragma unroll
+        for (int part = 0; part < NC; ++part) {
+          if (part + 1 < NC) read_values(max(step - 1, 0), part + 1, op[(part + 1) % 2]);
+          else read_keys(step + 1, 0, op[(part + 1) % 2]);
+          __builtin_amdgcn_sched_barrier(0);
+          outputs(part, op[part % 2]);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[c][i] = fmaf(s[c][i / 4][i % 4], M::kScaled ? now[0] : scale, -ref[c]);
+            if (kMask) x[c][i] = j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] : -INFINITY;
+          }
+        // f16 ends at 2^16: a term above 2^15 moves the reference
+        if constexpr (M::kScaled) {
+          bool up = false;
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            float m = x[c][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) m = fmaxf(m, x[c][i]);
+            up |= m + vlog > M::kMostLog;
+          }
+          if (__builtin_expect(__any(up), 0)) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+              float m = -INFINITY;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                x[c][i] = s[c][i / 4][i % 4] * now[0];
+                if (kMask) x[c][i] = j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] : -INFINITY;
+                m = fmaxf(m, x[c][i]);
+              }
+              const float r = fmaxf(ref[c], column_max(m + vlog) - M::kAimFixed), keep = __builtin_amdgcn_exp2f(ref[c] - r);
+              ref[c] = r;
+              sum[c] *= keep;
+#pragma unroll
+              for (int k = 0; k < MT; ++k) o[c][k] *= keep;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[c][i] -= r;
+            }
+          }
+        }
+        // keys of the step after
+#pragma unroll
+        for (int part = 0; part < NC; ++part) {
+          if (part + 1 < NC) read_keys(step + 1, part + 1, op[(NC + part + 1) % 2]);
+          else read_values(step, 0, op[(NC + part + 1) % 2]);
+          __builtin_amdgcn_sched_barrier(0);
+          scores(part, op[(NC + part) % 2]);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[c][i] = __builtin_amdgcn_exp2f(x[c][i]);
+            sum[c] += x[c][i];
+            if (M::kScaled) x[c][i] *= now[1];
+          }
+#pragma unroll
+          for (int b = 0; b < 4; ++b) p[c][b] = M::pair(x[c][2 * b], x[c][2 * b + 1]);
+        }
+        if (kMid && h == 0) {
+          // step 2u read the later chunks of step 2u - 1's values, which 2u + 3's replace
+          __syncthreads();
+          store_values(2 * u + 2, w);
+          load_values(2 * u + 4, d.v, w);
+          ask(2 * u + 7, 2 * u + 6, 2 * u + 6, d);
+        }
+      }
+      now = next;
+      __syncthreads();
+    };
+    // (waves may be in different ones of the two loops: each unit has the same barriers in both)
+    for (int u = 0; u < count;) {
+      while (u < count && !whole(u)) unit(u++, std::true_type());
+      while (u < count && whole(u)) unit(u++, std::false_type());
+    }
+#pragma unroll
+    for (int part = 0; part < NC; ++part) {
+      if (part) read_values(max(2 * count - 1, 0), part, op[0]);
+      outputs(part, op[0]);
+    }
+    // was the reference near enough?
+    bool bad = false;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      sum[c] = column_sum(sum[c]);
+      const bool sees = max(lo[c], begin << 6) < min(hi[c], (begin + count) << 6);
+      bool fine = sum[c] >= 0x1p-60f && sum[c] <= 0x1p60f;
+#pragma unroll
+      for (int k = 0; k < MT; ++k) fine &= fabsf(o[c][k][0] + o[c][k][1] + o[c][k][2] + o[c][k][3]) < INFINITY;
+      bad |= !M::kScaled && sees && !fine;
+    }
+    // (also: all have read LDS before the next tile or pass writes it)
+    if (!__syncthreads_or(bad) || pass) break;
+   }
+
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = col0 + c * 16 + n;
+      if (col >= columns) continue;
+      const unsigned i = (unsigned)col / (unsigned)g.group, h = (unsigned)col - i * (unsigned)g.group;
+      const int64_t head = (int64_t)(q0 + i) * g.hq + kvh * g.group + h;
+      const float inv = sum[c] == 0.0f ? 0.0f : 1.0f / sum[c];
+      float* to = sp.part + ((int64_t)split * a.n_tokens * g.hq + head) * (D + 2);
+#pragma unroll
+      for (int r = 0; r < MT; r += VC) {
+        // rows grp*4 + i of operands r .. r + VC - 1: VC channels from 16 r + VC (grp*4 + i) on
+        float v[4 * VC];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int x = 0; x < VC; ++x) v[i * VC + x] = o[c][r + x][i];
+        const int at = r * 16 + grp * 4 * VC;
+#pragma unroll
+        for (int x = 0; x < VC; ++x) {
+          if (used == 1) {
+            const u32x2 b = {M::pair(v[4 * x] * inv, v[4 * x + 1] * inv), M::pair(v[4 * x + 2] * inv, v[4 * x + 3] * inv)};
+            *reinterpret_cast<u32x2*>((uint16_t*)a.out + head * D + at + 4 * x) = b;
+          } else {
+            *reinterpret_cast<f32x2*>(to + at + 4 * x) = (f32x2){v[4 * x], v[4 * x + 1]};
+            *reinterpret_cast<f32x2*>(to + at + 4 * x + 2) = (f32x2){v[4 * x + 2], v[4 * x + 3]};
+          }
+        }
+      }
+      if (grp == 0) {
+        if (used > 1) to[D] = sum[c] == 0.0f ? -INFINITY : ref[c], to[D + 1] = sum[c];
+        if (split == 0 && sp.splits > 1) sp.used[head] = used;
+      }
+    }
+  }
+}
+
 // Few columns (1 or 2 tiles of 16 a workgroup); the tokens are split so that all
 // workgroups run at once.
 template <int D, int C, class M>
@@ -330,10 +796,24 @@ hipError_t narrow(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_
 }
 
 template <int D, class M>
+hipError_t wide(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, hipStream_t s) {
+  constexpr int C = D == 256 ? 1 : 2, W = D == 256 ? 4 : 8, H = kThreads / (D / 4);
+  const Split sp = split_of<D>(g, a, w, columns, 16 * C * W, w.n_cu * 2, kWaves);
+  const hipError_t e = launch(attend8_wide<D, C, W, M>, g, a, sp, 64 * W, s);
+  if (e != hipSuccess || sp.splits == 1) return e;
+  const int64_t heads = (int64_t)a.n_tokens * g.hq;
+  hipLaunchKernelGGL((combine<D, 1, M>), dim3((unsigned)((heads + H - 1) / H)), dim3(kThreads), 0, s, g, a, sp);
+  return hipGetLastError();
+}
+
+template <int D, class M>
 hipError_t by_columns(const Geo& g, const AttendArgs& a, const AttendWork& w, hipStream_t s) {
   const int64_t columns = (int64_t)(a.max_q > 0 ? std::min(a.max_q, a.n_tokens) : a.n_tokens) * g.group;
   if (columns <= 16) return narrow<D, 1, M>(g, a, w, columns, s);
-  return narrow<D, 2, M>(g, a, w, columns, s);
+  const int64_t at_once = w.n_cu * kOcc<D, 2>, narrow_wgs = (int64_t)a.n_rows * g.hk * ((columns + 31) / 32);
+  const bool few = a.max_kv > 0 && narrow_wgs <= at_once && narrow_wgs * a.max_kv <= at_once * 3500;
+  if (columns <= 128 || few) return narrow<D, 2, M>(g, a, w, columns, s);
+  return wide<D, M>(g, a, w, columns, s);
 }
 
 }  // namespace

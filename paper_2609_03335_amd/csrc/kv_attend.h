@@ -58,7 +58,7 @@ struct MmaF16 : F16 {
   // Fixed reference: the largest p z of some tokens that the query sees is 2^2 (a half step that f16 drops,
   // 2^-25, is 2^-27 of it), so that of all may be 14 powers of two above.  (600 normal queries over 9,000
   // keys: up to 10; at 2^6 a sixth of the workgroups had to run twice.)
-  static constexpr float kAim = 12.0f, kAimFixed = 2.0f, kMostTerm = 0x1p15f;
+  static constexpr float kAim = 12.0f, kAimFixed = 2.0f, kMostTerm = 0x1p15f, kMostLog = 15.0f;
   static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }

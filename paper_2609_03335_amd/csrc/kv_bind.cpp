@@ -22,6 +22,10 @@ decltype(&wf_kv_step) g_step;
 decltype(&wf_kv_store) g_store;
 decltype(&wf_kv_load) g_load;
 decltype(&wf_kv_attend) g_attend;
+decltype(&wf_kv_fork) g_fork;
+decltype(&wf_kv_release) g_release;
+decltype(&wf_kv_compact) g_compact;
+decltype(&wf_kv_copy) g_copy;
 
 struct Geometry {
   wf_kv_ctx* ctx;
@@ -125,6 +129,22 @@ at::Tensor fresh(const at::Tensor& like, at::IntArrayRef shape, at::ScalarType t
   return at::empty(shape, like.options().dtype(type));
 }
 
+// The outputs as a tuple.
+template <size_t N>
+PyObject* wrapped(const at::Tensor (&out)[N]) {
+  PyObject* tuple = PyTuple_New(N);
+  if (!tuple) return nullptr;
+  for (size_t i = 0; i < N; ++i) {
+    PyObject* x = THPVariable_Wrap(out[i]);
+    if (!x) {
+      Py_DECREF(tuple);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(tuple, i, x);
+  }
+  return tuple;
+}
+
 // new, n_tokens, lens, pool, ring, table -> (lens, pool, q_off, slot, pos, granted)
 PyObject* step(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -152,17 +172,7 @@ PyObject* step(PyObject*, PyObject* const* args, Py_ssize_t n) {
              (const int32_t*)data(pool), base + r, (int32_t*)data(ring), (int32_t*)data(table), base + r + 2,
              (int64_t*)data(&out[3]), base + 2 * r + 3, (uint8_t*)data(&out[5]), stream);
   if (st != WF_OK) return PyLong_FromLong(st);
-  PyObject* tuple = PyTuple_New(6);
-  if (!tuple) return nullptr;
-  for (int i = 0; i < 6; ++i) {
-    PyObject* x = THPVariable_Wrap(out[i]);
-    if (!x) {
-      Py_DECREF(tuple);
-      return nullptr;
-    }
-    PyTuple_SET_ITEM(tuple, i, x);
-  }
-  return tuple;
+  return wrapped(out);
   END_HANDLE_TH_ERRORS
 }
 
@@ -251,6 +261,116 @@ PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// The arrays of a batch that shares blocks: lens, pool, ring, table, shared, as the calls take them.
+struct Batch {
+  const at::Tensor *lens, *pool, *ring, *table, *shared;
+  int64_t rows = 0;
+  explicit Batch(Args& a)
+      : lens(a.dense(at::kInt)), pool(a.dense(at::kInt)), ring(a.dense(at::kInt)), table(a.dense(at::kInt)), shared(a.dense(at::kInt)) {
+    if (!a.ok) return;
+    if (lens->dim() != 1 || lens->size(0) > WF_KV_MAX_ROWS) {
+      a.ok = false;
+      return;
+    }
+    rows = lens->size(0);
+    a.holds(pool, 2);
+    a.holds(ring, a.g->n_blocks);
+    a.holds(table, rows * a.g->max_blocks);
+    a.rows(table, a.g->max_blocks);
+    a.holds(shared, a.g->n_blocks);
+  }
+  static const int32_t* in(const at::Tensor* t) { return (const int32_t*)data(t); }
+  static int32_t* out(const at::Tensor* t) { return (int32_t*)data(t); }
+};
+
+// src, dst, tokens, lens, pool, ring, table, shared -> (lens, pool, shared, granted, moves)
+PyObject* fork(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(args, n, 10);
+  void* stream = a.address();
+  const at::Tensor *src = a.dense(at::kInt), *dst = a.dense(at::kInt), *tokens = a.dense(at::kInt);
+  const Batch b(a);
+  if (!a.ok || src->dim() != 1 || dst->dim() != 1 || tokens->dim() != 1 || src->size(0) > WF_KV_MAX_FORKS ||
+      dst->size(0) != src->size(0) || tokens->size(0) != src->size(0))
+    return none();
+  const int64_t f = src->size(0), r = b.rows, blocks = a.g->n_blocks;
+  at::AutoDispatchBelowADInplaceOrView plain;
+  const at::Tensor flat = fresh(*b.lens, {r + 2 + blocks + 2 * f + WF_KV_PAGES_WORK}, at::kInt);
+  int32_t* base = static_cast<int32_t*>(flat.data_ptr());
+  int32_t *pool = base + r, *shared = pool + 2, *moves = shared + blocks, *work = moves + 2 * f;
+  const at::Tensor out[5] = {flat.narrow(0, 0, r), flat.narrow(0, r, 2), flat.narrow(0, r + 2, blocks), fresh(*b.lens, {f}, at::kByte),
+                             flat.narrow(0, r + 2 + blocks, 2 * f).view({2, f})};
+  const wf_status st = queued(g_fork, a.g->ctx, Batch::in(src), Batch::in(dst), Batch::in(tokens), (int32_t)f, (int32_t)r, Batch::in(b.lens), base,
+                              Batch::in(b.pool), pool, Batch::in(b.ring), Batch::out(b.table), Batch::in(b.shared), shared, moves, moves + f,
+                              (uint8_t*)data(&out[3]), work, stream);
+  if (st != WF_OK) return PyLong_FromLong(st);
+  return wrapped(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// release, lens, pool, ring, table, shared -> (lens, pool, shared)
+PyObject* release(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(args, n, 8);
+  void* stream = a.address();
+  const at::Tensor* ends = a.dense(at::kByte);
+  const Batch b(a);
+  a.holds(ends, b.rows);
+  if (!a.ok) return none();
+  const int64_t r = b.rows, blocks = a.g->n_blocks;
+  at::AutoDispatchBelowADInplaceOrView plain;
+  const at::Tensor flat = fresh(*b.lens, {r + 2 + blocks + WF_KV_PAGES_WORK}, at::kInt);
+  int32_t* base = static_cast<int32_t*>(flat.data_ptr());
+  const at::Tensor out[3] = {flat.narrow(0, 0, r), flat.narrow(0, r, 2), flat.narrow(0, r + 2, blocks)};
+  const wf_status st = queued(g_release, a.g->ctx, (const uint8_t*)data(ends), (int32_t)r, Batch::in(b.lens), base, Batch::in(b.pool), base + r,
+                              Batch::out(b.ring), Batch::in(b.table), Batch::in(b.shared), base + r + 2, base + r + 2 + blocks, stream);
+  if (st != WF_OK) return PyLong_FromLong(st);
+  return wrapped(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// keep, lens, pool, ring, table, shared -> (pool, ring, shared, done, moves)
+PyObject* compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(args, n, 8);
+  if (!a.ok) return none();
+  void* stream = a.address();
+  const int64_t k = a.integer(1, a.g->n_blocks - 1);
+  const Batch b(a);
+  if (!a.ok) return none();
+  const int64_t blocks = a.g->n_blocks, m = k < blocks - k ? k : blocks - k;
+  at::AutoDispatchBelowADInplaceOrView plain;
+  const at::Tensor flat = fresh(*b.lens, {2 + 2 * k + 2 * m + 1 + blocks + WF_KV_PAGES_WORK}, at::kInt);
+  int32_t* base = static_cast<int32_t*>(flat.data_ptr());
+  int32_t *ring = base + 2, *shared = ring + k, *moves = shared + k, *done = moves + 2 * m, *ids = done + 1, *work = ids + blocks;
+  const at::Tensor out[5] = {flat.narrow(0, 0, 2), flat.narrow(0, 2, k), flat.narrow(0, 2 + k, k), flat.narrow(0, 2 + 2 * k + 2 * m, 1),
+                             flat.narrow(0, 2 + 2 * k, 2 * m).view({2, m})};
+  const wf_status st = queued(g_compact, a.g->ctx, (int32_t)k, (int32_t)b.rows, Batch::in(b.lens), Batch::in(b.pool), base, Batch::in(b.ring), ring,
+                              Batch::out(b.table), Batch::in(b.shared), shared, moves, moves + m, done, ids, work, stream);
+  if (st != WF_OK) return PyLong_FromLong(st);
+  return wrapped(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// cache, moves, layers -> True
+PyObject* copy(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Args a(args, n, 5);
+  if (!a.ok) return none();
+  void* stream = a.address();
+  const at::Tensor *cache = a.dense(at::kByte), *moves = a.dense(at::kInt);
+  const int64_t layers = a.integer(0, WF_KV_MAX_LAYERS);
+  if (!a.ok || moves->dim() != 2 || moves->size(0) != 2 || moves->size(1) > WF_KV_MAX_BLOCKS) return none();
+  a.holds(cache, (layers > 1 ? layers : 1) * a.g->cache_bytes);
+  if (!a.ok) return none();
+  const int64_t m = moves->size(1);
+  const wf_status st = queued(g_copy, a.g->ctx, (uint8_t*)data(cache), a.g->cache_bytes, (int32_t)layers, Batch::in(moves), Batch::in(moves) + m,
+                              (int32_t)m, stream);
+  if (st != WF_OK) return PyLong_FromLong(st);
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
 void drop(PyObject* capsule) { delete static_cast<Geometry*>(PyCapsule_GetPointer(capsule, kName)); }
 
 // geometry(ctx, device, q_heads, kv_heads, head_dim, n_blocks, max_blocks, cache_bytes, f16): what the
@@ -268,14 +388,18 @@ PyObject* geometry(PyObject*, PyObject* args) {
   return c;
 }
 
-// calls(step, store, load, attend): their addresses in the loaded library.
+// calls(step, store, load, attend, fork, release, compact, copy): their addresses in the loaded library.
 PyObject* calls(PyObject*, PyObject* args) {
-  unsigned long long s, t, l, a;
-  if (!PyArg_ParseTuple(args, "KKKK", &s, &t, &l, &a)) return nullptr;
-  g_step = reinterpret_cast<decltype(g_step)>((uintptr_t)s);
-  g_store = reinterpret_cast<decltype(g_store)>((uintptr_t)t);
-  g_load = reinterpret_cast<decltype(g_load)>((uintptr_t)l);
-  g_attend = reinterpret_cast<decltype(g_attend)>((uintptr_t)a);
+  unsigned long long p[8];
+  if (!PyArg_ParseTuple(args, "KKKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7])) return nullptr;
+  g_step = reinterpret_cast<decltype(g_step)>((uintptr_t)p[0]);
+  g_store = reinterpret_cast<decltype(g_store)>((uintptr_t)p[1]);
+  g_load = reinterpret_cast<decltype(g_load)>((uintptr_t)p[2]);
+  g_attend = reinterpret_cast<decltype(g_attend)>((uintptr_t)p[3]);
+  g_fork = reinterpret_cast<decltype(g_fork)>((uintptr_t)p[4]);
+  g_release = reinterpret_cast<decltype(g_release)>((uintptr_t)p[5]);
+  g_compact = reinterpret_cast<decltype(g_compact)>((uintptr_t)p[6]);
+  g_copy = reinterpret_cast<decltype(g_copy)>((uintptr_t)p[7]);
   Py_RETURN_NONE;
 }
 
@@ -288,6 +412,10 @@ PyMethodDef g_methods[] = {{"step", fast(step), METH_FASTCALL, nullptr},
                            {"store", fast(store), METH_FASTCALL, nullptr},
                            {"load", fast(load), METH_FASTCALL, nullptr},
                            {"attend", fast(attend), METH_FASTCALL, nullptr},
+                           {"fork", fast(fork), METH_FASTCALL, nullptr},
+                           {"release", fast(release), METH_FASTCALL, nullptr},
+                           {"compact", fast(compact), METH_FASTCALL, nullptr},
+                           {"copy", fast(copy), METH_FASTCALL, nullptr},
                            {"geometry", geometry, METH_VARARGS, nullptr},
                            {"calls", calls, METH_VARARGS, nullptr},
                            {nullptr, nullptr, 0, nullptr}};

@@ -256,7 +256,8 @@ def _bind():
         return None
     lib = load()
     _kvbind.calls(*(ctypes.cast(f, ctypes.c_void_p).value
-                    for f in (lib.wf_kv_step, lib.wf_kv_store, lib.wf_kv_load, lib.wf_kv_attend)))
+                    for f in (lib.wf_kv_step, lib.wf_kv_store, lib.wf_kv_load, lib.wf_kv_attend, lib.wf_kv_fork,
+                              lib.wf_kv_release, lib.wf_kv_compact, lib.wf_kv_copy)))
     return _kvbind
 
 
@@ -380,6 +381,12 @@ def kv_fork(ctx: KVContext, src, dst, tokens, lens, pool, ring, table, shared, s
     if stream is not None:
         with _made_current(ctx, stream):
             return kv_fork(ctx, src, dst, tokens, lens, pool, ring, table, shared)
+    if ctx._bind is not None:
+        out = ctx._bind.fork(ctx._geometry, ctx._current(ctx.device), src, dst, tokens, lens, pool, ring, table, shared)
+        if out is not None:
+            if out.__class__ is int:
+                ctx._check(out)
+            return out
     import torch
     n, r, b = src.shape[0], lens.shape[0], ctx.n_blocks
     if not n == dst.shape[0] == tokens.shape[0]:
@@ -399,6 +406,12 @@ def kv_release(ctx: KVContext, release, lens, pool, ring, table, shared, stream=
     if stream is not None:
         with _made_current(ctx, stream):
             return kv_release(ctx, release, lens, pool, ring, table, shared)
+    if ctx._bind is not None:
+        out = ctx._bind.release(ctx._geometry, ctx._current(ctx.device), release, lens, pool, ring, table, shared)
+        if out is not None:
+            if out.__class__ is int:
+                ctx._check(out)
+            return out
     import torch
     r, b = lens.shape[0], ctx.n_blocks
     flat = lens.new_empty(r + 2 + b + WF_KV_PAGES_WORK, dtype=torch.int32)
@@ -415,6 +428,12 @@ def kv_compact(ctx: KVContext, keep: int, lens, pool, ring, table, shared, strea
     if stream is not None:
         with _made_current(ctx, stream):
             return kv_compact(ctx, keep, lens, pool, ring, table, shared)
+    if ctx._bind is not None:
+        out = ctx._bind.compact(ctx._geometry, ctx._current(ctx.device), keep, lens, pool, ring, table, shared)
+        if out is not None:
+            if out.__class__ is int:
+                ctx._check(out)
+            return out
     import torch
     r, b, k = lens.shape[0], ctx.n_blocks, max(int(keep), 0)
     m = max(min(k, b - k), 0)
@@ -431,6 +450,12 @@ def kv_copy(ctx: KVContext, cache, moves, layers: int = 1, stream=None) -> None:
     if stream is not None:
         with _made_current(ctx, stream):
             return kv_copy(ctx, cache, moves, layers)
+    if ctx._bind is not None:
+        out = ctx._bind.copy(ctx._geometry, ctx._current(ctx.device), cache, moves, layers)
+        if out is not None:
+            if out.__class__ is int:
+                ctx._check(out)
+            return None
     if moves.ndim != 2 or moves.shape[0] != 2:
         raise ValueError(f"moves: shape {tuple(moves.shape)}, [2, n] needed")
     n = moves.shape[1]
