@@ -29,9 +29,18 @@ __device__ __forceinline__ uint32_t seen_bytes(int at, int lo, int hi) {
   return from == 4 ? 0u : below & (~0u << 8 * from);
 }
 
+// As Pages, for tokens that are the same for a whole wave.
+struct UniformPages : Pages {
+  using Pages::Pages;
+  __device__ __forceinline__ unsigned id(int token) const {
+    const auto* at = (const __attribute__((address_space(4))) int32_t*)table;
+    return (unsigned)at[(unsigned)min(token, last) >> b_log2];
+  }
+};
+
 // Waves a SIMD that the registers are held to.
 template <int D, int C>
-constexpr int kOcc = D * C <= 64 ? 4 : D * C <= 128 ? 3 : D * C <= 256 ? 2 : 1;
+constexpr int kOcc = C == 1 ? (D == 64 ? 3 : D == 128 ? 2 : 1) : D == 64 ? 3 : D == 128 ? 2 : 1;
 
 // Up to this many shares of 16 columns are joined by the workgroup that is done last, more (or of
 // more columns) by a kernel of their own, with a workgroup for each head.
@@ -49,7 +58,7 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
   __shared__ float ref_of[kWaves][16 * C], sum_of[kWaves][16 * C];
   __shared__ int last;
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, grp = lane >> 4;
   // kv heads fastest (blocks of one head meet in one die's L2 where heads
   // divide the dies), then shares, then column tiles from the last (the longest under a
@@ -65,7 +74,7 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
   const int q0 = min(max(a.q_off[row], 0), a.n_tokens), q1 = min(max(a.q_off[row + 1], q0), a.n_tokens);
   const int64_t columns = (int64_t)(q1 - q0) * g.group;
   const int len = min(max(a.kv_len[row], 0), g.width << g.b_log2);
-  const Pages pages(g, a, row, kvh, len);
+  const UniformPages rows(g, a, row, kvh, len);
   const float scale = a.scale * kLog2e;
 
   for (int64_t tile = tile0; tile * 16 * C < columns; tile += sp.tiles) {
@@ -73,34 +82,54 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
     u32x4 q[C][KS];
     int lo[C], hi[C];
     int lo_min = len, lo_max = 0, hi_min = INT32_MAX, hi_max = 0;
+    auto note = [&](const Sight& see) __attribute__((always_inline)) {
+      // (what is seen at all: queries that see nothing do not count)
+      lo_min = min(lo_min, see.lo < see.hi ? see.lo : len);
+      lo_max = max(lo_max, see.lo);
+      hi_min = min(hi_min, see.hi);
+      hi_max = max(hi_max, see.lo < see.hi ? see.hi : 0);
+    };
+    // (columns past the last repeat it and are not written)
+    const unsigned col0 = (unsigned)(tile * 16 * C), col1 = (unsigned)min(tile * 16 * C + 16 * C, columns) - 1u;
+    const unsigned i0 = col0 / (unsigned)g.group, i1 = col1 / (unsigned)g.group;
+    unsigned own[C];  // the tokens of this lane's columns
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      // columns past the last repeat it and are not written
-      const unsigned col = (unsigned)min(tile * 16 * C + c * 16 + n, columns - 1);
-      const unsigned i = col / (unsigned)g.group, h = col - i * (unsigned)g.group;
-      const u32x4* src = reinterpret_cast<const u32x4*>((const uint16_t*)a.q + (int64_t)(q0 + i) * a.q_stride +
+      const unsigned col = min(col0 + c * 16 + n, col1);
+      own[c] = col / (unsigned)g.group;
+      const unsigned h = col - own[c] * (unsigned)g.group;
+      const u32x4* src = reinterpret_cast<const u32x4*>((const uint16_t*)a.q + (int64_t)(q0 + own[c]) * a.q_stride +
                                                         (int64_t)(kvh * g.group + h) * D + grp * 16);
 #pragma unroll
       for (int k = 0; k < KS; ++k) q[c][k] = src[k / 2 * 8 + k % 2];
-      const Sight see = sight_of(a.pos[q0 + i], len, a.window);
-      lo[c] = see.lo, hi[c] = see.hi;
-      // (what is seen at all: queries that see nothing do not count)
-      lo_min = min(lo_min, lo[c] < hi[c] ? lo[c] : len);
-      lo_max = max(lo_max, lo[c]);
-      hi_min = min(hi_min, hi[c]);
-      hi_max = max(hi_max, lo[c] < hi[c] ? hi[c] : 0);
     }
+    // Up to two tokens (all columns of single tokens are one): positions by scalar loads, as the blocks below.
+    if (i1 - i0 <= 1) {
+      const auto* pos = (const __attribute__((address_space(4))) int32_t*)a.pos + q0;
+      const Sight see0 = sight_of(pos[i0], len, a.window), see1 = sight_of(pos[i1], len, a.window);
+      note(see0);
+      note(see1);
 #pragma unroll
-    for (int off = 1; off < 16; off <<= 1) {
-      lo_min = min(lo_min, __shfl_xor(lo_min, off, 64));
-      lo_max = max(lo_max, __shfl_xor(lo_max, off, 64));
-      hi_min = min(hi_min, __shfl_xor(hi_min, off, 64));
-      hi_max = max(hi_max, __shfl_xor(hi_max, off, 64));
+      for (int c = 0; c < C; ++c) lo[c] = own[c] == i0 ? see0.lo : see1.lo, hi[c] = own[c] == i0 ? see0.hi : see1.hi;
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const Sight see = sight_of(a.pos[q0 + own[c]], len, a.window);
+        lo[c] = see.lo, hi[c] = see.hi;
+        note(see);
+      }
+#pragma unroll
+      for (int off = 1; off < 16; off <<= 1) {
+        lo_min = min(lo_min, __shfl_xor(lo_min, off, 64));
+        lo_max = max(lo_max, __shfl_xor(lo_max, off, 64));
+        hi_min = min(hi_min, __shfl_xor(hi_min, off, 64));
+        hi_max = max(hi_max, __shfl_xor(hi_max, off, 64));
+      }
+      lo_min = __builtin_amdgcn_readfirstlane(lo_min);
+      lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+      hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+      hi_max = __builtin_amdgcn_readfirstlane(hi_max);
     }
-    lo_min = __builtin_amdgcn_readfirstlane(lo_min);
-    lo_max = __builtin_amdgcn_readfirstlane(lo_max);
-    hi_min = __builtin_amdgcn_readfirstlane(hi_min);
-    hi_max = __builtin_amdgcn_readfirstlane(hi_max);
     // units of 64 tokens that any column sees, in equal shares of at least a unit a wave
     const int first = lo_min >> 6, units = max(0, ((hi_max + 63) >> 6) - first);
     // (a tile past those the launch knew of is not shared: its count would be another's)
@@ -117,38 +146,48 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
     for (int c = 0; c < C; ++c) ref[c] = -FLT_MAX, sum[c] = 0.0f;
 
     const int kgrp = n >> 2;  // the group whose keys this lane loads: row n of a score tile
-    // keys of a unit: token t*4 + n%4 of group n/4, 16 channels of each run of 64
-    u32x4 kw[4][J];
-    auto load_keys = [&](int u, unsigned id) __attribute__((always_inline)) {
-      const int off = ((u << 6) + kgrp * 16) & (g.b - 1);
-      const uint8_t* at = pages.cell(id) + (off + (n & 3)) * D + grp * 16;
+    // A unit as it is loaded.  Keys: token t*4 + n%4 of group n/4, 16 channels of each run of 64; values: of four
+    // tokens, four channels of each run of 64; the scales of the values' block.
+    struct Unit {
+      u32x4 kw[4][J], vw[J][4];
+      f32x2 scales;
+    };
+    // (units past this share's last are that one again: their bytes are on their way anyway)
+    const int u0 = first + split * share + wave, stop = max(end - 1, 0);
+    // The blocks of a unit's four groups come by scalar loads: vector loads return in order, a wave's and to
+    // a degree a CU's, so an id would arrive behind all the codes that were asked for before it.
+    unsigned ids[4];
+    auto ask = [&](int u) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) ids[x] = rows.id((min(u, stop) << 6) + x * 16);
+    };
+    auto id_of = [&](int x) __attribute__((always_inline)) {
+      const unsigned lo = x & 1 ? ids[1] : ids[0], hi = x & 1 ? ids[3] : ids[2];
+      return x & 2 ? hi : lo;
+    };
+    auto load_keys = [&](int u, Unit& w) __attribute__((always_inline)) {
+      const int off = ((min(u, stop) << 6) + kgrp * 16) & (g.b - 1);
+      const uint8_t* at = rows.cell(id_of(kgrp)) + (off + (n & 3)) * D + grp * 16;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int j = 0; j < J; ++j) kw[t][j] = *reinterpret_cast<const u32x4*>(at + t * 4 * D + j * 64);
+        for (int j = 0; j < J; ++j) w.kw[t][j] = *reinterpret_cast<const u32x4*>(at + t * 4 * D + j * 64);
     };
-
-    // a unit's keys are loaded while the one before is worked on, its blocks one earlier still
-    const int u0 = first + split * share + wave;
-    unsigned kid = pages.id((u0 << 6) + kgrp * 16), vid = pages.id((u0 << 6) + grp * 16);
-    load_keys(u0, kid);
-    kid = pages.id(((u0 + kWaves) << 6) + kgrp * 16);
-    for (int u = u0; u < end; u += kWaves) {
-      const int base = u << 6;
-      const uint8_t* vcell = pages.cell(vid);
-      const int voff = (base + grp * 16) & (g.b - 1);
-      vid = pages.id(base + (kWaves << 6) + grp * 16);
-      const f32x2 scales = *reinterpret_cast<const f32x2*>(vcell + 2 * g.b * D);
-      const float kz = scales[0] * scale;
-      float vz = scales[1];
-      // values: of four tokens, four channels of each run of 64
-      u32x4 vw[J][4];
+    auto load_values = [&](int u, Unit& w) __attribute__((always_inline)) {
+      const int off = ((min(u, stop) << 6) + grp * 16) & (g.b - 1);
+      const uint8_t* cell = rows.cell(id_of(grp));
+      w.scales = *reinterpret_cast<const f32x2*>(cell + 2 * g.b * D);
 #pragma unroll
       for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-          vw[j][t] = *reinterpret_cast<const u32x4*>(vcell + g.b * D + (voff + 4 * t) * D + (j * 64 + n * 4) * 4);
-
+          w.vw[j][t] = *reinterpret_cast<const u32x4*>(cell + g.b * D + (off + 4 * t) * D + (j * 64 + n * 4) * 4);
+    };
+    // `more` is called once the keys are multiplied
+    auto work = [&](int u, Unit& w, auto more) __attribute__((always_inline)) {
+      const int base = u << 6;
+      const float kz = w.scales[0] * scale;
+      float vz = w.scales[1];
       const bool whole = base >= lo_max && base + 64 <= hi_min;
       // what no query sees may be anything, no number too, which a probability of 0 would not hide
       if (base < lo_min || base + 64 > hi_max) {
@@ -158,11 +197,11 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
         for (int t = 0; t < 4; ++t) {
           const uint32_t mask = seen_bytes(j0 + t * 4, lo_min, hi_max);
 #pragma unroll
-          for (int j = 0; j < J; ++j) vw[j][t] &= mask;
+          for (int j = 0; j < J; ++j) w.vw[j][t] &= mask;
         }
       }
-      float vlog = 0.0f;
-      if constexpr (M::kScaled) vlog = scale_log(vz) - M::kAim;
+      float vlog = 0.0f, limit = M::kSlack;
+      if constexpr (M::kScaled) vlog = scale_log(vz), limit = fminf(limit, M::kMostLog - vlog);
       // 32 tokens at a time: score tiles 2h and 2h + 1, one product with the values
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -173,15 +212,12 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
           for (int c = 0; c < C; ++c) s[c][e] = (f32x4){0, 0, 0, 0};
 #pragma unroll
           for (int k = 0; k < KS; ++k) {
-            const u32x4 kk = operand8<M>(kw[2 * h + e][k / 2][k % 2 * 2], kw[2 * h + e][k / 2][k % 2 * 2 + 1], 1.0f);
+            const u32x4 kk = operand8<M>(w.kw[2 * h + e][k / 2][k % 2 * 2], w.kw[2 * h + e][k / 2][k % 2 * 2 + 1], 1.0f);
 #pragma unroll
             for (int c = 0; c < C; ++c) s[c][e] = M::mma(kk, q[c][k], s[c][e]);
           }
         }
-        if (h) {
-          load_keys(u + kWaves, kid);
-          kid = pages.id(base + (2 * kWaves << 6) + kgrp * 16);
-        }
+        if (h) more();
         const int j0 = base + grp * 16 + h * 8;
         float most[C];
         bool up = false;
@@ -197,18 +233,15 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
 #pragma unroll
           for (int i = 1; i < 8; ++i) m = fmaxf(m, s[c][i / 4][i % 4]);
           most[c] = m;
-          up |= m > ref[c] + M::kSlack;
+          up |= m > ref[c] + limit;
         }
-        // the reference moves only when a score passes it by the slack
+        // the reference moves only when a score (kScaled: or its term) passes it by the limit
         if (__builtin_expect(__any(up), 0)) {
 #pragma unroll
           for (int c = 0; c < C; ++c) {
             float r = most[c];
-            if constexpr (M::kScaled) {
-              r -= 40.0f;  // (values of next to nothing at the largest score: p stays far from fp32's end)
-#pragma unroll
-              for (int i = 0; i < 8; ++i) r = fmaxf(r, s[c][i / 4][i % 4] + vlog);
-            }
+            // (values of next to nothing at the largest score: p stays far from fp32's end)
+            if constexpr (M::kScaled) r = fmaxf(r - 40.0f, r + vlog - M::kAim);
             r = fmaxf(ref[c], column_max(r));
             const float keep = __builtin_amdgcn_exp2f(ref[c] - r);
             ref[c] = r;
@@ -228,31 +261,45 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
             sum[c] += e;
             x[i] = M::kScaled ? e * vz : e;
           }
-          if constexpr (M::kScaled) {  // ... or when a term passes what its type holds
-            float m = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
-            if (__builtin_expect(__any(m > M::kMostTerm), 0)) {
-              m = column_max(m);
-              const float up = m > M::kMostTerm && m < INFINITY ? __builtin_amdgcn_logf(m) - M::kAim : 0.0f;
-              const float keep = __builtin_amdgcn_exp2f(-up);
-              ref[c] += up;
-              sum[c] *= keep;
-#pragma unroll
-              for (int k = 0; k < MT; ++k) o[c][k] *= keep;
-#pragma unroll
-              for (int i = 0; i < 8; ++i) x[i] *= keep;
-            }
-          }
 #pragma unroll
           for (int b = 0; b < 4; ++b) p[c][b] = M::pair(x[2 * b], x[2 * b + 1]);
         }
 #pragma unroll
         for (int r = 0; r < MT; ++r) {
-          const u32x4 vv = operand8<M>(vw[r / 4][2 * h][r % 4], vw[r / 4][2 * h + 1][r % 4], M::kScaled ? 1.0f : vz);
+          const u32x4 vv = operand8<M>(w.vw[r / 4][2 * h][r % 4], w.vw[r / 4][2 * h + 1][r % 4], M::kScaled ? 1.0f : vz);
 #pragma unroll
           for (int c = 0; c < C; ++c) o[c][r] = M::mma(vv, p[c], o[c][r]);
         }
+      }
+    };
+    int u = u0;
+    ask(u);
+    if constexpr (C == 1) {
+      // the next unit is on its way while one is worked on, its blocks one earlier still
+      Unit w0, w1;
+      const auto none = [] {};
+      load_keys(u, w0);
+      load_values(u, w0);
+      ask(u + kWaves);
+      for (; u + kWaves < end; u += 2 * kWaves) {
+        load_keys(u + kWaves, w1);
+        load_values(u + kWaves, w1);
+        ask(u + 2 * kWaves);
+        work(u, w0, none);
+        load_keys(u + 2 * kWaves, w0);
+        load_values(u + 2 * kWaves, w0);
+        ask(u + 3 * kWaves);
+        work(u + kWaves, w1, none);
+      }
+      if (u < end) work(u, w0, none);
+    } else {
+      // (two units' registers would leave one wave a SIMD) the next keys alone
+      Unit w;
+      load_keys(u, w);
+      for (; u < end; u += kWaves) {
+        load_values(u, w);
+        ask(u + kWaves);
+        work(u, w, [&]() __attribute__((always_inline)) { load_keys(u + kWaves, w); });
       }
     }
 
@@ -810,9 +857,21 @@ template <int D, class M>
 hipError_t by_columns(const Geo& g, const AttendArgs& a, const AttendWork& w, hipStream_t s) {
   const int64_t columns = (int64_t)(a.max_q > 0 ? std::min(a.max_q, a.n_tokens) : a.n_tokens) * g.group;
   if (columns <= 16) return narrow<D, 1, M>(g, a, w, columns, s);
-  const int64_t at_once = w.n_cu * kOcc<D, 2>, narrow_wgs = (int64_t)a.n_rows * g.hk * ((columns + 31) / 32);
-  const bool few = a.max_kv > 0 && narrow_wgs <= at_once && narrow_wgs * a.max_kv <= at_once * 3500;
-  if (columns <= 128 || few) return narrow<D, 2, M>(g, a, w, columns, s);
+  if (columns <= 128) return narrow<D, 2, M>(g, a, w, columns, s);
+  // Narrow workgroups convert the codes for 32 columns, wide ones for 128 or 256, but take 10 us and more to fill
+  // their pipeline, and ragged rows leave CUs without one.  (The tokens of the call tell how many columns there are in all.)
+  // At 64 channels, where the softmax costs more than the products, wide ones win only where there are several for
+  // each CU: a prompt of 7,001 of 32 heads 280 us narrow against 256 wide, of 12 heads 110 against 132, of 2,000 of 32 heads
+  // 37 against 45; 7 and 30 chunks of up to 500 over 8,000 of 14 heads (f16) 56 against 62, 171 against 226.
+  // At 128 channels, narrow against wide: a prompt of 1,000 of 32 heads 29 and 38, of 2,000 70 and 65, of 4,000 199 and 136; 128
+  // tokens over 4,000 29 and 37, 256 over 4,000 43 and 42, over 16,000 102 and 84; 16 prompts of 400 119 and 74.
+  const int64_t all = (int64_t)a.n_tokens * g.hq;
+  if constexpr (D == 64) {
+    if (all < 256 * 3 * w.n_cu) return narrow<D, 2, M>(g, a, w, columns, s);
+  } else {
+    const int64_t at_once = w.n_cu * kOcc<D, 2>, wgs = (all + 31) / 32;
+    if (a.max_kv > 0 && wgs * 2 <= at_once * 5 && wgs * a.max_kv <= at_once * 3500) return narrow<D, 2, M>(g, a, w, columns, s);
+  }
   return wide<D, M>(g, a, w, columns, s);
 }
 
