@@ -13,25 +13,26 @@
 namespace wfkv {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kMostTile = 64, kMostBlock = 256, kSpan = kMostTile + kMostBlock;
+constexpr int kThreads = 256, kManyThreads = 512, kPasses = 2, kManyWaves = 4;  // of a workgroup; where there are many tokens
+// tokens of a tile, and that a workgroup looks at: up to a block's before the tile and behind it
+constexpr int kMostTile = 256, kMostBlock = 256, kSpan = kMostTile + 2 * kMostBlock;
 constexpr int kHeads = 4;                // query heads a lane group takes of a token, of many
 constexpr int64_t kManyVectors = 32768;  // query vectors of a call from which they are many
 
-// A launch's part of the work: queries of tokens [token, token + tokens), `groups` lane groups a token, by the first
-// `vector_blocks` workgroups; `items` tiles of `tile` tokens of a kv head by the others.
+// A launch's part of the work: `items` tiles of `tile` tokens of a kv head by the first `item_blocks` workgroups;
+// queries of tokens [token, token + tokens), `groups` lane groups a token, by the others.
 struct Share {
   int token, tokens;
-  unsigned groups, vector_blocks, items;
+  unsigned groups, item_blocks, items;
   int tile;
 };
 
 // A query's heads h0, h0 + groups, ...
-template <int D, class T, int N>
+template <int D, class T, int N, int W>
 __device__ __forceinline__ void queries(const Geo& g, const StoreArgs& a, const Share& part) {
   constexpr int L = D / 8;
   const int lane = threadIdx.x % L;
-  const unsigned v = blockIdx.x * (kThreads / L) + threadIdx.x / L;
+  const unsigned v = (blockIdx.x - part.item_blocks) * (W / L) + threadIdx.x / L;
   const unsigned groups = part.groups, i = v / groups, h0 = v - i * groups;
   if (i >= (unsigned)part.tokens) return;  // whole vectors leave
   const int t = part.token + (int)i;
@@ -57,17 +58,25 @@ __device__ __forceinline__ void queries(const Geo& g, const StoreArgs& a, const 
   }
 }
 
-// A token's key of a head, normed and rotated.
+// A key at a position, normed and rotated.
 template <int D, class T>
-__device__ __forceinline__ void key_of(const StoreArgs& a, int t, int kvh, int lane, const uint4& weight, float* x) {
+__device__ __forceinline__ void key_of(const StoreArgs& a, int pos, const uint4& raw, int lane, const uint4& weight, float* x) {
   constexpr int L = D / 8;
-  unpack<T>(reinterpret_cast<const uint4*>((const uint16_t*)a.k + t * a.k_stride + (int64_t)kvh * D)[lane], x);
-  if (a.how.k_weight) norm<L, T>(x, weight, a.how.eps);
   const int rot = a.how.rot_dim;
-  if (rot) {
-    const Turn turn = turn_of(a.how.cos_sin + (int64_t)min(max(a.pos[t], 0), a.how.n_pos - 1) * rot, rot, a.how.interleaved, lane);
-    rotate<L>(x, turn, rot, a.how.interleaved, lane);
-  }
+  Turn turn = {};
+  if (rot) turn = turn_of(a.how.cos_sin + (int64_t)min(max(pos, 0), a.how.n_pos - 1) * rot, rot, a.how.interleaved, lane);
+  unpack<T>(raw, x);
+  if (a.how.k_weight) norm<L, T>(x, weight, a.how.eps);
+  if (rot) rotate<L>(x, turn, rot, a.how.interleaved, lane);
+}
+
+// The bits of the largest magnitude of eight 16-bit values, as fp32's.
+template <int L, class T>
+__device__ __forceinline__ uint32_t largest(const uint4& raw) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  auto two = [](uint32_t w) { return __builtin_bit_cast(u16x2, w & 0x7fff7fffu); };
+  const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(two(raw.x), two(raw.y)), __builtin_elementwise_max(two(raw.z), two(raw.w)));
+  return __float_as_uint(T::to(vector_max<L>((uint32_t)max(m[0], m[1]))));
 }
 
 template <int L>
@@ -81,33 +90,65 @@ __device__ __forceinline__ uint32_t largest(const float* x) {
 // What a workgroup knows of the tokens of its span.
 struct Span {
   int64_t slot[kSpan];
+  int64_t cell[kSpan];        // its cell in the cache, and its place in it (-1: not this workgroup's)
+  int16_t off[kSpan];
+  uint8_t four[kSpan];        // whether it and the next three are the tokens of a word of values
   int lead[kSpan];            // first token of the token's run, -1: not this workgroup's
   uint32_t most[2][kSpan];    // of a run (at its first token): largest magnitudes of keys and values,
-  int power[2][kSpan];        // then the powers of their scales;
-  int begins[kSpan];          // whether it holds its block's first token
-  uint32_t bad[kSpan];        // of a token: something in it is not finite
-  int up[kSpan][3], ups;      // runs whose block is rounded anew: first token, powers to add
+  int8_t power[2][kSpan];     // then the powers of their scales;
+  uint8_t begins[kSpan];      // whether it holds its block's first token
+  uint8_t bad[kSpan];         // of a token: something in it is not finite
+  int16_t up[kSpan][3];       // runs whose block is rounded anew: first token, powers to add
+  int ups;
   int last_event[kSpan / 64];
   int first, end;             // this workgroup's tokens
 };
 
-template <int D, class T>
-__device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, unsigned item, int tile, Span& sp) {
-  constexpr int L = D / 8, V = kThreads / L;
-  const int kvh = (int)(item % (unsigned)g.hk), t0 = (int)(item / (unsigned)g.hk) * tile;
-  const int span = min(tile + g.b, a.n_tokens - t0);
-  const int lane = threadIdx.x % L, group = threadIdx.x / L;
+template <int D, class T, int P, int W>
+__device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, unsigned item, int tile, Span& sp, uint8_t (&codes_of_pass)[P][8 * W]) {
+  constexpr int L = D / 8, V = W / L, E = (kSpan + W - 1) / W;
+  const int kvh = (int)(item % (unsigned)g.hk), lane = threadIdx.x % L, group = threadIdx.x / L;
   if (threadIdx.x == 0) sp.ups = 0, sp.first = kSpan, sp.end = 0;
-  // events: tokens that begin a run, or are not stored
   const int64_t none = -1;
-  auto slot_at = [&](int i) {
-    const int64_t s = a.slot[t0 + i];
-    return s >= 0 && s >> g.b_log2 < g.n_blocks ? s : none;
+  auto valid = [&](int64_t s) { return s >= 0 && s >> g.b_log2 < g.n_blocks ? s : none; };
+  // A tile begins where the block of its first token begins, if that is in this call: runs of whole blocks
+  // are whole in a tile then, and its passes of V tokens are theirs.
+  auto aligned = [&](int x) {
+    if (x <= 0 || x >= a.n_tokens) return min(max(x, 0), a.n_tokens);
+    const auto* slot = (const __attribute__((address_space(4))) int64_t*)a.slot;
+    const int64_t s = slot[x];
+    const int k = (int)(s & (g.b - 1));
+    return k <= x && slot[x - k] == s - k ? x - k : x;
   };
-  uint64_t events[2], owned[2];
+  const int x0 = (int)(item / (unsigned)g.hk) * tile, t0 = aligned(x0), own = max(aligned(x0 + tile) - t0, 0);
+  const int span = min(own + g.b, a.n_tokens - t0);
+  const uint4 weight = a.how.k_weight ? reinterpret_cast<const uint4*>(a.how.k_weight)[lane] : make_uint4(0, 0, 0, 0);
+  auto slot_at = [&](int i) { return valid(a.slot[t0 + i]); };
+  // (all lane groups take part in every pass, on some token of the span)
+  auto at = [&](int p) __attribute__((always_inline)) { return min(p * V + group, span - 1); };
+  auto load = [&](int p, uint4& x, uint4& y, int& pos) __attribute__((always_inline)) {
+    const int t = t0 + at(p);
+    x = reinterpret_cast<const uint4*>((const uint16_t*)a.k + t * a.k_stride + (int64_t)kvh * D)[lane];
+    y = reinterpret_cast<const uint4*>((const uint16_t*)a.v + t * a.v_stride + (int64_t)kvh * D)[lane];
+    pos = a.how.rot_dim ? a.pos[t] : 0;
+  };
+  // The first P stay in registers, and are done before it is known which tokens are this workgroup's: every load that
+  // waits for another's result waits behind all that the CU has asked for.
+  float keys[P][8];
+  uint4 values[P];
+  {
+    uint4 raw[P];
+    int pos[P];
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const int i = p * kThreads + (int)threadIdx.x;
+    for (int p = 0; p < P; ++p) load(p, raw[p], values[p], pos[p]);
+#pragma unroll
+    for (int p = 0; p < P; ++p) key_of<D, T>(a, pos[p], raw[p], lane, weight, keys[p]);
+  }
+  // events: tokens that begin a run, or are not stored
+  uint64_t events[E], owned[E];
+#pragma unroll
+  for (int p = 0; p < E; ++p) {
+    const int i = p * W + (int)threadIdx.x;
     events[p] = owned[p] = 0;
     if (i - (int)(threadIdx.x & 63) >= kSpan) continue;
     bool event = true, mine = false;
@@ -115,7 +156,7 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
       const int64_t s = slot_at(i), before = t0 + i > 0 ? slot_at(i - 1) : none;
       sp.slot[i] = s;
       event = s < 0 || before < 0 || before >> g.b_log2 != s >> g.b_log2;
-      mine = event && s >= 0 && i < tile;
+      mine = event && s >= 0 && i < own;
       sp.most[0][i] = sp.most[1][i] = sp.bad[i] = 0;
       sp.begins[i] = 0;
     }
@@ -128,8 +169,8 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
   }
   __syncthreads();
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const int i = p * kThreads + (int)threadIdx.x;
+  for (int p = 0; p < E; ++p) {
+    const int i = p * W + (int)threadIdx.x;
     if (i >= span) continue;
     const uint64_t upto = events[p] & (~0ull >> (63 - (threadIdx.x & 63)));
     int lead = -1;
@@ -142,36 +183,53 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
       lead = w >= 0 ? sp.last_event[w] : -1;
     }
     sp.lead[i] = lead;
-    if (lead >= 0) {
-      atomicMin(&sp.first, i);
-      atomicMax(&sp.end, i + 1);
-      if ((sp.slot[i] & (g.b - 1)) == 0) sp.begins[lead] = 1;
+    if (lead >= 0 && (sp.slot[i] & (g.b - 1)) == 0) sp.begins[lead] = 1;
+    const uint64_t mine = __ballot(lead >= 0);
+    if (mine && (threadIdx.x & 63) == 0) {  // (lane 0 of a wave that has tokens of the span is in it)
+      atomicMin(&sp.first, i + __ffsll((unsigned long long)mine) - 1);
+      atomicMax(&sp.end, i + 64 - __clzll((long long)mine));
     }
   }
   __syncthreads();
   const int first = sp.first, end = sp.end;
-  const uint4 weight = a.how.k_weight ? reinterpret_cast<const uint4*>(a.how.k_weight)[lane] : make_uint4(0, 0, 0, 0);
-  // (all lane groups take part in every pass, on the span's last token if on no other)
-  for (int j = first; j < end; j += V) {
-    const int i = min(j + group, end - 1);
-    float x[8], y[8];
-    key_of<D, T>(a, t0 + i, kvh, lane, weight, x);
-    unpack<T>(reinterpret_cast<const uint4*>((const uint16_t*)a.v + (t0 + i) * a.v_stride + (int64_t)kvh * D)[lane], y);
-    const uint32_t k = largest<L>(x), v = largest<L>(y);
-    const int lead = sp.lead[i];
-    if (lane || lead < 0) continue;
+  if (first >= end) return;
+  const int passes = (end + V - 1) / V, begin = first / V;
+  auto measure = [&](int p, const float* x, const uint4& y) __attribute__((always_inline)) {
+    const uint32_t k = largest<L>(x), z = largest<L, T>(y);
+    const int i = at(p), lead = sp.lead[i];
+    if (lane || lead < 0) return;
     // infinities and NaN have the largest bit patterns
-    if (max(k, v) >= 0x7f800000u) {
+    if (max(k, z) >= 0x7f800000u) {
       sp.bad[i] = 1;
     } else {
       atomicMax(&sp.most[0][lead], k);
-      atomicMax(&sp.most[1][lead], v);
+      atomicMax(&sp.most[1][lead], z);
     }
+  };
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    if (p < passes) measure(p, keys[p], values[p]);
+  for (int p = max(P, begin); p < passes; ++p) {
+    float x[8];
+    uint4 raw, y;
+    int pos;
+    load(p, raw, y, pos);
+    key_of<D, T>(a, pos, raw, lane, weight, x);
+    measure(p, x, y);
   }
   __syncthreads();
-  auto cell_of = [&](int i) { return a.cache + ((sp.slot[i] >> g.b_log2) * g.hk + kvh) * (int64_t)g.cell; };
+  // where tokens lie, and whether they and the next three are four of a word, by a thread each
+  for (int i = first + (int)threadIdx.x; i < end; i += W) {
+    const int64_t s = sp.slot[i];
+    const int lead = sp.lead[i];
+    sp.cell[i] = ((s >> g.b_log2) * g.hk + kvh) * (int64_t)g.cell;
+    sp.off[i] = lead < 0 ? -1 : (int)(s & (g.b - 1));
+    sp.four[i] = lead >= 0 && (s & 3) == 0 && i + 3 < end && sp.lead[i + 3] == lead && sp.slot[i + 1] == s + 1 && sp.slot[i + 2] == s + 2 &&
+                 sp.slot[i + 3] == s + 3;
+  }
+  auto cell_of = [&](int i) { return a.cache + sp.cell[i]; };
   const int codes = 2 * g.b * D;  // bytes of them, then the scales
-  for (int i = first + (int)threadIdx.x; i < end; i += kThreads) {
+  for (int i = first + (int)threadIdx.x; i < end; i += W) {
     if (sp.lead[i] != i) continue;
     float* scales = reinterpret_cast<float*>(cell_of(i) + codes);
     int rise[2] = {0, 0};
@@ -183,23 +241,24 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
         e = max(e, old);
         rise[p] = old - e;
       }
-      sp.power[p][i] = e;
+      sp.power[p][i] = (int8_t)e;
       scales[p] = two_to(e);
     }
     if (rise[0] | rise[1]) {
       const int n = atomicAdd(&sp.ups, 1);
-      sp.up[n][0] = i, sp.up[n][1] = rise[0], sp.up[n][2] = rise[1];
+      sp.up[n][0] = (int16_t)i, sp.up[n][1] = (int16_t)rise[0], sp.up[n][2] = (int16_t)rise[1];
     }
   }
   __syncthreads();
   // codes under the old scale: 2^-40 of the largest is no code any more
-  for (int n = 0; n < sp.ups; ++n) {
-    uint4* at = reinterpret_cast<uint4*>(cell_of(sp.up[n][0]));
-    for (int x = threadIdx.x; x < codes / 16; x += kThreads) {
+  const int ups = sp.ups;
+  for (int n = 0; n < ups; ++n) {
+    uint4* cell = reinterpret_cast<uint4*>(cell_of(sp.up[n][0]));
+    for (int x = threadIdx.x; x < codes / 16; x += W) {
       const int rise = sp.up[n][x < codes / 32 ? 1 : 2];
       if (rise == 0) continue;
       const float by = two_to(max(rise, -40));
-      const uint4 w = at[x];
+      const uint4 w = cell[x];
       uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -213,86 +272,150 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
         nan = (nan >> 7) * 0xffu;
         u[i] = (c & ~nan) | (u[i] & nan);
       }
-      at[x] = make_uint4(u[0], u[1], u[2], u[3]);
+      cell[x] = make_uint4(u[0], u[1], u[2], u[3]);
     }
   }
-  if (sp.ups) __syncthreads();  // (the same for all: set before the last barrier)
-  for (int j = first; j < end; j += V) {
-    const int i = min(j + group, end - 1), lead = sp.lead[i];
-    float x[8], y[8];
-    key_of<D, T>(a, t0 + i, kvh, lane, weight, x);
-    unpack<T>(reinterpret_cast<const uint4*>((const uint16_t*)a.v + (t0 + i) * a.v_stride + (int64_t)kvh * D)[lane], y);
-    if (lead < 0 || j + group >= end) continue;
-    const float ks = two_to(-sp.power[0][lead]), vs = two_to(-sp.power[1][lead]);
+  if (ups) __syncthreads();
+  // Codes of a pass: its keys' in registers, its values' in LDS, as a thread stores two channels of four tokens.
+  auto encode = [&](int p, float* x, const uint4& raw, uint8_t* bytes) __attribute__((always_inline)) -> uint2 {
+    const int i = p * V + group, lead = i >= first && i < end ? sp.lead[i] : -1;
+    uint32_t kc[2] = {0, 0}, vc[2] = {0, 0};
+    if (lead >= 0) {
+      const int ke = sp.power[0][lead], ve = sp.power[1][lead];
+      const float ks = two_to(ke), vs = two_to(ve);
+      kc[0] = codes_under(x, ks), kc[1] = codes_under(x + 4, ks);
+      vc[0] = codes_under<T>(raw.x, raw.y, vs), vc[1] = codes_under<T>(raw.z, raw.w, vs);
+      if (__builtin_expect(max(ke, ve) == kMostPower, 0)) {  // values may pass 448 times the largest scale
+        float y[8];
+        unpack<T>(raw, y);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] *= ks, y[k] *= vs;
-    uint32_t kc[2] = {codes_of(x), codes_of(x + 4)}, vc[2] = {codes_of(y), codes_of(y + 4)};
-    if (sp.bad[i]) kc[0] = kc[1] = 0x7f7f7f7fu, vc[0] = vc[1] = 0;
-    uint8_t* cell = cell_of(i);
-    const int off = (int)(sp.slot[i] & (g.b - 1));
-    reinterpret_cast<uint2*>(cell + off * D)[lane] = make_uint2(kc[0], kc[1]);
-    uint8_t* to = cell + g.b * D + ((off >> 2) * D + lane * 8) * 4 + (off & 3);
+        for (int k = 0; k < 8; ++k) x[k] *= two_to(-ke), y[k] *= two_to(-ve);
+        kc[0] = codes_of(x), kc[1] = codes_of(x + 4), vc[0] = codes_of(y), vc[1] = codes_of(y + 4);
+      }
+      if (sp.bad[i]) kc[0] = kc[1] = 0x7f7f7f7fu, vc[0] = vc[1] = 0;
+    }
+    reinterpret_cast<uint2*>(bytes + group * D)[lane] = make_uint2(vc[0], vc[1]);
+    return make_uint2(kc[0], kc[1]);
+  };
+  auto store = [&](int p, const uint2& kc, const uint8_t* bytes) __attribute__((always_inline)) {
+    const int i = p * V + group;
+    const int off = i >= first && i < end ? sp.off[i] : -1;
+    if (off >= 0) reinterpret_cast<uint2*>(cell_of(i) + off * D)[lane] = kc;
+    const int q = (int)threadIdx.x / (D / 2), ch = (int)threadIdx.x % (D / 2) * 2, i0 = p * V + q * 4;
+    uint32_t two[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) to[4 * k] = (uint8_t)(vc[k / 4] >> (8 * (k % 4)));
+    for (int t = 0; t < 4; ++t) two[t] = *reinterpret_cast<const uint16_t*>(bytes + (q * 4 + t) * D + ch);
+    if (i0 >= first && i0 < end && sp.four[i0]) {
+      const uint32_t lo = (two[0] & 0xff) | (two[1] & 0xff) << 8 | (two[2] & 0xff) << 16 | two[3] << 24;
+      const uint32_t hi = two[0] >> 8 | (two[1] & 0xff00) | (two[2] & 0xff00) << 8 | (two[3] & 0xff00) << 16;
+      *reinterpret_cast<uint2*>(cell_of(i0) + g.b * D + sp.off[i0] * D + ch * 4) = make_uint2(lo, hi);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int k = i0 + t, off = k >= first && k < end ? sp.off[k] : -1;
+        if (off < 0) continue;
+        uint8_t* to = cell_of(k) + g.b * D + ((off >> 2) * D + ch) * 4 + (off & 3);
+        to[0] = (uint8_t)two[t], to[4] = (uint8_t)(two[t] >> 8);
+      }
+    }
+  };
+  // (a barrier waits for the stores before it: all of the passes in registers go out behind one)
+  uint2 kc[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    if (p < passes) kc[p] = encode(p, keys[p], values[p], codes_of_pass[p]);
+  __syncthreads();
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    if (p < passes) store(p, kc[p], codes_of_pass[p]);
+  for (int p = max(P, begin); p < passes; ++p) {
+    float x[8];
+    uint4 raw, y;
+    int pos;
+    load(p, raw, y, pos);
+    key_of<D, T>(a, pos, raw, lane, weight, x);
+    __syncthreads();
+    const uint2 c = encode(p, x, y, codes_of_pass[0]);
+    __syncthreads();
+    store(p, c, codes_of_pass[0]);
   }
 }
 
-// Workgroups up to `vector_blocks` take queries, the others keys and values.
 template <int D, class T, bool kMany>
-__global__ __launch_bounds__(kThreads) void store8(Geo g, StoreArgs a, Share part) {
+__global__ __launch_bounds__(kMany ? kManyThreads : kThreads, (kMany ? kManyWaves : 2)) void store8(Geo g, StoreArgs a, Share part) {
+  constexpr int W = kMany ? kManyThreads : kThreads;
   __shared__ Span span;
-  if (blockIdx.x < part.vector_blocks) {
-    queries<D, T, kMany ? kHeads : 1>(g, a, part);
+  __shared__ __attribute__((aligned(16))) uint8_t codes_of_pass[kMany ? kPasses : 1][8 * W];
+  if (blockIdx.x >= part.item_blocks) {
+    queries<D, T, kMany ? kHeads : 1, W>(g, a, part);
     return;
   }
-  for (unsigned item = blockIdx.x - part.vector_blocks; item < part.items; item += gridDim.x - part.vector_blocks) {
-    keys_values<D, T>(g, a, item, part.tile, span);
+  for (unsigned item = blockIdx.x; item < part.items; item += part.item_blocks) {
+    keys_values<D, T, kMany ? kPasses : 1, W>(g, a, item, part.tile, span, codes_of_pass);
     __syncthreads();
   }
 }
 
-// One vector a group of L lanes: keys and values of each token and kv head.
-template <int D, class T>
-__global__ __launch_bounds__(kThreads) void load8(Geo g, LoadArgs a) {
+// A group of L lanes takes one of a token's 2 hk vectors (keys, then values), or N of them, `groups` apart.
+template <int D, class T, int N>
+__global__ __launch_bounds__(kThreads) void load8(Geo g, LoadArgs a, unsigned groups) {
   constexpr int L = D / 8;
-  const int lane = threadIdx.x % L;
+  const int lane = threadIdx.x % L, vectors = 2 * g.hk;
   const unsigned v = blockIdx.x * (kThreads / L) + threadIdx.x / L;
-  const unsigned t = v / (2u * g.hk);
+  const unsigned t = v / groups, h0 = v - t * groups;
   if (t >= (unsigned)a.n_tokens) return;
-  const int h = (int)(v - t * (2u * g.hk));
-  const bool is_v = h >= g.hk;
-  const int kvh = is_v ? h - g.hk : h;
   const int64_t slot = a.slot[t], block = slot >> g.b_log2;
-  uint4* out = reinterpret_cast<uint4*>((uint16_t*)(is_v ? a.v : a.k) + ((int64_t)t * g.hk + kvh) * D) + lane;
-  if (slot < 0 || block >= g.n_blocks) {
-    *out = make_uint4(0, 0, 0, 0);
-    return;
-  }
-  const int off = (int)(slot & (g.b - 1));
-  const uint8_t* cell = a.cache + (block * g.hk + kvh) * (int64_t)g.cell;
-  const float s = reinterpret_cast<const float*>(cell + 2 * g.b * D)[is_v];
-  uint32_t codes[2];
-  if (!is_v) {
-    const uint2 w = reinterpret_cast<const uint2*>(cell + off * D)[lane];
-    codes[0] = w.x, codes[1] = w.y;
-  } else {
-    const uint8_t* from = cell + g.b * D + ((off >> 2) * D + lane * 8) * 4 + (off & 3);
-    codes[0] = codes[1] = 0;
+  const bool held = slot >= 0 && block < g.n_blocks;
+  const int off = (int)(slot & (g.b - 1)), by = 8 * (off & 3);
+  const uint8_t* cells = a.cache + (held ? block : 0) * g.hk * (int64_t)g.cell;
+  uint4 w[N][2];
+  uint32_t first[N];
+  float s[N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) codes[i / 4] |= (uint32_t)from[4 * i] << (8 * (i % 4));
-    // a token that is not a number says so in its key
-    if ((cell[off * D] & 0x7f) == 0x7f) codes[0] = codes[1] = 0x7f7f7f7fu;
+  for (int j = 0; j < N; ++j) {
+    const int h = min((int)(h0 + j * groups), vectors - 1);
+    const bool is_v = h >= g.hk;
+    const uint8_t* cell = cells + (is_v ? h - g.hk : h) * (int64_t)g.cell;
+    s[j] = reinterpret_cast<const float*>(cell + 2 * g.b * D)[is_v];
+    if (is_v) {
+      // the words of four tokens, as whole ones: one token's bytes would take as many lines
+      const uint4* from = reinterpret_cast<const uint4*>(cell + g.b * D + ((off >> 2) * D + lane * 8) * 4);
+      w[j][0] = from[0], w[j][1] = from[1];
+      first[j] = cell[off * D];
+    } else {
+      const uint2 x = reinterpret_cast<const uint2*>(cell + off * D)[lane];
+      w[j][0].x = x.x, w[j][0].y = x.y;
+    }
   }
-  float x[8];
-  values_of(codes[0], x);
-  values_of(codes[1], x + 4);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    x[i] *= s;
-    // the code's rounding can pass the type's range
-    if (fabsf(x[i]) > T::kMost) x[i] = copysignf(T::kMost, x[i]);
+  for (int j = 0; j < N; ++j) {
+    const int h = (int)(h0 + j * groups);
+    if (h >= vectors) break;
+    const bool is_v = h >= g.hk;
+    uint4* out = reinterpret_cast<uint4*>((uint16_t*)(is_v ? a.v : a.k) + ((int64_t)t * g.hk + (is_v ? h - g.hk : h)) * D) + lane;
+    if (!held) {
+      *out = make_uint4(0, 0, 0, 0);
+      continue;
+    }
+    uint32_t codes[2] = {w[j][0].x, w[j][0].y};
+    if (is_v) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        codes[i] = (w[j][i].x >> by & 0xff) | (w[j][i].y >> by & 0xff) << 8 | (w[j][i].z >> by & 0xff) << 16 | (w[j][i].w >> by & 0xff) << 24;
+      // a token that is not a number says so in its key
+      if ((first[j] & 0x7f) == 0x7f) codes[0] = codes[1] = 0x7f7f7f7fu;
+    }
+    float x[8];
+    values_of(codes[0], x);
+    values_of(codes[1], x + 4);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] *= s[j];
+      // the code's rounding can pass the type's range
+      if (fabsf(x[i]) > T::kMost) x[i] = copysignf(T::kMost, x[i]);
+    }
+    *out = pack<T>(x);
   }
-  *out = pack<T>(x);
 }
 
 // Tokens of one launch: a grid has fewer than 2^32 threads.
@@ -305,19 +428,21 @@ struct Store8 {
   template <int D, class T>
   hipError_t operator()() {
     constexpr int64_t L = D / 8;
-    const bool many = (int64_t)a.n_tokens * g.hq >= kManyVectors;
+    const bool many = (int64_t)a.n_tokens * (g.hq + 2 * g.hk) >= kManyVectors;
+    const int threads = many ? kManyThreads : kThreads;
     Share part;
-    part.tile = a.n_tokens * (int64_t)g.hk >= kManyVectors / 4 ? kMostTile : 16;
+    // two passes, or a block; one pass of a smaller workgroup
+    part.tile = many ? std::max(kPasses * kManyThreads / (int)L, g.b) : kThreads / (int)L;
     part.groups = (unsigned)(many ? (g.hq + kHeads - 1) / kHeads : g.hq);
     part.items = (unsigned)((a.n_tokens + part.tile - 1) / part.tile) * (unsigned)g.hk;
     // all keys and values in the first launch, so that no run is cut
     const int most = most_tokens(part.groups * L);
     for (part.token = 0; part.token < a.n_tokens; part.token += most, part.items = 0) {
       part.tokens = std::min(most, a.n_tokens - part.token);
-      part.vector_blocks = (unsigned)((part.tokens * (int64_t)part.groups * L + kThreads - 1) / kThreads);
-      const dim3 grid(part.vector_blocks + std::min(part.items, 1u << 22));
-      if (many) hipLaunchKernelGGL((store8<D, T, true>), grid, dim3(kThreads), 0, s, g, a, part);
-      else hipLaunchKernelGGL((store8<D, T, false>), grid, dim3(kThreads), 0, s, g, a, part);
+      part.item_blocks = std::min(part.items, 1u << 22);
+      const dim3 grid(part.item_blocks + (unsigned)((part.tokens * (int64_t)part.groups * L + threads - 1) / threads));
+      if (many) hipLaunchKernelGGL((store8<D, T, true>), grid, dim3(threads), 0, s, g, a, part);
+      else hipLaunchKernelGGL((store8<D, T, false>), grid, dim3(threads), 0, s, g, a, part);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
@@ -331,7 +456,9 @@ struct Load8 {
   hipStream_t s;
   template <int D, class T>
   hipError_t operator()() {
-    const int64_t width = (int64_t)2 * g.hk * (D / 8);
+    const bool many = (int64_t)a.n_tokens * 2 * g.hk >= kManyVectors;
+    const unsigned groups = many ? (2u * g.hk + kHeads - 1) / kHeads : 2u * g.hk;
+    const int64_t width = (int64_t)groups * (D / 8);
     const int most = most_tokens(width);
     for (int t0 = 0; t0 < a.n_tokens; t0 += most) {
       LoadArgs b = a;
@@ -339,7 +466,9 @@ struct Load8 {
       b.k = (uint16_t*)a.k + (int64_t)t0 * g.hk * D;
       b.v = (uint16_t*)a.v + (int64_t)t0 * g.hk * D;
       b.n_tokens = std::min(most, a.n_tokens - t0);
-      hipLaunchKernelGGL((load8<D, T>), dim3((unsigned)((b.n_tokens * width + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, g, b);
+      const dim3 grid((unsigned)((b.n_tokens * width + kThreads - 1) / kThreads));
+      if (many) hipLaunchKernelGGL((load8<D, T, kHeads>), grid, dim3(kThreads), 0, s, g, b, groups);
+      else hipLaunchKernelGGL((load8<D, T, 1>), grid, dim3(kThreads), 0, s, g, b, groups);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
