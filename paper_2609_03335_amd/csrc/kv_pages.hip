@@ -2,9 +2,11 @@
 //
 // Integer arithmetic only, but for the copies.  What has to be in order -- which fork gets which block
 // of the ring, the ring's new entries, the k-th block that moves and the k-th place for it -- comes from prefix
-// sums over lists or block ids; atomics only count, so that their order does not matter.  A kernel a phase,
-// as each needs all of the one before: bound by the launches' latency (2 to 3 us each), then by the arrays of
-// n_blocks entries.
+// sums over lists or block ids; atomics only count, so that their order does not matter.
+//
+// Each phase needs all of the one before.  Caches of up to kOneBlocks blocks are the work of one workgroup, with what
+// it knows of every block in LDS: one launch (from Python 8 us, of which the kernel is ...).  Larger ones take a
+// kernel a phase, 2 to 3 us and a place in the queue each.
 #include "kv.h"
 
 namespace wfkv {
@@ -12,6 +14,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kScan = 1024;              // threads of a workgroup that scans
+constexpr int kOneBlocks = 32768, kOneEntries = 32768;  // blocks and table entries of one workgroup
+constexpr int kSteps = kOneBlocks / kScan;
 constexpr int kChunks = WF_KV_PAGES_WORK / 4;  // parts of the block ids that are counted by themselves
 
 // Sum of the threads' values before this one in a workgroup of kScan, and of all.
@@ -172,6 +176,139 @@ __global__ __launch_bounds__(kScan) void release_write(Geo g, ReleaseArgs a) {
   }
 }
 
+// For one workgroup: entries of a list of up to kOneBlocks that a test picks, in order.  count() takes the
+// test of one's entries in steps of kScan, first() then gives the place of a step's first one in this wave.
+struct Picked {
+  uint16_t (*of)[kScan / 64];  // [kSteps][waves]: picked, then picked before
+  uint32_t* part;
+  __device__ __forceinline__ void count(int step, bool pick) {
+    const uint64_t mask = __ballot(pick);
+    if ((threadIdx.x & 63) == 0) of[step][threadIdx.x >> 6] = (uint16_t)__popcll(mask);
+  }
+  __device__ __forceinline__ uint32_t scan(int steps) {
+    __syncthreads();
+    uint16_t* at = &of[0][0] + threadIdx.x;
+    const bool in = (int)threadIdx.x < steps * (kScan / 64);
+    uint32_t total;
+    const uint32_t n = in ? *at : 0, x = before(n, &total, part);
+    if (in) *at = (uint16_t)x;
+    __syncthreads();
+    return total;
+  }
+  __device__ __forceinline__ uint32_t place(int step, bool pick) const {
+    return of[step][threadIdx.x >> 6] + (uint32_t)__popcll(__ballot(pick) & ((1ull << (threadIdx.x & 63)) - 1ull));
+  }
+};
+static_assert(kSteps * (kScan / 64) <= kScan, "a thread for every count");
+
+// The rows that `pick` names, each the work of a wave's 64 lanes (`act`); neighbours go to different waves.
+template <class P, class A>
+__device__ __forceinline__ void each_row(int n_rows, P pick, A act) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int r0 = 0; r0 < n_rows; r0 += kScan) {
+    const int r = r0 + lane * (kScan / 64) + wave;
+    uint64_t todo = __ballot(r < n_rows && pick(r));
+    while (todo) {
+      const int src = __ffsll((unsigned long long)todo) - 1;
+      todo &= todo - 1;
+      act(r0 + src * (kScan / 64) + wave, lane);
+    }
+  }
+}
+
+__global__ __launch_bounds__(kScan) void release_one(Geo g, ReleaseArgs a) {
+  __shared__ int left[kOneBlocks];
+  __shared__ uint16_t counts[kSteps][kScan / 64];
+  __shared__ uint32_t part[kScan / 64];
+  const Pool pool(g, a.pool_in);
+#pragma unroll 8
+  for (int b = threadIdx.x; b < g.n_blocks; b += kScan) left[b] = a.shared_in[b];
+  __syncthreads();
+  each_row(
+      a.n_rows,
+      [&](int r) {
+        const bool ends = a.release[r] != 0;
+        a.len_out[r] = ends ? 0 : a.len_in[r];
+        return ends;
+      },
+      [&](int r, int lane) {
+        const int32_t* mine = a.table + (int64_t)r * g.width;
+        const int have = held(g, a.len_in[r]);
+#pragma unroll 4
+        for (int j = lane; j < have; j += 64) {
+          const int id = mine[j];
+          if ((unsigned)id < (unsigned)g.n_blocks) atomicSub(left + id, 1);
+        }
+      });
+  __syncthreads();
+  Picked over{counts, part};
+  const int steps = (g.n_blocks + kScan - 1) / kScan;
+  for (int k = 0; k < steps; ++k) {
+    const int b = k * kScan + (int)threadIdx.x;
+    over.count(k, b < g.n_blocks && left[b] < 0);
+  }
+  const uint32_t all = over.scan(steps);
+  for (int k = 0; k < steps; ++k) {
+    const int b = k * kScan + (int)threadIdx.x;
+    const int n = b < g.n_blocks ? left[b] : 0;
+    const uint32_t at = over.place(k, n < 0);
+    if (n < 0) a.ring[(pool.head + pool.room + at) % pool.n] = b;
+    if (b < g.n_blocks) a.shared_out[b] = max(n, 0);
+  }
+  if (threadIdx.x == 0) {
+    a.pool_out[0] = (int)pool.head;
+    a.pool_out[1] = (int)min(pool.room + all, pool.n);
+  }
+}
+
+__global__ __launch_bounds__(kScan) void fork_one(Geo g, ForkArgs a) {
+  __shared__ int count[kOneBlocks];
+  __shared__ uint32_t part[kScan / 64];
+  const Pool pool(g, a.pool_in);
+#pragma unroll 8
+  for (int b = threadIdx.x; b < g.n_blocks; b += kScan) count[b] = a.shared_in[b];
+  const int i = (int)threadIdx.x;  // a fork a thread
+  const int k = i < a.n_forks ? fork_tokens(g, a, i) : -1;
+  const uint32_t need = k > 0 && (k & (g.b - 1)) != 0;
+  uint32_t total;
+  const uint32_t at = before(need, &total, part);
+  const bool ok = k >= 0 && (!need || at < pool.room);
+  const int full = ok ? k >> g.b_log2 : 0, src = ok ? a.src[i] : 0, dst = ok ? a.dst[i] : 0;
+  // lengths of the rows that no fork fills, then of those
+  copy_ints(a.len_in, a.len_out, a.n_rows, threadIdx.x, kScan);
+  if (i < a.n_forks) {
+    a.granted[i] = ok;
+    const int old = ok && need ? a.table[(int64_t)src * g.width + full] : -1, fresh = ok && need ? a.ring[(pool.head + at) % pool.n] : -1;
+    a.from[i] = old;
+    a.to[i] = fresh;
+    if (ok && need) a.table[(int64_t)dst * g.width + full] = fresh;
+  }
+  __syncthreads();
+  if (ok) a.len_out[dst] = k;
+  const int lane = threadIdx.x & 63;
+  uint64_t todo = __ballot(full > 0);
+  while (todo) {
+    const int who = __ffsll((unsigned long long)todo) - 1;
+    todo &= todo - 1;
+    const int n = __shfl(full, who, 64);
+    const int32_t* theirs = a.table + (int64_t)__shfl(src, who, 64) * g.width;
+    int32_t* mine = a.table + (int64_t)__shfl(dst, who, 64) * g.width;
+#pragma unroll 4
+    for (int j = lane; j < n; j += 64) {
+      const int id = theirs[j];
+      mine[j] = id;
+      if ((unsigned)id < (unsigned)g.n_blocks) atomicAdd(count + id, 1);
+    }
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < g.n_blocks; b += kScan) a.shared_out[b] = count[b];
+  if (threadIdx.x == 0) {
+    const uint32_t taken = min(total, pool.room);
+    a.pool_out[0] = (int)((pool.head + taken) % pool.n);
+    a.pool_out[1] = (int)(pool.room - taken);
+  }
+}
+
 // What ids[] of a block says: in use, free; below `keep` and free, kTaken - k: it becomes the place of the
 // k-th block that moves; from `keep` on and in use, k: it is that block.
 constexpr int kUsed = 0, kFree = -1, kTaken = -2;
@@ -258,25 +395,91 @@ __global__ __launch_bounds__(kThreads) void compact_rows(Geo g, CompactArgs a, u
   }
 }
 
-// 16 KiB of a pair of blocks in one layer a step of a workgroup.
-constexpr int kPiece = 4 * kThreads;
+__global__ __launch_bounds__(kScan) void compact_one(Geo g, CompactArgs a) {
+  // of a block: in use, free, or the place among those that move (`goes`); the k-th free one of the front
+  constexpr uint16_t kIn = 0xffff, kOut = 0xfffe;
+  __shared__ uint16_t state[kOneBlocks], hole_id[kOneBlocks];
+  __shared__ uint16_t counts[2][kSteps][kScan / 64];
+  __shared__ uint32_t part[kScan / 64];
+  const Pool pool(g, a.pool_in);
+  for (int b = threadIdx.x; b < g.n_blocks; b += kScan) state[b] = kIn;
+  __syncthreads();
+#pragma unroll 4
+  for (uint32_t i = threadIdx.x; i < pool.room; i += kScan) {
+    const int id = a.ring_in[(pool.head + i) % pool.n];
+    if ((unsigned)id < (unsigned)g.n_blocks) state[id] = kOut;
+  }
+  __syncthreads();
+  const int steps = (g.n_blocks + kScan - 1) / kScan;
+  Picked goes{counts[0], part}, holes{counts[1], part};
+  for (int k = 0; k < steps; ++k) {
+    const int b = k * kScan + (int)threadIdx.x;
+    const bool in = b < g.n_blocks, used = in && state[b] == kIn;
+    goes.count(k, used && b >= a.keep);
+    holes.count(k, in && !used && b < a.keep);
+  }
+  const uint32_t n_goes = goes.scan(steps), n_holes = holes.scan(steps);
+  const bool done = n_goes <= n_holes;
+  const int most = min(a.keep, g.n_blocks - a.keep);
+  for (int i = (int)(done ? n_goes : 0u) + (int)threadIdx.x; i < most; i += kScan) a.from[i] = a.to[i] = -1;
+  for (int i = (int)(done ? n_holes - n_goes : 0u) + (int)threadIdx.x; i < a.keep; i += kScan) a.ring_out[i] = -1;
+  if (threadIdx.x == 0) {
+    a.done[0] = done;
+    a.pool_out[0] = 0;
+    a.pool_out[1] = done ? (int)(n_holes - n_goes) : 0;
+  }
+  if (!done) return;  // (all threads)
+  for (int k = 0; k < steps; ++k) {
+    const int b = k * kScan + (int)threadIdx.x;
+    const bool in = b < g.n_blocks, used = in && state[b] == kIn;
+    const bool go = used && b >= a.keep, hole = in && !used && b < a.keep;
+    const uint32_t i = goes.place(k, go), j = holes.place(k, hole);
+    if (go) a.from[i] = b, state[b] = (uint16_t)i;  // (i < n_blocks / 2)
+    if (hole) hole_id[j] = (uint16_t)b;
+    if (hole && j < n_goes) a.to[j] = b;
+    if (hole && j >= n_goes) a.ring_out[j - n_goes] = b;
+  }
+  __syncthreads();
+  // counts by new id: those that stay, those that come, 0 for what is free
+  for (int b = threadIdx.x; b < a.keep; b += kScan)
+    if (state[b] == kIn) a.shared_out[b] = a.shared_in[b];
+  for (int b = a.keep + (int)threadIdx.x; b < g.n_blocks; b += kScan)
+    if (state[b] < kOut) a.shared_out[hole_id[state[b]]] = a.shared_in[b];
+  for (uint32_t j = n_goes + threadIdx.x; j < n_holes; j += kScan) a.shared_out[hole_id[j]] = 0;
+  each_row(
+      a.n_rows, [&](int r) { return a.len[r] > 0; },
+      [&](int r, int lane) {
+        int32_t* mine = a.table + (int64_t)r * g.width;
+        const int have = held(g, a.len[r]);
+#pragma unroll 4
+        for (int j = lane; j < have; j += 64) {
+          const int id = mine[j];
+          // (a free block, which no row should hold, stays as it is)
+          if (id >= a.keep && id < g.n_blocks && state[id] < kOut) mine[j] = hole_id[state[id]];
+        }
+      });
+}
 
+// A workgroup's step: 16 KiB of a pair of blocks in one layer, four loads of a thread on their way at once (its
+// registers are plain vectors and filled without a condition: what may be missing would go through LDS, one by one).
+constexpr int kPiece = 4 * kThreads;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// grid: pieces x pairs (those after come in turns), layers
 __global__ __launch_bounds__(kThreads) void copy(CopyArgs a, int n_blocks, int vectors, unsigned pieces) {
-  const uint64_t all = (uint64_t)pieces * a.n * a.n_layers;
-  for (uint64_t x = blockIdx.x; x < all; x += gridDim.x) {
-    const unsigned piece = (unsigned)(x % pieces);
-    const uint64_t y = x / pieces;
-    const int i = (int)(y % (unsigned)a.n), layer = (int)(y / (unsigned)a.n);
-    const int from = a.from[i], to = a.to[i];
+  const unsigned piece = blockIdx.x % pieces, step = gridDim.x / pieces;
+  u32x4* base = reinterpret_cast<u32x4*>(a.cache + blockIdx.y * a.layer_stride);
+  const auto* froms = (const __attribute__((address_space(4))) int32_t*)a.from;
+  const auto* tos = (const __attribute__((address_space(4))) int32_t*)a.to;
+  const int v0 = (int)(piece * kPiece + threadIdx.x);
+  for (unsigned i = blockIdx.x / pieces; i < (unsigned)a.n; i += step) {
+    const int from = froms[i], to = tos[i];
     if (from == to || (unsigned)from >= (unsigned)n_blocks || (unsigned)to >= (unsigned)n_blocks) continue;
-    uint4* base = reinterpret_cast<uint4*>(a.cache + layer * a.layer_stride);
-    const uint4* src = base + (int64_t)from * vectors;
-    uint4* dst = base + (int64_t)to * vectors;
-    const int v0 = (int)(piece * kPiece + threadIdx.x);
-    uint4 w[4];
+    const u32x4* src = base + (int64_t)from * vectors;
+    u32x4* dst = base + (int64_t)to * vectors;
+    u32x4 w[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (v0 + k * kThreads < vectors) w[k] = src[v0 + k * kThreads];
+    for (int k = 0; k < 4; ++k) w[k] = src[min(v0 + k * kThreads, vectors - 1)];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (v0 + k * kThreads < vectors) dst[v0 + k * kThreads] = w[k];
@@ -293,6 +496,11 @@ unsigned groups_of(int64_t n, int threads) { return (unsigned)std::max<int64_t>(
 }  // namespace
 
 hipError_t launch_fork(const Geo& g, const ForkArgs& a, hipStream_t s) {
+  // (a workgroup goes through the forks' entries in steps of 1,024)
+  if (g.n_blocks <= kOneBlocks && a.n_forks <= kScan && (int64_t)a.n_forks * g.width <= kOneEntries / 2) {
+    hipLaunchKernelGGL(fork_one, dim3(1), dim3(kScan), 0, s, g, a);
+    return hipGetLastError();
+  }
   const unsigned copies = groups_of(std::max(g.n_blocks, a.n_rows), kScan);
   hipLaunchKernelGGL(fork_grant, dim3(1 + copies), dim3(kScan), 0, s, g, a);
   hipError_t e = hipGetLastError();
@@ -303,6 +511,10 @@ hipError_t launch_fork(const Geo& g, const ForkArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_release(const Geo& g, const ReleaseArgs& a, hipStream_t s) {
+  if (g.n_blocks <= kOneBlocks && (int64_t)a.n_rows * g.width <= 2 * kOneEntries) {
+    hipLaunchKernelGGL(release_one, dim3(1), dim3(kScan), 0, s, g, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(release_begin, dim3(groups_of(std::max(g.n_blocks, a.n_rows), kThreads)), dim3(kThreads), 0, s, g, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.n_rows) {
@@ -319,6 +531,10 @@ hipError_t launch_release(const Geo& g, const ReleaseArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_compact(const Geo& g, const CompactArgs& a, hipStream_t s) {
+  if (g.n_blocks <= kOneBlocks && (int64_t)a.n_rows * g.width <= kOneEntries) {
+    hipLaunchKernelGGL(compact_one, dim3(1), dim3(kScan), 0, s, g, a);
+    return hipGetLastError();
+  }
   const unsigned over = groups_of(g.n_blocks, kThreads);
   hipLaunchKernelGGL(compact_begin, dim3(over), dim3(kThreads), 0, s, g, a);
   hipError_t e = hipGetLastError();
@@ -341,8 +557,8 @@ hipError_t launch_compact(const Geo& g, const CompactArgs& a, hipStream_t s) {
 hipError_t launch_copy(const Geo& g, const CopyArgs& a, int n_cu, hipStream_t s) {
   const int vectors = (int)((int64_t)g.hk * g.cell / 16);
   const unsigned pieces = (unsigned)((vectors + kPiece - 1) / kPiece);
-  const uint64_t all = (uint64_t)pieces * a.n * a.n_layers;
-  hipLaunchKernelGGL(copy, dim3((unsigned)std::min<uint64_t>(all, (uint64_t)n_cu * 16)), dim3(kThreads), 0, s, a, g.n_blocks, vectors, pieces);
+  const int64_t pairs = std::max<int64_t>(1, std::min<int64_t>(a.n, (int64_t)n_cu * 16 / ((int64_t)pieces * a.n_layers)));
+  hipLaunchKernelGGL(copy, dim3((unsigned)(pairs * pieces), (unsigned)a.n_layers), dim3(kThreads), 0, s, a, g.n_blocks, vectors, pieces);
   return hipGetLastError();
 }
 
