@@ -462,6 +462,7 @@ __global__ __launch_bounds__(kScan) void compact_one(Geo g, CompactArgs a) {
 
 // A workgroup's step: 16 KiB of a pair of blocks in one layer, four loads of a thread on their way at once (its
 // registers are plain vectors and filled without a condition: what may be missing would go through LDS, one by one).
+// Stores past the caches: 900 blocks of 131 KB 51 -> 47 us (5.1 TB/s), 800 of 66 KB in two layers 47 -> 40; eight loads 52 us.
 constexpr int kPiece = 4 * kThreads;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -482,7 +483,7 @@ __global__ __launch_bounds__(kThreads) void copy(CopyArgs a, int n_blocks, int v
     for (int k = 0; k < 4; ++k) w[k] = src[min(v0 + k * kThreads, vectors - 1)];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (v0 + k * kThreads < vectors) dst[v0 + k * kThreads] = w[k];
+      if (v0 + k * kThreads < vectors) __builtin_nontemporal_store(w[k], dst + v0 + k * kThreads);
   }
 }
 
