@@ -388,18 +388,25 @@ PyObject* geometry(PyObject*, PyObject* args) {
   return c;
 }
 
-// calls(step, store, load, attend, fork, release, compact, copy): their addresses in the loaded library.
+// calls(step, store, load, attend): their addresses in the loaded library.
 PyObject* calls(PyObject*, PyObject* args) {
-  unsigned long long p[8];
-  if (!PyArg_ParseTuple(args, "KKKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7])) return nullptr;
-  g_step = reinterpret_cast<decltype(g_step)>((uintptr_t)p[0]);
-  g_store = reinterpret_cast<decltype(g_store)>((uintptr_t)p[1]);
-  g_load = reinterpret_cast<decltype(g_load)>((uintptr_t)p[2]);
-  g_attend = reinterpret_cast<decltype(g_attend)>((uintptr_t)p[3]);
-  g_fork = reinterpret_cast<decltype(g_fork)>((uintptr_t)p[4]);
-  g_release = reinterpret_cast<decltype(g_release)>((uintptr_t)p[5]);
-  g_compact = reinterpret_cast<decltype(g_compact)>((uintptr_t)p[6]);
-  g_copy = reinterpret_cast<decltype(g_copy)>((uintptr_t)p[7]);
+  unsigned long long s, t, l, a;
+  if (!PyArg_ParseTuple(args, "KKKK", &s, &t, &l, &a)) return nullptr;
+  g_step = reinterpret_cast<decltype(g_step)>((uintptr_t)s);
+  g_store = reinterpret_cast<decltype(g_store)>((uintptr_t)t);
+  g_load = reinterpret_cast<decltype(g_load)>((uintptr_t)l);
+  g_attend = reinterpret_cast<decltype(g_attend)>((uintptr_t)a);
+  Py_RETURN_NONE;
+}
+
+// page_calls(fork, release, compact, copy): likewise.
+PyObject* page_calls(PyObject*, PyObject* args) {
+  unsigned long long f, r, c, k;
+  if (!PyArg_ParseTuple(args, "KKKK", &f, &r, &c, &k)) return nullptr;
+  g_fork = reinterpret_cast<decltype(g_fork)>((uintptr_t)f);
+  g_release = reinterpret_cast<decltype(g_release)>((uintptr_t)r);
+  g_compact = reinterpret_cast<decltype(g_compact)>((uintptr_t)c);
+  g_copy = reinterpret_cast<decltype(g_copy)>((uintptr_t)k);
   Py_RETURN_NONE;
 }
 
@@ -418,6 +425,7 @@ PyMethodDef g_methods[] = {{"step", fast(step), METH_FASTCALL, nullptr},
                            {"copy", fast(copy), METH_FASTCALL, nullptr},
                            {"geometry", geometry, METH_VARARGS, nullptr},
                            {"calls", calls, METH_VARARGS, nullptr},
+                           {"page_calls", page_calls, METH_VARARGS, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_kvbind", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

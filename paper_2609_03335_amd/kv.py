@@ -255,9 +255,9 @@ def _bind():
     except ImportError:
         return None
     lib = load()
-    _kvbind.calls(*(ctypes.cast(f, ctypes.c_void_p).value
-                    for f in (lib.wf_kv_step, lib.wf_kv_store, lib.wf_kv_load, lib.wf_kv_attend, lib.wf_kv_fork,
-                              lib.wf_kv_release, lib.wf_kv_compact, lib.wf_kv_copy)))
+    address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+    _kvbind.calls(*map(address, (lib.wf_kv_step, lib.wf_kv_store, lib.wf_kv_load, lib.wf_kv_attend)))
+    _kvbind.page_calls(*map(address, (lib.wf_kv_fork, lib.wf_kv_release, lib.wf_kv_compact, lib.wf_kv_copy)))
     return _kvbind
 
 
