@@ -16,6 +16,7 @@ constexpr int kThreads = 256;
 constexpr int kScan = 1024;              // threads of a workgroup that scans
 constexpr int kOneBlocks = 32768, kOneEntries = 32768;  // blocks and table entries of one workgroup
 constexpr int kSteps = kOneBlocks / kScan;
+constexpr int kAtOnce = 4;               // ids of a thread that are looked at at once
 constexpr int kChunks = WF_KV_PAGES_WORK / 4;  // parts of the block ids that are counted by themselves
 
 // Sum of the threads' values before this one in a workgroup of kScan, and of all.
@@ -143,39 +144,6 @@ __device__ __forceinline__ uint32_t sum_of(uint32_t x, uint32_t* part) {
   return total;
 }
 
-__global__ __launch_bounds__(kScan) void release_count(Geo g, ReleaseArgs a) {
-  __shared__ uint32_t part[kScan / 64];
-  const Chunk c(g, blockIdx.x, gridDim.x);
-  uint32_t n = 0;
-  for (int b = c.first + (int)threadIdx.x; b < c.last; b += kScan) n += a.shared_out[b] < 0;
-  n = sum_of(n, part);
-  if (threadIdx.x == 0) a.work[blockIdx.x] = (int)n;
-}
-
-__global__ __launch_bounds__(kScan) void release_write(Geo g, ReleaseArgs a) {
-  __shared__ uint32_t part[kScan / 64];
-  const Pool pool(g, a.pool_in);
-  const Chunk c(g, blockIdx.x, gridDim.x);
-  const uint32_t mine = threadIdx.x < gridDim.x ? (uint32_t)a.work[threadIdx.x] : 0;
-  const uint32_t all = sum_of(mine, part);
-  uint32_t base = sum_of(threadIdx.x < blockIdx.x ? mine : 0, part);
-  for (int b0 = c.first; b0 < c.last; b0 += kScan) {
-    const int b = b0 + (int)threadIdx.x;
-    const uint32_t over = b < c.last && a.shared_out[b] < 0;
-    uint32_t total;
-    const uint32_t at = base + before(over, &total, part);
-    if (over) {
-      a.ring[(pool.head + pool.room + at) % pool.n] = b;
-      a.shared_out[b] = 0;
-    }
-    base += total;
-  }
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    a.pool_out[0] = (int)pool.head;
-    a.pool_out[1] = (int)min(pool.room + all, pool.n);
-  }
-}
-
 // For one workgroup: entries of a list of up to kOneBlocks that a test picks, in order.  count() takes the
 // test of one's entries in steps of kScan, first() then gives the place of a step's first one in this wave.
 struct Picked {
@@ -201,18 +169,82 @@ struct Picked {
 };
 static_assert(kSteps * (kScan / 64) <= kScan, "a thread for every count");
 
-// The rows that `pick` names, each the work of a wave's 64 lanes (`act`); neighbours go to different waves.
-template <class P, class A>
-__device__ __forceinline__ void each_row(int n_rows, P pick, A act) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int r0 = 0; r0 < n_rows; r0 += kScan) {
-    const int r = r0 + lane * (kScan / 64) + wave;
-    uint64_t todo = __ballot(r < n_rows && pick(r));
-    while (todo) {
-      const int src = __ffsll((unsigned long long)todo) - 1;
-      todo &= todo - 1;
-      act(r0 + src * (kScan / 64) + wave, lane);
+__global__ __launch_bounds__(kScan) void release_count(Geo g, ReleaseArgs a) {
+  __shared__ uint32_t part[kScan / 64];
+  const Chunk c(g, blockIdx.x, gridDim.x);
+  uint32_t n = 0;
+#pragma unroll 4
+  for (int b = c.first + (int)threadIdx.x; b < c.last; b += kScan) n += a.shared_out[b] < 0;
+  n = sum_of(n, part);
+  if (threadIdx.x == 0) a.work[blockIdx.x] = (int)n;
+}
+
+// The sum of the chunks' counts before this one (of every `stride`-th entry of work, from `at` on), and of all.
+__device__ __forceinline__ uint32_t chunks_before(const int32_t* work, int stride, int at, uint32_t* all, uint32_t* part) {
+  __shared__ uint32_t mine;
+  const uint32_t n = threadIdx.x < gridDim.x ? (uint32_t)work[stride * threadIdx.x + at] : 0;
+  const uint32_t x = before(n, all, part);
+  if (threadIdx.x == blockIdx.x) mine = x;
+  __syncthreads();
+  const uint32_t out = mine;
+  __syncthreads();
+  return out;
+}
+
+__global__ __launch_bounds__(kScan) void release_write(Geo g, ReleaseArgs a) {
+  __shared__ uint32_t part[kScan / 64];
+  __shared__ uint16_t counts[kAtOnce][kScan / 64];
+  const Pool pool(g, a.pool_in);
+  const Chunk c(g, blockIdx.x, gridDim.x);
+  uint32_t all;
+  uint32_t base = chunks_before(a.work, 1, 0, &all, part);
+  Picked over{counts, part};
+  for (int b0 = c.first; b0 < c.last; b0 += kAtOnce * kScan) {
+    bool mine[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int b = b0 + k * kScan + (int)threadIdx.x;
+      mine[k] = a.shared_out[min(b, c.last - 1)] < 0 && b < c.last;
     }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) over.count(k, mine[k]);
+    const uint32_t total = over.scan(kAtOnce);
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int b = b0 + k * kScan + (int)threadIdx.x;
+      const uint32_t at = base + over.place(k, mine[k]);
+      if (mine[k]) {
+        a.ring[(pool.head + pool.room + at) % pool.n] = b;
+        a.shared_out[b] = 0;
+      }
+    }
+    base += total;
+    __syncthreads();
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    a.pool_out[0] = (int)pool.head;
+    a.pool_out[1] = (int)min(pool.room + all, pool.n);
+  }
+}
+
+// The table entries of the rows' blocks, have(r) of row r: act(its index in the table, its id), for ids of the cache.  Eight
+// a thread are on their way at once.
+template <class H, class A>
+__device__ __forceinline__ void each_entry(const Geo& g, const int32_t* table, int n_rows, H have, A act) {
+  constexpr int N = 8;
+  const unsigned width = (unsigned)g.width, all = (unsigned)n_rows * width;
+  for (unsigned x0 = threadIdx.x; x0 < all; x0 += N * kScan) {
+    int id[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const unsigned x = min(x0 + u * kScan, all - 1), r = x / width;
+      id[u] = (int)(x - r * width) < have((int)r) ? (int)x : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) id[u] = id[u] >= 0 ? table[id[u]] : -1;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      if (x0 + u * kScan < all && (unsigned)id[u] < (unsigned)g.n_blocks) act(x0 + u * kScan, id[u]);
   }
 }
 
@@ -224,22 +256,28 @@ __global__ __launch_bounds__(kScan) void release_one(Geo g, ReleaseArgs a) {
 #pragma unroll 8
   for (int b = threadIdx.x; b < g.n_blocks; b += kScan) left[b] = a.shared_in[b];
   __syncthreads();
-  each_row(
-      a.n_rows,
-      [&](int r) {
-        const bool ends = a.release[r] != 0;
-        a.len_out[r] = ends ? 0 : a.len_in[r];
-        return ends;
-      },
-      [&](int r, int lane) {
-        const int32_t* mine = a.table + (int64_t)r * g.width;
-        const int have = held(g, a.len_in[r]);
-#pragma unroll 4
-        for (int j = lane; j < have; j += 64) {
-          const int id = mine[j];
-          if ((unsigned)id < (unsigned)g.n_blocks) atomicSub(left + id, 1);
-        }
-      });
+  // (few rows end at a time: a wave takes one after the other of those, neighbours go to different waves)
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int r0 = 0; r0 < a.n_rows; r0 += kScan) {
+    const int r = r0 + lane * (kScan / 64) + wave, len = r < a.n_rows ? a.len_in[r] : 0;
+    const bool ends = r < a.n_rows && a.release[r] != 0;
+    if (r < a.n_rows) a.len_out[r] = ends ? 0 : len;
+    uint64_t todo = __ballot(ends);
+    while (todo) {
+      const int who = __ffsll((unsigned long long)todo) - 1;
+      todo &= todo - 1;
+      const int32_t* mine = a.table + (int64_t)(r0 + who * (kScan / 64) + wave) * g.width;
+      const int have = held(g, __shfl(len, who, 64));
+      for (int j0 = lane; j0 < have; j0 += 8 * 64) {
+        int id[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) id[u] = mine[min(j0 + u * 64, have - 1)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (j0 + u * 64 < have && (unsigned)id[u] < (unsigned)g.n_blocks) atomicSub(left + id[u], 1);
+      }
+    }
+  }
   __syncthreads();
   Picked over{counts, part};
   const int steps = (g.n_blocks + kScan - 1) / kScan;
@@ -285,19 +323,27 @@ __global__ __launch_bounds__(kScan) void fork_one(Geo g, ForkArgs a) {
   }
   __syncthreads();
   if (ok) a.len_out[dst] = k;
-  const int lane = threadIdx.x & 63;
-  uint64_t todo = __ballot(full > 0);
-  while (todo) {
-    const int who = __ffsll((unsigned long long)todo) - 1;
-    todo &= todo - 1;
-    const int n = __shfl(full, who, 64);
-    const int32_t* theirs = a.table + (int64_t)__shfl(src, who, 64) * g.width;
-    int32_t* mine = a.table + (int64_t)__shfl(dst, who, 64) * g.width;
-#pragma unroll 4
-    for (int j = lane; j < n; j += 64) {
-      const int id = theirs[j];
-      mine[j] = id;
-      if ((unsigned)id < (unsigned)g.n_blocks) atomicAdd(count + id, 1);
+  // the whole blocks, eight entries of a thread at once, of all forks together
+  __shared__ int of_fork[3][kScan];
+  of_fork[0][i] = full, of_fork[1][i] = src, of_fork[2][i] = dst;
+  __syncthreads();
+  constexpr int N = 8;
+  const unsigned width = (unsigned)g.width, all = (unsigned)a.n_forks * width;
+  for (unsigned x0 = threadIdx.x; x0 < all; x0 += N * kScan) {
+    int id[N];
+    int64_t to[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const unsigned x = min(x0 + u * kScan, all - 1), f = x / width, j = x - f * width;
+      const bool in = x0 + u * kScan < all && (int)j < of_fork[0][f];
+      to[u] = in ? (int64_t)of_fork[2][f] * g.width + j : -1;
+      id[u] = in ? a.table[(int64_t)of_fork[1][f] * g.width + j] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      if (to[u] < 0) continue;
+      a.table[to[u]] = id[u];
+      if ((unsigned)id[u] < (unsigned)g.n_blocks) atomicAdd(count + id[u], 1);
     }
   }
   __syncthreads();
@@ -329,6 +375,7 @@ __global__ __launch_bounds__(kScan) void compact_count(Geo g, CompactArgs a) {
   __shared__ uint32_t part[kScan / 64];
   const Chunk c(g, blockIdx.x, gridDim.x);
   uint32_t goes = 0, hole = 0;
+#pragma unroll 4
   for (int b = c.first + (int)threadIdx.x; b < c.last; b += kScan) {
     const bool used = a.ids[b] == kUsed;
     goes += used && b >= a.keep;
@@ -342,10 +389,9 @@ __global__ __launch_bounds__(kScan) void compact_count(Geo g, CompactArgs a) {
 __global__ __launch_bounds__(kScan) void compact_place(Geo g, CompactArgs a) {
   __shared__ uint32_t part[kScan / 64];
   const Chunk c(g, blockIdx.x, gridDim.x);
-  const bool in = threadIdx.x < gridDim.x, lower = threadIdx.x < blockIdx.x;
-  const uint32_t my_goes = in ? (uint32_t)a.work[2 * threadIdx.x] : 0, my_holes = in ? (uint32_t)a.work[2 * threadIdx.x + 1] : 0;
-  const uint32_t goes = sum_of(my_goes, part), holes = sum_of(my_holes, part);
-  uint32_t g0 = sum_of(lower ? my_goes : 0, part), h0 = sum_of(lower ? my_holes : 0, part);
+  __shared__ uint16_t counts[2][kAtOnce][kScan / 64];
+  uint32_t goes, holes;
+  uint32_t g0 = chunks_before(a.work, 2, 0, &goes, part), h0 = chunks_before(a.work, 2, 1, &holes, part);
   const bool done = goes <= holes;
   const int most = min(a.keep, g.n_blocks - a.keep);
   // what is left of the outputs
@@ -358,18 +404,29 @@ __global__ __launch_bounds__(kScan) void compact_place(Geo g, CompactArgs a) {
     a.pool_out[1] = done ? (int)(holes - goes) : 0;
   }
   if (!done) return;
-  for (int b0 = c.first; b0 < c.last; b0 += kScan) {
-    const int b = b0 + (int)threadIdx.x;
-    const bool used = b < c.last && a.ids[b] == kUsed, idle = b < c.last && !used;
-    const uint32_t go = used && b >= a.keep, hole = idle && b < a.keep;
-    uint32_t total;
-    const uint32_t i = g0 + before(go, &total, part);
-    g0 += total;
-    const uint32_t j = h0 + before(hole, &total, part);
-    h0 += total;
-    if (go) a.from[i] = b, a.ids[b] = (int)i;
-    if (hole && j < goes) a.to[j] = b, a.ids[b] = kTaken - (int)j;
-    if (hole && j >= goes) a.ring_out[j - goes] = b;
+  Picked go{counts[0], part}, hole{counts[1], part};
+  for (int b0 = c.first; b0 < c.last; b0 += kAtOnce * kScan) {
+    bool goes_b[kAtOnce], hole_b[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int b = b0 + k * kScan + (int)threadIdx.x;
+      const bool used = a.ids[min(b, c.last - 1)] == kUsed;
+      goes_b[k] = used && b < c.last && b >= a.keep;
+      hole_b[k] = !used && b < c.last && b < a.keep;
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) go.count(k, goes_b[k]), hole.count(k, hole_b[k]);
+    const uint32_t n_go = go.scan(kAtOnce), n_hole = hole.scan(kAtOnce);
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int b = b0 + k * kScan + (int)threadIdx.x;
+      const uint32_t i = g0 + go.place(k, goes_b[k]), j = h0 + hole.place(k, hole_b[k]);
+      if (goes_b[k]) a.from[i] = b, a.ids[b] = (int)i;
+      if (hole_b[k] && j < goes) a.to[j] = b, a.ids[b] = kTaken - (int)j;
+      if (hole_b[k] && j >= goes) a.ring_out[j - goes] = b;
+    }
+    g0 += n_go, h0 += n_hole;
+    __syncthreads();
   }
 }
 
@@ -440,23 +497,24 @@ __global__ __launch_bounds__(kScan) void compact_one(Geo g, CompactArgs a) {
     if (hole && j >= n_goes) a.ring_out[j - n_goes] = b;
   }
   __syncthreads();
-  // counts by new id: those that stay, those that come, 0 for what is free
-  for (int b = threadIdx.x; b < a.keep; b += kScan)
-    if (state[b] == kIn) a.shared_out[b] = a.shared_in[b];
-  for (int b = a.keep + (int)threadIdx.x; b < g.n_blocks; b += kScan)
-    if (state[b] < kOut) a.shared_out[hole_id[state[b]]] = a.shared_in[b];
+  // counts by new id: of what stays, and of what comes; 0 for what is free
+  for (int b0 = threadIdx.x; b0 < g.n_blocks; b0 += 8 * kScan) {
+    int n[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) n[u] = a.shared_in[min(b0 + u * kScan, g.n_blocks - 1)];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int b = b0 + u * kScan;
+      if (b >= g.n_blocks) break;
+      if (b < a.keep ? state[b] == kIn : state[b] < kOut) a.shared_out[b < a.keep ? b : hole_id[state[b]]] = n[u];
+    }
+  }
   for (uint32_t j = n_goes + threadIdx.x; j < n_holes; j += kScan) a.shared_out[hole_id[j]] = 0;
-  each_row(
-      a.n_rows, [&](int r) { return a.len[r] > 0; },
-      [&](int r, int lane) {
-        int32_t* mine = a.table + (int64_t)r * g.width;
-        const int have = held(g, a.len[r]);
-#pragma unroll 4
-        for (int j = lane; j < have; j += 64) {
-          const int id = mine[j];
-          // (a free block, which no row should hold, stays as it is)
-          if (id >= a.keep && id < g.n_blocks && state[id] < kOut) mine[j] = hole_id[state[id]];
-        }
+  each_entry(
+      g, a.table, a.n_rows, [&](int r) { return held(g, a.len[r]); },
+      [&](unsigned at, int id) {
+        // (a free block, which no row should hold, stays as it is)
+        if (id >= a.keep && state[id] < kOut) a.table[at] = hole_id[state[id]];
       });
 }
 
@@ -498,7 +556,7 @@ unsigned groups_of(int64_t n, int threads) { return (unsigned)std::max<int64_t>(
 
 hipError_t launch_fork(const Geo& g, const ForkArgs& a, hipStream_t s) {
   // (a workgroup goes through the forks' entries in steps of 1,024)
-  if (g.n_blocks <= kOneBlocks && a.n_forks <= kScan && (int64_t)a.n_forks * g.width <= kOneEntries / 2) {
+  if (g.n_blocks <= kOneBlocks && a.n_forks <= kScan && (int64_t)a.n_forks * g.width <= kOneEntries) {
     hipLaunchKernelGGL(fork_one, dim3(1), dim3(kScan), 0, s, g, a);
     return hipGetLastError();
   }
@@ -512,7 +570,7 @@ hipError_t launch_fork(const Geo& g, const ForkArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_release(const Geo& g, const ReleaseArgs& a, hipStream_t s) {
-  if (g.n_blocks <= kOneBlocks && (int64_t)a.n_rows * g.width <= 2 * kOneEntries) {
+  if (g.n_blocks <= kOneBlocks && (int64_t)a.n_rows * g.width <= kOneEntries) {
     hipLaunchKernelGGL(release_one, dim3(1), dim3(kScan), 0, s, g, a);
     return hipGetLastError();
   }
