@@ -1,7 +1,7 @@
 """Plan a window, then serve the activations that the best plan gives to one
-device, with continuous batching over the paged 4-bit cache:
+device, with continuous batching over the paged cache, in 4 or 8 bits:
 
-    python examples/serve_activations.py [--rows 16] [--layers 4] [--blocks 160]
+    python examples/serve_activations.py [--rows 16] [--layers 4] [--blocks 160] [--codes e2m1|e4m3]
 
 The scheduler scores the window's plans on the GPU and picks the best; the
 activations of its device 0 become requests, in the order of their predicted
@@ -26,9 +26,9 @@ class Replica:
     """A batch of `rows` requests on one GPU: their lengths, blocks and caches."""
 
     def __init__(self, *, rows=16, layers=4, q_heads=16, kv_heads=8, head_dim=128, block=16, blocks=160, row_blocks=64,
-                 vocabulary=997, rot_dim=None, window=0, dtype="bf16", device=0, seed=0):
+                 vocabulary=997, rot_dim=None, window=0, dtype="bf16", codes="e2m1", device=0, seed=0):
         self.ctx = wf.KVContext(device, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, block_tokens=block,
-                                n_blocks=blocks, max_blocks=row_blocks, dtype=dtype)
+                                n_blocks=blocks, max_blocks=row_blocks, dtype=dtype, codes=codes)
         at, width, i32 = f"cuda:{device}", q_heads * head_dim, torch.int32
         self.rows, self.window, self.rot = rows, window, head_dim if rot_dim is None else rot_dim
         self.lens = torch.zeros(rows, dtype=i32, device=at)
@@ -141,9 +141,10 @@ def main():
     p.add_argument("--rows", type=int, default=16)
     p.add_argument("--layers", type=int, default=4)
     p.add_argument("--blocks", type=int, default=160)
+    p.add_argument("--codes", choices=("e2m1", "e4m3"), default="e2m1")
     a = p.parse_args()
     activations = granted_activations()
-    replica = Replica(rows=a.rows, layers=a.layers, blocks=a.blocks)
+    replica = Replica(rows=a.rows, layers=a.layers, blocks=a.blocks, codes=a.codes)
     requests = requests_of(activations, replica.embed.shape[0], np.random.default_rng(0))
     t0 = time.perf_counter()
     answers = serve(replica, requests)

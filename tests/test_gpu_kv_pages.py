@@ -397,3 +397,86 @@ def test_rows_that_share_are_served_as_if_they_did_not(codes):
     assert one.pool[1].item() == keep and sorted(one.ring.tolist()) == list(range(keep)) and not one.shared.any()
     one.ctx.close()
     own.ctx.close()
+
+
+def test_both_ways_of_a_call_agree():
+    """The native binding and the longer way give the same, and the longer way takes what the other leaves."""
+    rng = np.random.default_rng(12)
+    rows, width, b = 30, 6, 16
+    lens, pool, ring, table, shared = state_of(rng, rows, b, width, spare=20)
+    n = len(ring)
+    with ctx_of(n, width, b, "e4m3") as ctx:
+        assert ctx._bind is not None, "_kvbind is not built"
+        bind = ctx._bind
+        f = i32([[int(np.nonzero(lens)[0][0]), int(d), 33] for d in np.nonzero(lens == 0)[0][:4]])
+        ends = (rng.random(rows) < 0.3).astype(np.uint8)
+        data = torch.randint(0, 256, (ctx.cache_bytes,), device=DEV).to(torch.uint8)
+        results = []
+        for way in (bind, None):
+            ctx._bind = way
+            t, r, c = dev(table), dev(ring), data.clone()
+            fork = pkg.kv_fork(ctx, *(dev(f[:, i]) for i in range(3)), dev(lens), dev(pool), r, t, dev(shared))
+            assert pkg.kv_copy(ctx, c, fork[4]) is None
+            out = pkg.kv_release(ctx, dev(ends), fork[0], fork[1], r, t, fork[2])
+            used = n - int(out[1][1])
+            more = pkg.kv_compact(ctx, max(used, 1), out[0], out[1], r, t, out[2])
+            pkg.kv_copy(ctx, c, more[4])
+            results.append([*fork, *out, *more, t, r, c])
+        ctx._bind = bind
+        for x, y in zip(*results):
+            assert x.dtype == y.dtype and x.shape == y.shape and torch.equal(x, y)
+        # addresses, which only the longer way takes
+        t, c = dev(table), data.clone()
+        again = pkg.kv_fork(ctx, *(dev(f[:, i]) for i in range(3)), dev(lens), dev(pool), dev(ring), t.data_ptr(), dev(shared))
+        pkg.kv_copy(ctx, c.data_ptr(), again[4])
+        for x, y in zip(again, results[0][:5]):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_calls_on_a_given_stream(handle):
+    """stream= takes the work in order with what is queued there, and owns the outputs."""
+    rng = np.random.default_rng(13)
+    rows, width, b = 40, 5, 16
+    lens, pool, ring, table, shared = state_of(rng, rows, b, width, spare=20)
+    with ctx_of(len(ring), width, b) as ctx:
+        side = torch.cuda.Stream()
+        given = side.cuda_stream if handle else side
+        src = dev(i32([int(np.argmax(lens))])), dev(i32([int(np.nonzero(lens == 0)[0][0])])), dev(i32([21]))
+        args = [dev(x) for x in (lens, pool, ring, table, shared)]
+        cache = torch.randint(0, 256, (ctx.cache_bytes,), device=DEV).to(torch.uint8)
+        ends = torch.zeros(rows, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            big = torch.randn(4096, 4096, device=DEV)
+            for _ in range(20):
+                big = big @ big * 1e-2
+            ends[3] = 1                                      # behind the products, on the same stream
+        want = E.fork([tuple(int(x) for x in (src[0][0], src[1][0], 21))], lens, pool, ring, table, shared, b)
+        out = pkg.kv_fork(ctx, *src, *args, stream=given)
+        pkg.kv_copy(ctx, cache, out[4], stream=given)
+        after = pkg.kv_release(ctx, ends, out[0], out[1], args[2], args[3], out[2], stream=given)
+        side.synchronize()
+        same(dict(zip(("lens", "pool", "shared", "granted", "moves"), out), table=args[3]), want)
+        flags = np.zeros(rows, np.uint8)
+        flags[3] = 1
+        same(dict(zip(("lens", "pool", "shared"), after), ring=args[2]), E.release(flags, want["lens"], want["pool"], ring, want["table"], want["shared"], b))
+
+
+@pytest.mark.parametrize("codes", ["e2m1", "e4m3"])
+def test_the_example_serves_with_either_codes(codes):
+    """The serving example ends all requests; with 8 bits each step attends to what is stored."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_activations.py")
+    spec = importlib.util.spec_from_file_location("serve_activations", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    replica = example.Replica(rows=4, layers=2, q_heads=8, kv_heads=2, head_dim=64, blocks=30, row_blocks=8, codes=codes)
+    assert replica.ctx.codes == codes
+    rng = np.random.default_rng(3)
+    jobs = [(rng.integers(0, 997, int(rng.integers(1, 90))).tolist(), int(rng.integers(1, 8))) for _ in range(9)]
+    answers = example.serve(replica, jobs, chunk=40)
+    assert [len(a) for a in answers] == [count for _, count in jobs]
+    assert replica.pool[1].item() == 30 and sorted(replica.ring.tolist()) == list(range(30))
+    replica.close()
