@@ -222,6 +222,34 @@ def test_invalid_device_values_stay_in_bounds():
             assert (cache == 3).all()
 
 
+def test_invalid_device_values_in_a_larger_cache():
+    """The same where every phase is a kernel of its own: more blocks and entries than one workgroup takes."""
+    rows, b, width, n, keep = 70, 16, 600, 40_000, 17_000
+    rng = np.random.default_rng(6)
+    guards = []
+
+    def guarded(k, low=-2 ** 31, high=2 ** 31 - 1):
+        g = torch.full((64 + k + 64,), 77, dtype=torch.int32, device=DEV)
+        g[64:-64] = dev(rng.integers(low, high, k).astype(np.int32))
+        guards.append(g)
+        return g[64:-64]
+    with ctx_of(n, width, b) as ctx:
+        moves = min(keep, n - keep)
+        for pool in ([-5, 10 ** 9], [10 ** 9, -3], [7, n]):
+            # ids of anything, and ids of the cache that come several times
+            for low, high in ((-2 ** 31, 2 ** 31 - 1), (-2, n + 2)):
+                p, table, ring, work = dev(i32(pool)), guarded(rows * width, low, high), guarded(n, low, high), guarded(1024)
+                flags, lens = torch.ones(rows, dtype=torch.uint8, device=DEV), guarded(rows, -2 ** 31, 2 * width * b)
+                ctx.wf_kv_fork(guarded(rows, -2, rows + 2), guarded(rows, -2, rows + 2), guarded(rows, -9, 2 ** 31 - 1), rows, rows, lens,
+                               guarded(rows), p, guarded(2), ring, table, guarded(n, -3, 3), guarded(n), guarded(rows), guarded(rows), flags, work)
+                ctx.wf_kv_release(flags, rows, lens, guarded(rows), p, guarded(2), ring, table, guarded(n, -3, 3), guarded(n), work)
+                ctx.wf_kv_compact(keep, rows, lens, p, guarded(2), ring, guarded(keep), table, guarded(n), guarded(keep), guarded(moves),
+                                  guarded(moves), guarded(1), guarded(n), work)
+        torch.cuda.synchronize()
+        for g in guards:
+            assert (g[:64] == 77).all() and (g[-64:] == 77).all()
+
+
 def test_refusals():
     n, width, rows = 10, 4, 3
     z = lambda k, t=torch.int32: torch.zeros(k, dtype=t, device=DEV)
