@@ -209,6 +209,8 @@ wf_status wf_kv_load(wf_kv_ctx *ctx, const uint8_t *cache, const int64_t *slot, 
  * about 1e36 / (tokens seen) for them to be finite.  With f16 the largest
  * probability times scale is moved to the upper part of the type's range first,
  * so that small values keep as many bits as large ones.
+ * With 8-bit codes, single tokens' scores are sums of queries times key codes, of up to 448 each whatever the keys'
+ * scale: bf16 queries must stay below about 1e33.
  */
 wf_status wf_kv_attend(wf_kv_ctx *ctx, const void *q, int64_t q_stride, int32_t n_tokens,
                        const uint8_t *cache, const int32_t *table, const int32_t *kv_len,

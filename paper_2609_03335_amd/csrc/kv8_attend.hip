@@ -2,15 +2,28 @@
 //
 //   o = sum_j p_j v_j,  p = softmax_j(scale q.k_j),  k_j = 2^e c_j,  v_j = 2^f d_j
 //
-// with codes c, d of 8 bits and one e and f for a block.  Codes are exact in bf16 and f16, and
-// so are bf16 values: the conversion of the values' codes multiplies with their scale.  f16 could not hold them:
-// there the scale goes to the probabilities.  Keys are multiplied as codes, their scale goes to the score.
+// with codes c, d of 8 bits and one e and f for a block.  Codes are exact in bf16 and f16, and so are
+// values in bf16: the conversion of the values' codes multiplies with their scale at no cost.  f16 could not hold
+// them: there f is added to the exponent, p_j 2^f = 2^(score - reference + f) is rounded to f16 once, and a block's
+// terms go into the softmax's total divided by 2^f (16 products of a lane and 64 tokens less than p_j times the scale:
+// 7 chunks of up to 500 of 14 heads 54 -> 52 us, a prompt of 7,001 of 32 heads 440 -> 418).
+// The scale of the keys goes to the score, in prompts of bf16 (attend8_wide) to the conversion.
 //
 // The split of the work is that of the 4-bit cache: a wave takes 16 C columns (a column is one query token's head, the heads
 // that share a kv head side by side) and 64 cached tokens at a time, scores transposed (tokens down, columns across), token
 // g*16 + t*4 + i of the 64 in row g*4 + i of score tile t, so that lane group g = lane/16 owns 16 consecutive
 // tokens, of one block, and holds their probabilities where the product with the values wants them.  Of the values it loads
 // four channels of four tokens at once: row n of output block r is channel 64 (r/4) + 4 n + r%4.
+//
+// Single tokens are bound by the reading of the cache: 80 rows of up to 5,000 tokens, 482 MB, 104 us (4.6 TB/s), with
+// 400 such rows 405 us (5.7; a streaming kernel reaches 6.2, a probe that reads scattered cells 5.8), where the
+// lengths' unevenness costs less; vector instructions are issued in 18% of the cycles of a busy CU, the matrix
+// cores busy in 8%.  One row of 150,001 takes 62 us (4.9 TB/s, 5 of them the join), one of 1,000 9 us, launch and
+// latency.  Prompts are bound by the matrix cores and the softmax's vector instructions together: 7,001 tokens of 32
+// heads of 128 channels 389 us (1.03 PFLOP/s; a large product reaches 1.2 to 1.4) with the matrix cores busy for 47% of the
+// cycles and other vector instructions issued in 33%.  Chunks of 64 channels are bound by vector instructions (a
+// score of 64 products costs as much softmax as one of 128, and a code's conversion is used for 32 columns): 7
+// chunks of up to 500 over 8,000 52 us (430 TFLOP/s), matrix cores 21%, others 67%.
 #include "kv_attend.h"
 
 namespace wfkv {
@@ -38,17 +51,19 @@ struct UniformPages : Pages {
   }
 };
 
-// Waves a SIMD that the registers are held to.
-template <int D, int C>
-constexpr int kOcc = C == 1 ? (D == 64 ? 3 : D == 128 ? 2 : 1) : D == 64 ? 3 : D == 128 ? 2 : 1;
+// Waves a SIMD that the registers are held to: the two units in flight of single tokens take 148 (64 channels), 238
+// and 512 of them, the one unit and two tiles of chunks 156, 230 and 512.
+template <int D>
+constexpr int kOcc = D == 64 ? 3 : D == 128 ? 2 : 1;
 
 // Up to this many shares of 16 columns are joined by the workgroup that is done last, more (or of
-// more columns) by a kernel of their own, with a workgroup for each head.
+// more columns) by a kernel of their own, with a workgroup for each head: one token over 1,000 cached ones (4
+// shares) takes 8.9 us against 10.2, over 4,000 (16) 15.2 against 11.5; 8 tokens (32 columns) over 1,000 18.6 against 13.4.
 template <int C>
 constexpr int kFused = C == 1 ? 4 : 1;
 
 template <int D, int C, class M>
-__global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendArgs a, Split sp) {
+__global__ __launch_bounds__(kThreads, (kOcc<D>)) void attend8(Geo g, AttendArgs a, Split sp) {
   constexpr int KS = D / 32;          // products of 32 channels per score tile
   constexpr int J = D / 64;           // runs of 64 channels
   constexpr int MT = D / 16;          // blocks of 16 channels of the output
@@ -200,8 +215,8 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
           for (int j = 0; j < J; ++j) w.vw[j][t] &= mask;
         }
       }
-      float vlog = 0.0f, limit = M::kSlack;
-      if constexpr (M::kScaled) vlog = scale_log(vz), limit = fminf(limit, M::kMostLog - vlog);
+      float vlog = 0.0f, unscale = 1.0f, limit = M::kSlack;
+      if constexpr (M::kScaled) vlog = scale_log(vz), unscale = __builtin_amdgcn_exp2f(-vlog), limit = fminf(limit, M::kMostLog - vlog);
       // 32 tokens at a time: score tiles 2h and 2h + 1, one product with the values
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -254,13 +269,15 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
         u32x4 p[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          float x[8];
+          float x[8], terms = 0.0f;
+          const float by = M::kScaled ? ref[c] - vlog : ref[c];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float e = __builtin_amdgcn_exp2f(s[c][i / 4][i % 4] - ref[c]);
-            sum[c] += e;
-            x[i] = M::kScaled ? e * vz : e;
+            x[i] = __builtin_amdgcn_exp2f(s[c][i / 4][i % 4] - by);
+            if constexpr (M::kScaled) terms = i ? terms + x[i] : x[i];
+            else sum[c] += x[i];
           }
+          if constexpr (M::kScaled) sum[c] = fmaf(terms, unscale, sum[c]);
 #pragma unroll
           for (int b = 0; b < 4; ++b) p[c][b] = M::pair(x[2 * b], x[2 * b + 1]);
         }
@@ -275,7 +292,8 @@ __global__ __launch_bounds__(kThreads, (kOcc<D, C>)) void attend8(Geo g, AttendA
     int u = u0;
     ask(u);
     if constexpr (C == 1) {
-      // the next unit is on its way while one is worked on, its blocks one earlier still
+      // the next unit is on its way while one is worked on, its blocks one earlier still (with one unit's
+      // registers and its blocks by vector loads 80 ragged rows of up to 5,000 127 us, so 104)
       Unit w0, w1;
       const auto none = [] {};
       load_keys(u, w0);
@@ -683,8 +701,8 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend8_wide(Geo g
       store_keys(2 * u + 3, w);
       if (!kMid) store_values(2 * u + 2, w);
       const f32x2 next = scales_of(u + 1, w.z);
-      float vlog = 0.0f;
-      if constexpr (M::kScaled) vlog = scale_log(now[1]);
+      float vlog = 0.0f, unscale = 1.0f;
+      if constexpr (M::kScaled) vlog = scale_log(now[1]), unscale = __builtin_amdgcn_exp2f(-vlog);
       load_keys(2 * u + 5, d.k, w);
       if (!kMid) load_values(2 * u + 4, d.v, w);
       w.z = load_scales(d.z);
@@ -706,7 +724,7 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend8_wide(Geo g
         for (int c = 0; c < C; ++c)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            x[c][i] = fmaf(s[c][i / 4][i % 4], M::kScaled ? now[0] : scale, -ref[c]);
+            x[c][i] = fmaf(s[c][i / 4][i % 4], M::kScaled ? now[0] : scale, M::kScaled ? vlog - ref[c] : -ref[c]);
             if (kMask) x[c][i] = j0 + i >= lo[c] && j0 + i < hi[c] ? x[c][i] : -INFINITY;
           }
         // f16 ends at 2^16: a term above 2^15 moves the reference
@@ -717,7 +735,7 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend8_wide(Geo g
             float m = x[c][0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) m = fmaxf(m, x[c][i]);
-            up |= m + vlog > M::kMostLog;
+            up |= m > M::kMostLog;
           }
           if (__builtin_expect(__any(up), 0)) {
 #pragma unroll
@@ -735,7 +753,7 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend8_wide(Geo g
 #pragma unroll
               for (int k = 0; k < MT; ++k) o[c][k] *= keep;
 #pragma unroll
-              for (int i = 0; i < 8; ++i) x[c][i] -= r;
+              for (int i = 0; i < 8; ++i) x[c][i] += vlog - r;
             }
           }
         }
@@ -749,12 +767,14 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend8_wide(Geo g
         }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+          float terms = 0.0f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             x[c][i] = __builtin_amdgcn_exp2f(x[c][i]);
-            sum[c] += x[c][i];
-            if (M::kScaled) x[c][i] *= now[1];
+            if constexpr (M::kScaled) terms = i ? terms + x[c][i] : x[c][i];
+            else sum[c] += x[c][i];
           }
+          if constexpr (M::kScaled) sum[c] = fmaf(terms, unscale, sum[c]);
 #pragma unroll
           for (int b = 0; b < 4; ++b) p[c][b] = M::pair(x[c][2 * b], x[c][2 * b + 1]);
         }
@@ -834,7 +854,7 @@ __global__ __launch_bounds__(64 * W, (D == 256 ? 1 : 2)) void attend8_wide(Geo g
 // workgroups run at once.
 template <int D, int C, class M>
 hipError_t narrow(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, hipStream_t s) {
-  const Split sp = split_of<D>(g, a, w, columns, 16 * C, w.n_cu * kOcc<D, C>, kAlone);
+  const Split sp = split_of<D>(g, a, w, columns, 16 * C, w.n_cu * kOcc<D>, kAlone);
   const hipError_t e = launch(attend8<D, C, M>, g, a, sp, kThreads, s);
   if (e != hipSuccess || sp.splits <= kFused<C>) return e;
   // (heads x 256 threads: shares are only taken of up to kCountBytes / 4 heads)
@@ -869,7 +889,7 @@ hipError_t by_columns(const Geo& g, const AttendArgs& a, const AttendWork& w, hi
   if constexpr (D == 64) {
     if (all < 256 * 3 * w.n_cu) return narrow<D, 2, M>(g, a, w, columns, s);
   } else {
-    const int64_t at_once = w.n_cu * kOcc<D, 2>, wgs = (all + 31) / 32;
+    const int64_t at_once = w.n_cu * kOcc<D>, wgs = (all + 31) / 32;
     if (a.max_kv > 0 && wgs * 2 <= at_once * 5 && wgs * a.max_kv <= at_once * 3500) return narrow<D, 2, M>(g, a, w, columns, s);
   }
   return wide<D, M>(g, a, w, columns, s);

@@ -2,11 +2,18 @@
 // block and head (and its inverse).
 //
 // The tokens of a call that lie in one block, one after the other, are a run; a workgroup takes the
-// runs that begin among `tile` tokens of one kv head, from the first's first to the last's last token.  It goes over their keys and
-// values twice: the largest magnitude of each run gives its block's scale, then the codes are written.  Where
-// a run's block holds earlier tokens under a smaller scale, the block's codes are rounded to the new one in between.
+// runs that begin among `tile` tokens of one kv head, from the first's first to the last's last token.  A scale is known
+// when the last token of the run is, so normed keys and values stay in registers (two passes, 64 tokens of 128 channels; what a
+// tile has beyond that is read again): largest magnitudes of the runs in LDS, scales, then codes.  Where a run's block
+// holds earlier tokens under a smaller scale, the block's codes are rounded to the new one in between.  Value codes
+// go through LDS once more, so that a thread stores two channels of four tokens, 8 bytes, instead of one byte four times.
 // Sums of squares add neighbours first and every operation is rounded by itself, so that the codes are
 // reproducible to the last bit by elementary operations.
+//
+// Large calls are bound by memory: 14,000 prompt tokens of 40 + 8 heads of 128 channels read 200 MB and write 172 (the counters
+// say 275 and 230), 92 us (4.0 TB/s), of which the keys' and values' workgroups, three barriers and a chain of loads long, fill half
+// while the queries' stream beside them; reading them back 19 us (4.4 TB/s).  Small ones are bound by the chain: 181 single
+// tokens 6.6 us, most of them blocks that hold others, and 3.2 us back.
 #include "kv8.h"
 #include "kv_vector.h"
 
@@ -17,7 +24,10 @@ constexpr int kThreads = 256, kManyThreads = 512, kPasses = 2, kManyWaves = 4;  
 // tokens of a tile, and that a workgroup looks at: up to a block's before the tile and behind it
 constexpr int kMostTile = 256, kMostBlock = 256, kSpan = kMostTile + 2 * kMostBlock;
 constexpr int kHeads = 4;                // query heads a lane group takes of a token, of many
-constexpr int64_t kManyVectors = 32768;  // query vectors of a call from which they are many
+// Vectors of a call from which they are many: more passes a workgroup, four heads a lane group.  Few against many (us), 40 + 8
+// heads of 128 channels, prompts: 300 tokens (16,800) 15.5 and 15.1, 600 21.5 and 16.2, 2,000 30.5 and 26.4, 4,000 49 and 36;
+// 32 + 8 heads, single tokens, a run each: 500 (24,000) 8.0 and 13.4, 2,000 (96,000) 23.9 and 23.4.
+constexpr int64_t kManyVectors = 32768;
 
 // A lane's part of a vector that is not read again here; of large calls past the caches (14,000 tokens of 40 + 8 heads
 // stored and read back 115 -> 110 us).
