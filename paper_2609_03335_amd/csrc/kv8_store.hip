@@ -11,9 +11,9 @@
 // reproducible to the last bit by elementary operations.
 //
 // Large calls are bound by memory: 14,000 prompt tokens of 40 + 8 heads of 128 channels read 200 MB and write 172 (the counters
-// say 275 and 230), 92 us (4.0 TB/s), of which the keys' and values' workgroups, three barriers and a chain of loads long, fill half
+// say 265, rotations over again, and 172), 86 us (4.3 TB/s), of which the keys' and values' workgroups, three barriers and a chain of loads long, fill half
 // while the queries' stream beside them; reading them back 19 us (4.4 TB/s).  Small ones are bound by the chain: 181 single
-// tokens 6.6 us, most of them blocks that hold others, and 3.2 us back.
+// tokens 6.1 us, most of them blocks that hold others, and 3.2 us back.
 #include "kv8.h"
 #include "kv_vector.h"
 
@@ -128,8 +128,11 @@ struct Span {
 template <int D, class T, int P, int W>
 __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, unsigned item, int tile, Span& sp, uint8_t (&codes_of_pass)[P][8 * W]) {
   constexpr int L = D / 8, V = W / L, E = (kSpan + W - 1) / W;
-  const int kvh = (int)(item % (unsigned)g.hk), lane = threadIdx.x % L, group = threadIdx.x / L;
-  if (threadIdx.x == 0) sp.ups = 0, sp.first = kSpan, sp.end = 0;
+  // (opaque, so that what follows from it is worked out here and not kept in registers, or scratch, across items: 110 -> 103 us)
+  unsigned tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int kvh = (int)(item % (unsigned)g.hk), lane = (int)(tid % L), group = (int)(tid / L);
+  if (tid == 0) sp.ups = 0, sp.first = kSpan, sp.end = 0;
   const int64_t none = -1;
   auto valid = [&](int64_t s) { return s >= 0 && s >> g.b_log2 < g.n_blocks ? s : none; };
   // A tile begins where the block of its first token begins, if that is in this call: runs of whole blocks
@@ -169,9 +172,9 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
   uint64_t events[E], owned[E];
 #pragma unroll
   for (int p = 0; p < E; ++p) {
-    const int i = p * W + (int)threadIdx.x;
+    const int i = p * W + (int)tid;
     events[p] = owned[p] = 0;
-    if (i - (int)(threadIdx.x & 63) >= kSpan) continue;
+    if (i - (int)(tid & 63) >= kSpan) continue;
     bool event = true, mine = false;
     if (i < span) {
       const int64_t s = slot_at(i), before = t0 + i > 0 ? slot_at(i - 1) : none;
@@ -183,7 +186,7 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
     }
     events[p] = __ballot(event);
     owned[p] = __ballot(mine);
-    if ((threadIdx.x & 63) == 0) {
+    if ((tid & 63) == 0) {
       const int at = 63 - __clzll((long long)events[p]);
       sp.last_event[i >> 6] = events[p] == 0 ? -2 : owned[p] >> at & 1 ? i + at : -1;
     }
@@ -191,9 +194,9 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
   __syncthreads();
 #pragma unroll
   for (int p = 0; p < E; ++p) {
-    const int i = p * W + (int)threadIdx.x;
+    const int i = p * W + (int)tid;
     if (i >= span) continue;
-    const uint64_t upto = events[p] & (~0ull >> (63 - (threadIdx.x & 63)));
+    const uint64_t upto = events[p] & (~0ull >> (63 - (tid & 63)));
     int lead = -1;
     if (upto) {
       const int at = 63 - __clzll((long long)upto);
@@ -206,7 +209,7 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
     sp.lead[i] = lead;
     if (lead >= 0 && (sp.slot[i] & (g.b - 1)) == 0) sp.begins[lead] = 1;
     const uint64_t mine = __ballot(lead >= 0);
-    if (mine && (threadIdx.x & 63) == 0) {  // (lane 0 of a wave that has tokens of the span is in it)
+    if (mine && (tid & 63) == 0) {  // (lane 0 of a wave that has tokens of the span is in it)
       atomicMin(&sp.first, i + __ffsll((unsigned long long)mine) - 1);
       atomicMax(&sp.end, i + 64 - __clzll((long long)mine));
     }
@@ -240,7 +243,7 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
   }
   __syncthreads();
   // where tokens lie, and whether they and the next three are four of a word, by a thread each
-  for (int i = first + (int)threadIdx.x; i < end; i += W) {
+  for (int i = first + (int)tid; i < end; i += W) {
     const int64_t s = sp.slot[i];
     const int lead = sp.lead[i];
     sp.cell[i] = ((s >> g.b_log2) * g.hk + kvh) * (int64_t)g.cell;
@@ -250,7 +253,7 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
   }
   auto cell_of = [&](int i) { return a.cache + sp.cell[i]; };
   const int codes = 2 * g.b * D;  // bytes of them, then the scales
-  for (int i = first + (int)threadIdx.x; i < end; i += W) {
+  for (int i = first + (int)tid; i < end; i += W) {
     if (sp.lead[i] != i) continue;
     float* scales = reinterpret_cast<float*>(cell_of(i) + codes);
     int rise[2] = {0, 0};
@@ -275,7 +278,7 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
   const int ups = sp.ups;
   for (int n = 0; n < ups; ++n) {
     uint4* cell = reinterpret_cast<uint4*>(cell_of(sp.up[n][0]));
-    for (int x = threadIdx.x; x < codes / 16; x += W) {
+    for (int x = (int)tid; x < codes / 16; x += W) {
       const int rise = sp.up[n][x < codes / 32 ? 1 : 2];
       if (rise == 0) continue;
       const float by = two_to(max(rise, -40));
@@ -322,7 +325,7 @@ __device__ __forceinline__ void keys_values(const Geo& g, const StoreArgs& a, un
     const int i = p * V + group;
     const int off = i >= first && i < end ? sp.off[i] : -1;
     if (off >= 0) reinterpret_cast<uint2*>(cell_of(i) + off * D)[lane] = kc;
-    const int q = (int)threadIdx.x / (D / 2), ch = (int)threadIdx.x % (D / 2) * 2, i0 = p * V + q * 4;
+    const int q = (int)(tid / (D / 2)), ch = (int)(tid % (D / 2)) * 2, i0 = p * V + q * 4;
     uint32_t two[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) two[t] = *reinterpret_cast<const uint16_t*>(bytes + (q * 4 + t) * D + ch);
@@ -466,7 +469,10 @@ struct Store8 {
       const dim3 grid(part.item_blocks + streams);
       // (items of more passes, which would be a tail, all first: blocks of 256 tokens 98 us against 153; of 64 100 against 96)
       const bool shared_out = many && part.tile == kPasses * kManyThreads / (int)L;
-      part.every = part.item_blocks && shared_out ? grid.x / part.item_blocks : 1;
+      // (an odd number: workgroups go to the eight dies in turn, and all are to have their share of these; 28 + 4 heads, every 3rd
+      // for every 4th: 84 -> 65 us.  The heads of a tile on one die, where they find its rotations, read 220 MB for 265,
+      // and took 104 us for 103.)
+      part.every = part.item_blocks && shared_out ? (grid.x / part.item_blocks - 1) | 1 : 1;
       if (many) hipLaunchKernelGGL((store8<D, T, true>), grid, dim3(threads), 0, s, g, a, part);
       else hipLaunchKernelGGL((store8<D, T, false>), grid, dim3(threads), 0, s, g, a, part);
       const hipError_t e = hipGetLastError();
