@@ -51,8 +51,8 @@ struct UniformPages : Pages {
   }
 };
 
-// Waves a SIMD that the registers are held to: the two units in flight of single tokens take 148 (64 channels), 238
-// and 512 of them, the one unit and two tiles of chunks 156, 230 and 512.
+// Waves a SIMD that the registers are held to: the two units in flight of single tokens take 149 (64 channels), 237
+// and 490 of them, the one unit and two tiles of chunks 163 and 233.
 template <int D>
 constexpr int kOcc = D == 64 ? 3 : D == 128 ? 2 : 1;
 
@@ -73,8 +73,7 @@ __global__ __launch_bounds__(kThreads, (kOcc<D>)) void attend8(Geo g, AttendArgs
   __shared__ float ref_of[kWaves][16 * C], sum_of[kWaves][16 * C];
   __shared__ int last;
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // kv heads fastest (blocks of one head meet in one die's L2 where heads
   // divide the dies), then shares, then column tiles from the last (the longest under a
   // causal mask) to the first, then rows
@@ -93,6 +92,10 @@ __global__ __launch_bounds__(kThreads, (kOcc<D>)) void attend8(Geo g, AttendArgs
   const float scale = a.scale * kLog2e;
 
   for (int64_t tile = tile0; tile * 16 * C < columns; tile += sp.tiles) {
+    // (opaque, so that what follows from it is worked out here and not kept in registers across tiles)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int n = lane & 15, grp = lane >> 4;
     // this lane's columns: their query, and the tokens [lo, hi) they see
     u32x4 q[C][KS];
     int lo[C], hi[C];
@@ -877,20 +880,25 @@ template <int D, class M>
 hipError_t by_columns(const Geo& g, const AttendArgs& a, const AttendWork& w, hipStream_t s) {
   const int64_t columns = (int64_t)(a.max_q > 0 ? std::min(a.max_q, a.n_tokens) : a.n_tokens) * g.group;
   if (columns <= 16) return narrow<D, 1, M>(g, a, w, columns, s);
-  if (columns <= 128) return narrow<D, 2, M>(g, a, w, columns, s);
+  // (of 256 channels one tile fits the registers with two units in flight, and two need scratch: 80 rows of 8 tokens over
+  // up to 5,000 278 us with one tile against 348, f16 281 against 412.  A code is then converted for 16 columns, for 64 by
+  // wide workgroups: 80 rows of 40 columns 265 us narrow and 298 wide, of 64 425 and 345.)
+  constexpr int C = D == 256 ? 1 : 2;
+  if (columns <= (D == 256 ? 48 : 128)) return narrow<D, C, M>(g, a, w, columns, s);
   // Narrow workgroups convert the codes for 32 columns, wide ones for 128 or 256, but take 10 us and more to fill
   // their pipeline, and ragged rows leave CUs without one.  (The tokens of the call tell how many columns there are in all.)
   // At 64 channels, where the softmax costs more than the products, wide ones win only where there are several for
   // each CU: a prompt of 7,001 of 32 heads 280 us narrow against 256 wide, of 12 heads 110 against 132, of 2,000 of 32 heads
   // 37 against 45; 7 and 30 chunks of up to 500 over 8,000 of 14 heads (f16) 56 against 62, 171 against 226.
   // At 128 channels, narrow against wide: a prompt of 1,000 of 32 heads 29 and 38, of 2,000 70 and 65, of 4,000 199 and 136; 128
-  // tokens over 4,000 29 and 37, 256 over 4,000 43 and 42, over 16,000 102 and 84; 16 prompts of 400 119 and 74.
+  // tokens over 4,000 29 and 37, 256 over 4,000 43 and 42, over 16,000 102 and 84; 16 prompts of 400 119 and 74.  At 256: 40 tokens of 32 heads over
+  // up to 5,000 36 and 47, 8 rows of them 84 and 87; 300 tokens over 16,000 442 and 295; a prompt of 2,000 281 and 142.
   const int64_t all = (int64_t)a.n_tokens * g.hq;
   if constexpr (D == 64) {
-    if (all < 256 * 3 * w.n_cu) return narrow<D, 2, M>(g, a, w, columns, s);
+    if (all < 256 * 3 * w.n_cu) return narrow<D, C, M>(g, a, w, columns, s);
   } else {
     const int64_t at_once = w.n_cu * kOcc<D>, wgs = (all + 31) / 32;
-    if (a.max_kv > 0 && wgs * 2 <= at_once * 5 && wgs * a.max_kv <= at_once * 3500) return narrow<D, 2, M>(g, a, w, columns, s);
+    if (a.max_kv > 0 && wgs * 2 <= at_once * 5 && wgs * a.max_kv <= at_once * 3500) return narrow<D, C, M>(g, a, w, columns, s);
   }
   return wide<D, M>(g, a, w, columns, s);
 }
