@@ -20,10 +20,10 @@
 // lengths' unevenness costs less; vector instructions are issued in 18% of the cycles of a busy CU, the matrix
 // cores busy in 8%.  One row of 150,001 takes 62 us (4.9 TB/s, 5 of them the join), one of 1,000 9 us, launch and
 // latency.  Prompts are bound by the matrix cores and the softmax's vector instructions together: 7,001 tokens of 32
-// heads of 128 channels 389 us (1.03 PFLOP/s; a large product reaches 1.2 to 1.4) with the matrix cores busy for 47% of the
+// heads of 128 channels 377 to 390 us by card (1.03 to 1.06 PFLOP/s; a large product reaches 1.2 to 1.4) with the matrix cores busy for 47% of the
 // cycles and other vector instructions issued in 33%.  Chunks of 64 channels are bound by vector instructions (a
 // score of 64 products costs as much softmax as one of 128, and a code's conversion is used for 32 columns): 7
-// chunks of up to 500 over 8,000 52 us (430 TFLOP/s), matrix cores 21%, others 67%.
+// chunks of up to 500 over 8,000 52 us (430 TFLOP/s), matrix cores 23%, others 66%.
 #include "kv_attend.h"
 
 namespace wfkv {

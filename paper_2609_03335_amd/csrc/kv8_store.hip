@@ -11,9 +11,9 @@
 // reproducible to the last bit by elementary operations.
 //
 // Large calls are bound by memory: 14,000 prompt tokens of 40 + 8 heads of 128 channels read 200 MB and write 172 (the counters
-// say 265, rotations over again, and 172), 86 us (4.3 TB/s), of which the keys' and values' workgroups, three barriers and a chain of loads long, fill half
+// say 265, rotations by each die, and 172: 5.1 TB/s), 85 us, of which the keys' and values' workgroups, three barriers and a chain of loads long, fill half
 // while the queries' stream beside them; reading them back 19 us (4.4 TB/s).  Small ones are bound by the chain: 181 single
-// tokens 6.1 us, most of them blocks that hold others, and 3.2 us back.
+// tokens 6.4 us, most of them blocks that hold others, and 3.2 us back.
 #include "kv8.h"
 #include "kv_vector.h"
 
