@@ -281,7 +281,7 @@ wf_status wf_kv_compact(wf_kv_ctx *ctx, int32_t keep, int32_t n_rows, const int3
  * Copies block from[i] to block to[i], all heads, in n_layers caches `layer_stride` bytes apart (a multiple of 16, at
  * least the bytes of one; any where n_layers is 1).  Pairs with an id outside the cache (as -1) or
  * with the same one twice are left out.  No block may be `to` of two pairs, or `to` of one and `from` of another.  Codes of either
- * kind.  from, to int32 [n].
+ * kind; an 8-bit block keeps its scales, those of a fork's copy then count what the row it came from holds in it.  from, to int32 [n].
  */
 wf_status wf_kv_copy(wf_kv_ctx *ctx, uint8_t *cache, int64_t layer_stride, int32_t n_layers, const int32_t *from,
                      const int32_t *to, int32_t n, void *hip_stream);

@@ -387,6 +387,40 @@ def test_attend_few_queries_over_many_tokens(hq, hk, d, nq):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("nq", [3, 6, 7, 16])
+def test_attend_256_channels_between_single_tokens_and_prompts(nq, dtype):
+    check_attend(8, 1, 256, 16, [(2900, nq, None), (70, nq, None), (nq, nq, None), (0, 0, None)], dtype, seed=nq)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d,nq", [(8, 1, 64, 1), (8, 2, 128, 1), (8, 1, 64, 30), (4, 1, 128, 200), (1024, 16, 64, 50)])
+@pytest.mark.parametrize("scale", [-0.05, 0.0])
+def test_attend_scales_that_are_not_positive(scale, hq, hk, d, nq, dtype):
+    check_attend(hq, hk, d, 16, [(210, nq, None), (33, min(nq, 33), None)], dtype, scale=scale, seed=nq, hints=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d,nq", [(8, 1, 64, 1), (8, 1, 64, 30), (4, 1, 128, 200), (4, 1, 256, 40)])
+def test_attend_blocks_of_zeros(hq, hk, d, nq, dtype):
+    """Blocks whose values are all 0 have the least scale: their probabilities count in the total all the same."""
+    rng = np.random.default_rng(nq)
+    b, n = 16, 304
+    q, cache, table, kv, q_off, pos = attend_case(rng, hq, hk, d, b, [(n, nq, None)], dtype)
+    T = n
+    x = rng.standard_normal((2, T, hk, d)).astype(np.float32)
+    x[1, (np.arange(T) // b) % 3 > 0] = 0
+    slot = table[0, np.arange(T) // b].astype(np.int64) * b + np.arange(T) % b
+    with ctx_of(hq, hk, d, b, cache.n, table.shape[1], dtype) as ctx:
+        raw = dev(cache.bytes).view(-1)
+        k, v = dev(x[0], TYPES[dtype]), dev(x[1], TYPES[dtype])
+        pkg.kv_store(ctx, torch.zeros(T, hq, d, dtype=TYPES[dtype], device=DEV), k, v, dev(np.arange(T, dtype=np.int32)), dev(slot), raw)
+        cache.bytes = raw.cpu().numpy().reshape(cache.bytes.shape)
+        want, mag, dots, top = E.attend(host(q), cache, table, kv, q_off, pos, 0.1, 0)
+        got = host(pkg.kv_attend(ctx, q, raw, dev(table), dev(kv), dev(q_off), dev(pos), scale=0.1, max_q=nq, max_kv=n))
+    assert (np.abs(got - want) <= bound(dtype, want, mag, dots, d, n, top)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("hq,hk,d,b,nq,window", [(8, 2, 64, 16, 1, 50), (8, 2, 64, 16, 13, 50), (8, 2, 128, 32, 1, 0), (4, 1, 256, 16, 40, 33),
                                                  (8, 1, 64, 16, 150, 60), (4, 1, 128, 64, 150, 0), (4, 1, 256, 32, 150, 20),
                                                  (1024, 16, 64, 16, 110, 60)])
