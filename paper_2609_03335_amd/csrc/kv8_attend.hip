@@ -865,9 +865,11 @@ hipError_t narrow(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_
   return hipGetLastError();
 }
 
+// (256 channels: four waves, a SIMD each, of two tiles of columns: a prompt of 7,001 of 32 heads 900 us, 892 TFLOP/s, against
+// 1,328 with one; f16 1,007 against 1,380, though some of its registers go to scratch.)
 template <int D, class M>
 hipError_t wide(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, hipStream_t s) {
-  constexpr int C = D == 256 ? 1 : 2, W = D == 256 ? 4 : 8, H = kThreads / (D / 4);
+  constexpr int C = 2, W = D == 256 ? 4 : 8, H = kThreads / (D / 4);
   const Split sp = split_of<D>(g, a, w, columns, 16 * C * W, w.n_cu * 2, kWaves);
   const hipError_t e = launch(attend8_wide<D, C, W, M>, g, a, sp, 64 * W, s);
   if (e != hipSuccess || sp.splits == 1) return e;
@@ -881,8 +883,8 @@ hipError_t by_columns(const Geo& g, const AttendArgs& a, const AttendWork& w, hi
   const int64_t columns = (int64_t)(a.max_q > 0 ? std::min(a.max_q, a.n_tokens) : a.n_tokens) * g.group;
   if (columns <= 16) return narrow<D, 1, M>(g, a, w, columns, s);
   // (of 256 channels one tile fits the registers with two units in flight, and two need scratch: 80 rows of 8 tokens over
-  // up to 5,000 278 us with one tile against 348, f16 281 against 412.  A code is then converted for 16 columns, for 64 by
-  // wide workgroups: 80 rows of 40 columns 265 us narrow and 298 wide, of 64 425 and 345.)
+  // up to 5,000 278 us with one tile against 348, f16 281 against 412.  A code is then converted for 16 columns, for 128 by
+  // wide workgroups: 80 rows of 40 columns 265 us narrow and 349 wide, of 64 425 and 405, of 96 442 and 368.)
   constexpr int C = D == 256 ? 1 : 2;
   if (columns <= (D == 256 ? 48 : 128)) return narrow<D, C, M>(g, a, w, columns, s);
   // Narrow workgroups convert the codes for 32 columns, wide ones for 128 or 256, but take 10 us and more to fill
@@ -892,13 +894,14 @@ hipError_t by_columns(const Geo& g, const AttendArgs& a, const AttendWork& w, hi
   // 37 against 45; 7 and 30 chunks of up to 500 over 8,000 of 14 heads (f16) 56 against 62, 171 against 226.
   // At 128 channels, narrow against wide: a prompt of 1,000 of 32 heads 29 and 38, of 2,000 70 and 65, of 4,000 199 and 136; 128
   // tokens over 4,000 29 and 37, 256 over 4,000 43 and 42, over 16,000 102 and 84; 16 prompts of 400 119 and 74.  At 256: 40 tokens of 32 heads over
-  // up to 5,000 36 and 47, 8 rows of them 84 and 87; 300 tokens over 16,000 442 and 295; a prompt of 2,000 281 and 142.
+  // up to 5,000 36 and 55, 8 rows of them 83 and 79; 100 tokens 56 and 68, over 16,000 151 and 137; 300 over 1,000 50 and 42; a
+  // prompt of 400 41 and 30, of 1,000 108 and 49.
   const int64_t all = (int64_t)a.n_tokens * g.hq;
   if constexpr (D == 64) {
     if (all < 256 * 3 * w.n_cu) return narrow<D, C, M>(g, a, w, columns, s);
   } else {
     const int64_t at_once = w.n_cu * kOcc<D>, wgs = (all + 31) / 32;
-    if (a.max_kv > 0 && wgs * 2 <= at_once * 5 && wgs * a.max_kv <= at_once * 3500) return narrow<D, C, M>(g, a, w, columns, s);
+    if (a.max_kv > 0 && wgs * 2 <= at_once * (D == 256 ? 2 : 5) && wgs * a.max_kv <= at_once * 3500) return narrow<D, C, M>(g, a, w, columns, s);
   }
   return wide<D, M>(g, a, w, columns, s);
 }
