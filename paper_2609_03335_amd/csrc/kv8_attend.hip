@@ -870,7 +870,10 @@ hipError_t narrow(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_
 template <int D, class M>
 hipError_t wide(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, hipStream_t s) {
   constexpr int C = 2, W = D == 256 ? 4 : 8, H = kThreads / (D / 4);
-  const Split sp = split_of<D>(g, a, w, columns, 16 * C * W, w.n_cu * 2, kWaves);
+  // A CU holds one workgroup of 128 or 256 channels.  The shares of one row are alike and are to run all at once (200 tokens of 32
+  // heads of 128 over 16,000 79 us, with twice the shares 113; 400 127 and 195); of several rows, which are not, twice as many
+  // even out (8 rows of 100 tokens over up to 5,000 65 us against 83, 4 of 300 94 against 142).
+  const Split sp = split_of<D>(g, a, w, columns, 16 * C * W, w.n_cu * (D > 64 && a.n_rows == 1 ? 1 : 2), kWaves);
   const hipError_t e = launch(attend8_wide<D, C, W, M>, g, a, sp, 64 * W, s);
   if (e != hipSuccess || sp.splits == 1) return e;
   const int64_t heads = (int64_t)a.n_tokens * g.hq;
