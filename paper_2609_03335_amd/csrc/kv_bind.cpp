@@ -129,6 +129,16 @@ at::Tensor fresh(const at::Tensor& like, at::IntArrayRef shape, at::ScalarType t
   return at::empty(shape, like.options().dtype(type));
 }
 
+// A part of an array of one dimension as a tensor of its own: what narrow() and view() give, without their dispatch (a fork and
+// its copies 10.0 -> 8.9 us from Python, a compaction 10.3 -> 9.2).
+at::Tensor part(const at::Tensor& flat, int64_t from, at::IntArrayRef shape) {
+  at::Tensor out = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(flat.storage()), flat.key_set(), flat.dtype());
+  c10::TensorImpl* impl = out.unsafeGetTensorImpl();
+  impl->set_storage_offset(flat.storage_offset() + from);
+  impl->set_sizes_contiguous(shape);
+  return out;
+}
+
 // The outputs as a tuple.
 template <size_t N>
 PyObject* wrapped(const at::Tensor (&out)[N]) {
@@ -298,8 +308,8 @@ PyObject* fork(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const at::Tensor flat = fresh(*b.lens, {r + 2 + blocks + 2 * f + WF_KV_PAGES_WORK}, at::kInt);
   int32_t* base = static_cast<int32_t*>(flat.data_ptr());
   int32_t *pool = base + r, *shared = pool + 2, *moves = shared + blocks, *work = moves + 2 * f;
-  const at::Tensor out[5] = {flat.narrow(0, 0, r), flat.narrow(0, r, 2), flat.narrow(0, r + 2, blocks), fresh(*b.lens, {f}, at::kByte),
-                             flat.narrow(0, r + 2 + blocks, 2 * f).view({2, f})};
+  const at::Tensor out[5] = {part(flat, 0, {r}), part(flat, r, {2}), part(flat, r + 2, {blocks}), fresh(*b.lens, {f}, at::kByte),
+                             part(flat, r + 2 + blocks, {2, f})};
   const wf_status st = queued(g_fork, a.g->ctx, Batch::in(src), Batch::in(dst), Batch::in(tokens), (int32_t)f, (int32_t)r, Batch::in(b.lens), base,
                               Batch::in(b.pool), pool, Batch::in(b.ring), Batch::out(b.table), Batch::in(b.shared), shared, moves, moves + f,
                               (uint8_t*)data(&out[3]), work, stream);
@@ -321,7 +331,7 @@ PyObject* release(PyObject*, PyObject* const* args, Py_ssize_t n) {
   at::AutoDispatchBelowADInplaceOrView plain;
   const at::Tensor flat = fresh(*b.lens, {r + 2 + blocks + WF_KV_PAGES_WORK}, at::kInt);
   int32_t* base = static_cast<int32_t*>(flat.data_ptr());
-  const at::Tensor out[3] = {flat.narrow(0, 0, r), flat.narrow(0, r, 2), flat.narrow(0, r + 2, blocks)};
+  const at::Tensor out[3] = {part(flat, 0, {r}), part(flat, r, {2}), part(flat, r + 2, {blocks})};
   const wf_status st = queued(g_release, a.g->ctx, (const uint8_t*)data(ends), (int32_t)r, Batch::in(b.lens), base, Batch::in(b.pool), base + r,
                               Batch::out(b.ring), Batch::in(b.table), Batch::in(b.shared), base + r + 2, base + r + 2 + blocks, stream);
   if (st != WF_OK) return PyLong_FromLong(st);
@@ -343,8 +353,8 @@ PyObject* compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const at::Tensor flat = fresh(*b.lens, {2 + 2 * k + 2 * m + 1 + blocks + WF_KV_PAGES_WORK}, at::kInt);
   int32_t* base = static_cast<int32_t*>(flat.data_ptr());
   int32_t *ring = base + 2, *shared = ring + k, *moves = shared + k, *done = moves + 2 * m, *ids = done + 1, *work = ids + blocks;
-  const at::Tensor out[5] = {flat.narrow(0, 0, 2), flat.narrow(0, 2, k), flat.narrow(0, 2 + k, k), flat.narrow(0, 2 + 2 * k + 2 * m, 1),
-                             flat.narrow(0, 2 + 2 * k, 2 * m).view({2, m})};
+  const at::Tensor out[5] = {part(flat, 0, {2}), part(flat, 2, {k}), part(flat, 2 + k, {k}), part(flat, 2 + 2 * k + 2 * m, {1}),
+                             part(flat, 2 + 2 * k, {2, m})};
   const wf_status st = queued(g_compact, a.g->ctx, (int32_t)k, (int32_t)b.rows, Batch::in(b.lens), Batch::in(b.pool), base, Batch::in(b.ring), ring,
                               Batch::out(b.table), Batch::in(b.shared), shared, moves, moves + m, done, ids, work, stream);
   if (st != WF_OK) return PyLong_FromLong(st);

@@ -8,7 +8,7 @@
 // memory (2 to 3 us a kernel), not the bytes: a few hundred KB.  Caches of up to kOneBlocks blocks are the work of one
 // workgroup, with what it knows of every block in LDS (4 bytes of it or 2, what 160 KB hold), barriers between the
 // phases and eight loads of a thread on their way at once: one launch.  4 forks among 16 rows and 100 blocks 4.3 us, the copies
-// 3.0 (10 us a call of both from Python); 4 of 64 rows of 7,984 blocks released 7.2 us (as kernels of a phase each 15 from Python,
+// 3.0 (8.9 us a call of both from Python); 4 of 64 rows of 7,984 blocks released 7.2 us (as kernels of a phase each 15 from Python,
 // so 8); a compaction of 767 blocks and 24 rows 6.0 us, of 6,263 and 96 rows 14.2.
 // Larger ones take a kernel a phase, ids and entries over all CUs: 1,500 rows of up to 377 entries and 249,669 blocks released
 // 3.0 + 6.8 + 3.2 + 4.9 us, of which the walk over the rows' entries (atomics in L2) is the longest; 250 forks of rows of 236

@@ -461,6 +461,37 @@ def test_both_ways_of_a_call_agree():
             assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("inference", [False, True])
+def test_outputs_are_ordinary_tensors(inference):
+    """Parts of one allocation, but tensors like others: changed in place, used with gradients, kept when the others go."""
+    rng = np.random.default_rng(4)
+    lens, pool, ring, table, shared = state_of(rng, 6, 16, 5)
+    lens[:2], table[0, :3] = (40, 0), np.arange(3)
+    with ctx_of(len(ring), 5) as ctx, torch.inference_mode(inference):
+        src, dst, want = dev(i32([0])), dev(i32([1])), dev(i32([40]))
+        rg, tb = dev(ring), dev(table)
+        outs = [*pkg.kv_fork(ctx, src, dst, want, dev(lens), dev(pool), rg, tb, dev(shared)),
+                *pkg.kv_release(ctx, dev(np.zeros(6, np.uint8)), dev(lens), dev(pool), rg, tb, dev(shared)),
+                *pkg.kv_compact(ctx, len(ring) - 1, dev(lens), dev(pool), rg, tb, dev(shared))]
+        shapes = [(6,), (2,), (len(ring),), (1,), (2, 1), (6,), (2,), (len(ring),), (2,), (len(ring) - 1,), (len(ring) - 1,), (1,), (2, 1)]
+        assert [tuple(x.shape) for x in outs] == shapes
+        before = [x.clone() for x in outs]
+        for i, x in enumerate(outs):
+            assert x.is_contiguous() and x.is_inference() == inference and not x.requires_grad
+            x += 1 + i
+        for i, (x, y) in enumerate(zip(outs, before)):
+            assert torch.equal(x, y + 1 + i)
+        kept = outs[2]
+        want = kept.clone()
+        del outs, x
+        torch.full((1 << 16,), 5, dtype=torch.int32, device=DEV)
+        assert torch.equal(kept, want)
+        if not inference:
+            w = torch.ones(6, device=DEV, requires_grad=True)
+            (w * before[0]).sum().backward()
+            assert torch.equal(w.grad, before[0].float())
+
+
 @pytest.mark.parametrize("handle", [False, True])
 def test_calls_on_a_given_stream(handle):
     """stream= takes the work in order with what is queued there, and owns the outputs."""
