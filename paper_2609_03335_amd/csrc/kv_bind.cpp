@@ -10,6 +10,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <climits>
 #include <cstdint>
 
@@ -97,6 +98,13 @@ struct Args {
   // ... whose rows, where it has several axes, are `pitch` elements apart.
   void rows(const at::Tensor* t, int64_t pitch) {
     if (ok && t && t->dim() > 1 && t->numel() != t->size(0) * pitch) ok = false;
+  }
+  // ... of `layers` caches, one after the other (axes that say otherwise, or nothing, are for the caller).
+  void caches(const at::Tensor* t, int64_t layers) {
+    holds(t, std::max<int64_t>(layers, 1) * g->cache_bytes);
+    if (!ok || layers < 2 || t->dim() < 2 || t->numel() == layers * g->cache_bytes) return;
+    ok = false;
+    for (const int64_t apart : t->strides()) ok |= apart == g->cache_bytes;
   }
   // [n, heads, D] with dense heads; its token stride.
   int64_t tokens(const at::Tensor* t, int64_t n, int64_t heads) {
@@ -371,7 +379,7 @@ PyObject* copy(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const at::Tensor *cache = a.dense(at::kByte), *moves = a.dense(at::kInt);
   const int64_t layers = a.integer(0, WF_KV_MAX_LAYERS);
   if (!a.ok || moves->dim() != 2 || moves->size(0) != 2 || moves->size(1) > WF_KV_MAX_BLOCKS) return none();
-  a.holds(cache, (layers > 1 ? layers : 1) * a.g->cache_bytes);
+  a.caches(cache, layers);
   if (!a.ok) return none();
   const int64_t m = moves->size(1);
   const wf_status st = queued(g_copy, a.g->ctx, (uint8_t*)data(cache), a.g->cache_bytes, (int32_t)layers, Batch::in(moves), Batch::in(moves) + m,

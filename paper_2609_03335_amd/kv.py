@@ -139,6 +139,17 @@ class KVContext:
                              "contiguous heads needed")
         return x.data_ptr(), st[0] if n > 1 else width
 
+    def _apart(self, cache, layers: int) -> int:
+        """How far the caches of `layers` layers lie apart in a buffer: the context's own bytes, unless a tensor's
+        first axis are the layers of a larger cache, of which the context has the front."""
+        if layers < 2 or getattr(cache, "ndim", 0) < 2 or cache.numel() == layers * self.cache_bytes or self.cache_bytes in cache.stride():
+            return self.cache_bytes
+        pitch = cache.numel() // max(cache.shape[0], 1)
+        if cache.shape[0] == layers and pitch > self.cache_bytes:
+            return pitch
+        raise ValueError(f"cache: shape {tuple(cache.shape)} does not say where {layers} layers of {self.cache_bytes} bytes lie; "
+                         "give layer_stride")
+
     def _s(self, stream) -> Optional[int]:
         """The stream's handle; by default the current stream of the context's device."""
         if stream is None and self._current is not None:
@@ -222,7 +233,7 @@ class KVContext:
             b(ids, 4 * n, "ids"), b(work, 4 * WF_KV_PAGES_WORK, "work"), self._s(stream)))
 
     def wf_kv_copy(self, cache, from_, to, n: int, *, layers: int = 1, layer_stride: Optional[int] = None, stream=None) -> None:
-        m, step = max(int(n), 0), self.cache_bytes if layer_stride is None else int(layer_stride)
+        m, step = max(int(n), 0), self._apart(cache, int(layers)) if layer_stride is None else int(layer_stride)
         need = self.cache_bytes + max(int(layers) - 1, 0) * max(step, 0)
         self._check(self.lib.wf_kv_copy(self.handle, self._b(cache, need, "cache", 1), step, int(layers), self._b(from_, 4 * m, "from"),
                                         self._b(to, 4 * m, "to"), int(n), self._s(stream)))
@@ -445,12 +456,14 @@ def kv_compact(ctx: KVContext, keep: int, lens, pool, ring, table, shared, strea
     return pool_out, ring_out, shared_out, done, moves.view(2, m)
 
 
-def kv_copy(ctx: KVContext, cache, moves, layers: int = 1, stream=None) -> None:
-    """Copies blocks moves[0] to moves[1] (those of kv_fork or kv_compact) in `layers` caches that lie one after the other in `cache`."""
+def kv_copy(ctx: KVContext, cache, moves, layers: int = 1, stream=None, layer_stride: Optional[int] = None) -> None:
+    """Copies blocks moves[0] to moves[1] (those of kv_fork or kv_compact) in `layers` caches that lie one after the other in `cache`,
+    layer_stride bytes apart.  By default that is the bytes of one; in a tensor [layers, bytes of a larger cache] (a context
+    that goes on with the front of each after kv_compact) the length of a row.  Where other axes leave it open, it has to be given."""
     if stream is not None:
         with _made_current(ctx, stream):
-            return kv_copy(ctx, cache, moves, layers)
-    if ctx._bind is not None:
+            return kv_copy(ctx, cache, moves, layers, None, layer_stride)
+    if ctx._bind is not None and layer_stride is None:
         out = ctx._bind.copy(ctx._geometry, ctx._current(ctx.device), cache, moves, layers)
         if out is not None:
             if out.__class__ is int:
@@ -460,4 +473,4 @@ def kv_copy(ctx: KVContext, cache, moves, layers: int = 1, stream=None) -> None:
         raise ValueError(f"moves: shape {tuple(moves.shape)}, [2, n] needed")
     n = moves.shape[1]
     at = ctx._b(moves, 8 * n, "moves")
-    ctx.wf_kv_copy(cache, at, at + 4 * n, n, layers=layers)
+    ctx.wf_kv_copy(cache, at, at + 4 * n, n, layers=layers, layer_stride=layer_stride)

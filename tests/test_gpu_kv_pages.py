@@ -539,3 +539,30 @@ def test_the_example_serves_with_either_codes(codes):
     assert [len(a) for a in answers] == [count for _, count in jobs]
     assert replica.pool[1].item() == 30 and sorted(replica.ring.tolist()) == list(range(30))
     replica.close()
+
+
+@pytest.mark.parametrize("codes", ["e2m1", "e4m3"])
+def test_copies_in_the_front_of_larger_caches(codes):
+    """After a compaction: blocks of each layer move within its front, and nothing else changes, either way of the call."""
+    layers, n, keep = 3, 20, 9
+    rng = np.random.default_rng(15)
+    with ctx_of(n, 4, codes=codes) as whole, ctx_of(keep, 4, codes=codes) as ctx:
+        data = rng.integers(0, 256, (layers, n, whole.cache_bytes // n), dtype=np.uint8)
+        moves, want = dev(i32([[0, 7, -1, 12], [3, 8, 1, 2]])), data.copy()      # (12 is no block of this context)
+        for f, t in ((0, 3), (7, 8)):
+            want[:, t] = want[:, f]
+        bind = ctx._bind
+        for way in (bind, None):
+            ctx._bind = way
+            for shape in ((layers, -1), (layers, n, whole.cache_bytes // n)):
+                cache = dev(data).view(shape)
+                pkg.kv_copy(ctx, cache, moves, layers=layers)
+                assert np.array_equal(cache.cpu().numpy().reshape(data.shape), want)
+            flat = dev(data).view(-1)
+            pkg.kv_copy(ctx, flat, moves, layers=layers, layer_stride=whole.cache_bytes)
+            assert np.array_equal(flat.cpu().numpy().reshape(data.shape), want)
+            cache = dev(data).view(layers, -1)
+            with pytest.raises(ValueError):
+                pkg.kv_copy(ctx, cache, moves, layers=2)
+            assert np.array_equal(cache.cpu().numpy().reshape(data.shape), data)
+        ctx._bind = bind

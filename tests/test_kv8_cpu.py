@@ -122,3 +122,55 @@ def test_oracle_pages_keep_their_counts():
             s = K.step(rng.integers(0, 40, rows), lens, pool, ring, table, b, 0)
             lens, pool, ring, table = s["lens"], s["pool"], s["ring"], s["table"]
         check()
+
+
+def context_without_a_gpu(n_blocks):
+    """A context whose calls of the library are recorded, over host tensors."""
+    import torch
+
+    class Library:
+        made = []
+
+        def wf_kv_copy(self, handle, cache, step, layers, *rest):
+            self.made.append((step, layers))
+            return pkg.WF_OK
+
+        def wf_kv_ctx_destroy(self, handle):
+            pass
+
+    ctx = pkg.KVContext.__new__(pkg.KVContext)
+    ctx.lib, ctx.handle, ctx.device, ctx._bind, ctx._current = Library(), 1, -1, None, None
+    ctx.cache_bytes = pkg.wf_kv_cache_bytes(**dict(GOOD, n_blocks=n_blocks), codes="e4m3")
+    return ctx, torch.full((2, 3), -1, dtype=torch.int32)
+
+
+def test_copies_go_to_the_layers_of_a_larger_cache():
+    """A context of fewer blocks goes on with the front of each layer's cache: the layers of that tensor are as far apart as they were."""
+    import torch
+    whole = pkg.wf_kv_cache_bytes(**GOOD, codes="e4m3")
+    ctx, moves = context_without_a_gpu(4)
+    part = ctx.cache_bytes
+    zeros = lambda *shape: torch.zeros(shape, dtype=torch.uint8)
+    for cache, layers, apart in ((zeros(3, whole), 3, whole), (zeros(2, whole), 2, whole), (zeros(3, 10, whole // 10), 3, whole),
+                                 (zeros(3 * whole), 3, part), (zeros(3, part), 3, part), (zeros(5, part), 3, part),
+                                 (zeros(2, 3, part), 5, part), (zeros(3 * 4, part // 4), 3, part), (zeros(3, whole), 1, part)):
+        pkg.kv_copy(ctx, cache, moves, layers=layers)
+        assert ctx.lib.made.pop() == (apart, layers), (tuple(cache.shape), layers)
+    pkg.kv_copy(ctx, zeros(4, whole), moves, layers=2, layer_stride=whole)
+    assert ctx.lib.made.pop() == (whole, 2)
+    pkg.kv_copy(ctx, zeros(2, part), moves, layers=2, layer_stride=part)
+    assert ctx.lib.made.pop() == (part, 2)
+
+
+def test_layers_that_no_axis_shows_are_refused():
+    import torch
+    whole = pkg.wf_kv_cache_bytes(**GOOD, codes="e4m3")
+    ctx, moves = context_without_a_gpu(4)
+    zeros = lambda *shape: torch.zeros(shape, dtype=torch.uint8)
+    # layers of a larger cache, more or fewer of them than are to be copied in; blocks without an axis of layers
+    for cache, layers in ((zeros(4, whole), 2), (zeros(2, whole), 4), (zeros(3 * 10, whole // 10), 3), (zeros(1, 3 * whole), 3)):
+        with pytest.raises(ValueError):
+            pkg.kv_copy(ctx, cache, moves, layers=layers)
+    with pytest.raises(ValueError):
+        pkg.kv_copy(ctx, zeros(3, whole), moves, layers=3, layer_stride=2 * whole)     # past the end
+    assert not ctx.lib.made
