@@ -119,6 +119,11 @@ wf_status wf_kv_ctx_create(int hip_device, const wf_kv_desc *desc, wf_kv_ctx **o
 /* Free the context (NULL is a no-op).  Work queued on it must have completed. */
 void wf_kv_ctx_destroy(wf_kv_ctx *ctx);
 
+/* The context goes on with a cache of n_blocks blocks (1..WF_KV_MAX_BLOCKS), as after wf_kv_compact with n_blocks = keep:
+ * calls from now on take rings, counts and caches of that size.  Host only: its work areas stay, nothing is allocated, and
+ * work that is queued or captured keeps the number that it was made with. */
+wf_status wf_kv_ctx_set_blocks(wf_kv_ctx *ctx, int32_t n_blocks);
+
 /* As wf_plan_last_error, for this part of the library. */
 const char *wf_kv_last_error(const wf_kv_ctx *ctx);
 
@@ -260,8 +265,8 @@ wf_status wf_kv_release(wf_kv_ctx *ctx, const uint8_t *release, int32_t n_rows, 
 
 /*
  * Moves the blocks in use to ids below `keep` (1 .. n_blocks - 1), so that the cache can go on with n_blocks =
- * keep: a context of that geometry takes the front of the same buffers (block b keeps its place), the new
- * ring, pool and shared counts and the same table.
+ * keep: the context (wf_kv_ctx_set_blocks) or another of that geometry takes the front of the same buffers (block b
+ * keeps its place), the new ring, pool and shared counts and the same table.
  *   - In use is every block that is not in the ring.  The k-th block in use from `keep` on, in ascending order, moves to the
  *     k-th free one below: from[k], to[k], for wf_kv_copy; the other entries of from and to are -1.
  *   - Table entries of blocks that rows hold (len of them) are rewritten; shared_out [keep] has the counts by new id.

@@ -52,7 +52,7 @@ EXPORTS = ("wf_plan_ctx_create", "wf_plan_ctx_destroy", "wf_plan_last_error",
 # every symbol declared in include/wf_kv.h
 KV_EXPORTS = ("wf_kv_cache_bytes", "wf_kv_ctx_create", "wf_kv_ctx_destroy", "wf_kv_last_error",
               "wf_kv_step", "wf_kv_store", "wf_kv_load", "wf_kv_attend", "wf_kv_fork", "wf_kv_release", "wf_kv_compact",
-              "wf_kv_copy")
+              "wf_kv_copy", "wf_kv_ctx_set_blocks")
 
 
 class WFError(RuntimeError):
@@ -165,6 +165,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.wf_kv_release.argtypes = [vp, vp, i32] + [vp] * 10
     lib.wf_kv_compact.argtypes = [vp, i32, i32] + [vp] * 14
     lib.wf_kv_copy.argtypes = [vp, vp, i64, i32, vp, vp, i32, vp]
+    lib.wf_kv_ctx_set_blocks.argtypes = [vp, i32]
     for name in KV_EXPORTS:
         if name not in ("wf_kv_ctx_destroy", "wf_kv_last_error"):
             getattr(lib, name).restype = i32

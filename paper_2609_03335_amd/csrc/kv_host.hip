@@ -159,6 +159,13 @@ void wf_kv_ctx_destroy(wf_kv_ctx* ctx) {
   delete ctx;
 }
 
+wf_status wf_kv_ctx_set_blocks(wf_kv_ctx* ctx, int32_t n_blocks) {
+  if (!ctx) return null_ctx();
+  if (n_blocks < 1 || n_blocks > WF_KV_MAX_BLOCKS) return fail(ctx, WF_EINVAL, "n_blocks=%d outside [1, %d]", n_blocks, WF_KV_MAX_BLOCKS);
+  ctx->g.n_blocks = n_blocks;
+  return WF_OK;
+}
+
 const char* wf_kv_last_error(const wf_kv_ctx* ctx) { return ctx ? ctx->err : g_kv_err; }
 
 wf_status wf_kv_step(wf_kv_ctx* ctx, const int32_t* new_tokens, int32_t n_rows, int32_t n_tokens,

@@ -63,16 +63,29 @@ class KVContext:
         self.handle = h
         self.device = device
         self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
-        self.block_tokens, self.n_blocks, self.max_blocks = block_tokens, n_blocks, max_blocks
+        self.block_tokens, self.max_blocks = block_tokens, max_blocks
         self.codes = "e4m3" if d.dtype & WF_KV_E4M3 else "e2m1"
         self.dtype = d.dtype & ~WF_KV_E4M3
         self.torch_dtype = torch_type(self.dtype)
         self._current = _current_stream()
         self._bind = _bind() if self._current is not None else None
-        self.cache_bytes = wf_kv_cache_bytes(q_heads, kv_heads, head_dim, block_tokens, n_blocks, max_blocks, d.dtype)
+        self._blocks(n_blocks)
+
+    def _blocks(self, n_blocks: int) -> None:
+        """What the checks of arguments go by, for a cache of n_blocks blocks."""
+        self.n_blocks = n_blocks
+        self.cache_bytes = wf_kv_cache_bytes(self.q_heads, self.kv_heads, self.head_dim, self.block_tokens, n_blocks, self.max_blocks,
+                                             self.dtype | _CODES[self.codes])
         if self._bind is not None:
-            self._geometry = self._bind.geometry(h.value, device, q_heads, kv_heads, head_dim, n_blocks, max_blocks,
-                                                 self.cache_bytes, self.dtype == WF_KV_F16)
+            self._geometry = self._bind.geometry(self.handle.value, self.device, self.q_heads, self.kv_heads, self.head_dim, n_blocks,
+                                                 self.max_blocks, self.cache_bytes, self.dtype == WF_KV_F16)
+
+    def wf_kv_ctx_set_blocks(self, n_blocks: int) -> None:
+        """The context goes on with a cache of n_blocks blocks, as after kv_compact with keep=n_blocks: nothing is allocated
+        (another context would take work areas of its own, 272 MiB) or waited for."""
+        n = min(max(int(n_blocks), -1), 2 ** 31 - 1)      # (refused as it is, not taken for what its low bits are)
+        self._check(self.lib.wf_kv_ctx_set_blocks(self.handle, n))
+        self._blocks(n)
 
     def _check(self, st):
         if st != WF_OK:
@@ -434,8 +447,8 @@ def kv_release(ctx: KVContext, release, lens, pool, ring, table, shared, stream=
 
 def kv_compact(ctx: KVContext, keep: int, lens, pool, ring, table, shared, stream=None):
     """All blocks in use move below `keep`.  table is updated in place; returns (pool, ring, shared, done, moves): moves for
-    kv_copy, the others for a context with n_blocks=keep over the front of the same caches.  done is 0 where more blocks are in
-    use: nothing has moved then."""
+    kv_copy, the others for a cache of keep blocks, the front of the same one (ctx.wf_kv_ctx_set_blocks(keep), once the moves are
+    copied).  done is 0 where more blocks are in use: nothing has moved then."""
     if stream is not None:
         with _made_current(ctx, stream):
             return kv_compact(ctx, keep, lens, pool, ring, table, shared)

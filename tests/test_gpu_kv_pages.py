@@ -566,3 +566,65 @@ def test_copies_in_the_front_of_larger_caches(codes):
                 pkg.kv_copy(ctx, cache, moves, layers=2)
             assert np.array_equal(cache.cpu().numpy().reshape(data.shape), data)
         ctx._bind = bind
+
+
+@pytest.mark.parametrize("codes", ["e2m1", "e4m3"])
+def test_a_context_goes_on_with_fewer_blocks(codes):
+    """After a compaction the context takes the front of its caches without any memory of its own, and all calls are then those of a
+    context that was made with so many blocks."""
+    hq, hk, d, b, width, rows, layers = 4, 2, 64, 16, 6, 12, 2
+    rng = np.random.default_rng(16)
+    lens, pool, ring, table, shared = (dev(x) for x in state_of(rng, rows, b, width, spare=40))
+    n = ring.numel()
+    keep = n - 25
+    with ctx_of(n, width, b, codes, hq, hk, d) as ctx, ctx_of(keep, width, b, codes, hq, hk, d) as new:
+        caches = torch.randint(0, 120, (layers, ctx.cache_bytes), device=DEV).to(torch.uint8)     # (codes that are numbers, small scales)
+        pool, ring, shared, done, moves = pkg.kv_compact(ctx, keep, lens, pool, ring, table, shared)
+        assert done.item() == 1 and (moves >= 0).any()
+        pkg.kv_copy(ctx, caches, moves, layers=layers)
+        bad = (0, -3, (1 << 30) + 1, (1 << 32) + 3)
+        for x in bad:
+            with pytest.raises(pkg.WFError) as e:
+                ctx.wf_kv_ctx_set_blocks(x)
+            assert e.value.status == pkg.WF_EINVAL and ctx.n_blocks == n
+        torch.cuda.synchronize()
+        free = torch.cuda.mem_get_info()[0]
+        ctx.wf_kv_ctx_set_blocks(keep)
+        assert torch.cuda.mem_get_info()[0] == free
+        assert (ctx.n_blocks, ctx.cache_bytes) == (keep, new.cache_bytes)
+        g = torch.Generator(device=DEV)
+        g.manual_seed(2)
+        counts = dev(i32(np.where(rng.random(rows) < 0.6, rng.integers(0, 4, rows), 0)))
+        T = int(counts.sum())
+        x = torch.randn(layers, T, hq + 2 * hk, d, generator=g, device=DEV).to(torch.bfloat16)
+        free_rows = np.nonzero(lens.cpu().numpy() == 0)[0]
+        f = dev(i32([[int(lens.argmax()), int(r), 37] for r in free_rows[:3]]))
+
+        def run(c, way):
+            c._bind = way
+            t, r, all_ = table.clone(), ring.clone(), caches.clone()
+            got = list(pkg.kv_fork(c, *(f[:, i].contiguous() for i in range(3)), lens, pool, r, t, shared))
+            pkg.kv_copy(c, all_, got[4], layers=layers)
+            step = pkg.kv_step(c, counts, T, got[0], got[1], r, t)
+            for i in range(layers):
+                q = pkg.kv_store(c, x[i, :, :hq], x[i, :, hq:hq + hk], x[i, :, hq + hk:], step[4], step[3], all_[i])
+                got += [pkg.kv_attend(c, q, all_[i], t, step[0], step[2], step[4], scale=0.1), *pkg.kv_load(c, all_[i], step[3])]
+            ends = torch.ones(rows, dtype=torch.uint8, device=DEV)
+            ends[1] = 0
+            rest = pkg.kv_release(c, ends, step[0], step[1], r, t, got[2])
+            last = pkg.kv_compact(c, keep - 2, rest[0], rest[1], r, t, rest[2])
+            return [*got, *step, *rest, last[0], last[3], t, r, all_]
+
+        results = [run(c, way) for c in (new, ctx) for way in (c._bind, None)]
+        for other in results[1:]:
+            for y, z in zip(results[0], other):
+                assert torch.equal(y.view(torch.uint8), z.view(torch.uint8))
+        assert results[0][3].all()                     # the forks were granted
+        with pytest.raises(pkg.WFError):
+            pkg.kv_compact(ctx, keep, lens, pool, ring, table, shared)
+        with pytest.raises(ValueError):
+            pkg.kv_release(ctx, torch.ones(rows, dtype=torch.uint8, device=DEV), lens, pool, ring[:-1], table, shared)
+        ctx.wf_kv_ctx_set_blocks(n)                    # and back
+        assert ctx.cache_bytes == caches.shape[1]
+        pkg.kv_copy(ctx, caches, dev(i32([[0], [n - 1]])), layers=layers)
+        assert torch.equal(caches.view(layers, n, -1)[:, 0], caches.view(layers, n, -1)[:, n - 1])

@@ -174,3 +174,25 @@ def test_layers_that_no_axis_shows_are_refused():
     with pytest.raises(ValueError):
         pkg.kv_copy(ctx, zeros(3, whole), moves, layers=3, layer_stride=2 * whole)     # past the end
     assert not ctx.lib.made
+
+
+def test_blocks_of_no_context_are_refused():
+    lib = _lib.load()
+    assert lib.wf_kv_ctx_set_blocks(None, 4) == pkg.WF_EINVAL and b"NULL" in lib.wf_kv_last_error(None)
+
+
+def test_a_context_checks_by_the_blocks_it_was_given():
+    """Number of blocks and bytes of a cache follow; a refused number changes neither."""
+    ctx, _ = context_without_a_gpu(10)
+    asked = []
+    ctx.lib.wf_kv_ctx_set_blocks = lambda handle, n: asked.append(n) or (pkg.WF_OK if 1 <= n <= 1 << 30 else pkg.WF_EINVAL)
+    ctx.lib.wf_kv_last_error = lambda handle: b"refused"
+    ctx.q_heads, ctx.kv_heads, ctx.head_dim, ctx.block_tokens, ctx.max_blocks = 8, 2, 64, 16, 4
+    ctx.codes, ctx.dtype = "e4m3", pkg.WF_KV_BF16
+    for n in (4, 10, 1, 1 << 22):
+        ctx.wf_kv_ctx_set_blocks(n)
+        assert ctx.n_blocks == n == asked[-1] and ctx.cache_bytes == pkg.wf_kv_cache_bytes(**dict(GOOD, n_blocks=n), codes="e4m3")
+    for n in (0, -1, (1 << 30) + 1, (1 << 32) + 3, -(1 << 40)):
+        with pytest.raises(pkg.WFError):
+            ctx.wf_kv_ctx_set_blocks(n)
+        assert ctx.n_blocks == 1 << 22 and not 1 <= asked[-1] <= 1 << 30
