@@ -228,7 +228,7 @@ wf_status wf_kv_attend(wf_kv_ctx *ctx, const void *q, int64_t q_stride, int32_t 
  * calls below read shared_in and write shared_out, int32 [n_blocks] each, as wf_kv_step does with lengths and
  * pool: the old arrays stay as they were, a caller keeps two of each and swaps them.  table, ring, len_* and pool_* are
  * those of wf_kv_step.  A batch that shares blocks ends its rows with wf_kv_release, not with
- * new_tokens[r] < 0.  work int32 [WF_KV_PAGES_WORK] is overwritten.
+ * new_tokens[r] < 0.  work int32 [WF_KV_PAGES_WORK] may be overwritten.
  */
 #define WF_KV_PAGES_WORK 1024
 
@@ -245,7 +245,7 @@ wf_status wf_kv_attend(wf_kv_ctx *ctx, const void *q, int64_t q_stride, int32_t 
  *   - All forks see the rows as they are before the call.  No row may be dst of two forks.
  *   - len_out[dst[i]] = k (granted), other rows keep their length; pool_out and the entries of table follow.
  * Arrays: src, dst, tokens, from, to int32 [n_forks]; granted uint8 [n_forks].  len_out, pool_out and shared_out
- * must not be len_in, pool_in and shared_in.
+ * must not be len_in, pool_in and shared_in.  work is not used and may be NULL.
  */
 wf_status wf_kv_fork(wf_kv_ctx *ctx, const int32_t *src, const int32_t *dst, const int32_t *tokens, int32_t n_forks,
                      int32_t n_rows, const int32_t *len_in, int32_t *len_out, const int32_t *pool_in,

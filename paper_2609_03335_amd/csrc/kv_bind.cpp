@@ -313,14 +313,14 @@ PyObject* fork(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return none();
   const int64_t f = src->size(0), r = b.rows, blocks = a.g->n_blocks;
   at::AutoDispatchBelowADInplaceOrView plain;
-  const at::Tensor flat = fresh(*b.lens, {r + 2 + blocks + 2 * f + WF_KV_PAGES_WORK}, at::kInt);
+  const at::Tensor flat = fresh(*b.lens, {r + 2 + blocks + 2 * f}, at::kInt);
   int32_t* base = static_cast<int32_t*>(flat.data_ptr());
-  int32_t *pool = base + r, *shared = pool + 2, *moves = shared + blocks, *work = moves + 2 * f;
+  int32_t *pool = base + r, *shared = pool + 2, *moves = shared + blocks;
   const at::Tensor out[5] = {part(flat, 0, {r}), part(flat, r, {2}), part(flat, r + 2, {blocks}), fresh(*b.lens, {f}, at::kByte),
                              part(flat, r + 2 + blocks, {2, f})};
   const wf_status st = queued(g_fork, a.g->ctx, Batch::in(src), Batch::in(dst), Batch::in(tokens), (int32_t)f, (int32_t)r, Batch::in(b.lens), base,
                               Batch::in(b.pool), pool, Batch::in(b.ring), Batch::out(b.table), Batch::in(b.shared), shared, moves, moves + f,
-                              (uint8_t*)data(&out[3]), work, stream);
+                              (uint8_t*)data(&out[3]), (int32_t*)nullptr, stream);
   if (st != WF_OK) return PyLong_FromLong(st);
   return wrapped(out);
   END_HANDLE_TH_ERRORS

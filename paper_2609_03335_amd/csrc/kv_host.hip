@@ -257,13 +257,13 @@ wf_status wf_kv_attend(wf_kv_ctx* ctx, const void* q, int64_t q_stride, int32_t 
 wf_status wf_kv_fork(wf_kv_ctx* ctx, const int32_t* src, const int32_t* dst, const int32_t* tokens, int32_t n_forks,
                      int32_t n_rows, const int32_t* len_in, int32_t* len_out, const int32_t* pool_in,
                      int32_t* pool_out, const int32_t* ring, int32_t* table, const int32_t* shared_in,
-                     int32_t* shared_out, int32_t* from, int32_t* to, uint8_t* granted, int32_t* work,
+                     int32_t* shared_out, int32_t* from, int32_t* to, uint8_t* granted, int32_t* /* work */,
                      void* hip_stream) {
   if (!ctx) return null_ctx();
   if (n_forks < 0 || n_forks > WF_KV_MAX_FORKS) return fail(ctx, WF_EINVAL, "n_forks=%d outside [0, %d]", n_forks, WF_KV_MAX_FORKS);
   if (n_rows < 0 || n_rows > WF_KV_MAX_ROWS) return fail(ctx, WF_EINVAL, "n_rows=%d outside [0, %d]", n_rows, WF_KV_MAX_ROWS);
-  if (!pool_in || !pool_out || !ring || !shared_in || !shared_out || !work)
-    return fail(ctx, WF_EINVAL, "pool_in, pool_out, ring, shared_in, shared_out or work is NULL");
+  if (!pool_in || !pool_out || !ring || !shared_in || !shared_out)
+    return fail(ctx, WF_EINVAL, "pool_in, pool_out, ring, shared_in or shared_out is NULL");
   if (n_rows && (!len_in || !len_out || !table)) return fail(ctx, WF_EINVAL, "a row array (len_in, len_out, table) is NULL");
   if (n_forks && (!src || !dst || !tokens || !from || !to || !granted))
     return fail(ctx, WF_EINVAL, "an array of forks (src, dst, tokens, from, to, granted) is NULL");

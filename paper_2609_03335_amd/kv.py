@@ -216,7 +216,7 @@ class KVContext:
             self._wide(out, 2 * n * self.q_heads * self.head_dim, "out"), self._s(stream)))
 
     def wf_kv_fork(self, src, dst, tokens, n_forks: int, n_rows: int, len_in, len_out, pool_in, pool_out, ring, table, shared_in,
-                   shared_out, from_, to, granted, work, stream=None) -> None:
+                   shared_out, from_, to, granted, work=None, stream=None) -> None:
         b, f, r, n = self._b, max(int(n_forks), 0), max(int(n_rows), 0), self.n_blocks
         self._check(self.lib.wf_kv_fork(
             self.handle, b(src, 4 * f, "src"), b(dst, 4 * f, "dst"), b(tokens, 4 * f, "tokens"), int(n_forks), int(n_rows),
@@ -415,12 +415,12 @@ def kv_fork(ctx: KVContext, src, dst, tokens, lens, pool, ring, table, shared, s
     n, r, b = src.shape[0], lens.shape[0], ctx.n_blocks
     if not n == dst.shape[0] == tokens.shape[0]:
         raise ValueError(f"src, dst and tokens: {n}, {dst.shape[0]} and {tokens.shape[0]} entries")
-    flat = lens.new_empty(r + 2 + b + 2 * n + WF_KV_PAGES_WORK, dtype=torch.int32)
+    flat = lens.new_empty(r + 2 + b + 2 * n, dtype=torch.int32)
     granted = lens.new_empty(n, dtype=torch.uint8)
-    lens_out, pool_out, shared_out, moves, work = flat.split((r, 2, b, 2 * n, WF_KV_PAGES_WORK))
+    lens_out, pool_out, shared_out, moves = flat.split((r, 2, b, 2 * n))
     at = moves.data_ptr()
     ctx.wf_kv_fork(src, dst, tokens, n, r, lens, lens_out.data_ptr(), pool, pool_out.data_ptr(), ring, table, shared,
-                   shared_out.data_ptr(), at, at + 4 * n, granted.data_ptr(), work.data_ptr())
+                   shared_out.data_ptr(), at, at + 4 * n, granted.data_ptr())
     return lens_out, pool_out, shared_out, granted, moves.view(2, n)
 
 

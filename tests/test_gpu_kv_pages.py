@@ -628,3 +628,28 @@ def test_a_context_goes_on_with_fewer_blocks(codes):
         assert ctx.cache_bytes == caches.shape[1]
         pkg.kv_copy(ctx, caches, dev(i32([[0], [n - 1]])), layers=layers)
         assert torch.equal(caches.view(layers, n, -1)[:, 0], caches.view(layers, n, -1)[:, n - 1])
+
+
+def test_forks_take_no_scratch():
+    """wf_kv_fork needs no work array, and leaves one that is given alone; the helper's outputs are all that it allocates."""
+    rng = np.random.default_rng(17)
+    rows, width, b = 9, 5, 16
+    lens, pool, ring, table, shared = state_of(rng, rows, b, width, spare=20)
+    forks = [(int(np.argmax(lens)), int(r), 35) for r in np.nonzero(lens == 0)[0]]
+    want, f = E.fork(forks, lens, pool, ring, table, shared, b), dev(i32(forks))
+    n, m = len(ring), len(forks)
+    empty = lambda k, t=torch.int32: torch.empty(k, dtype=t, device=DEV)
+    with ctx_of(n, width, b) as ctx:
+        src, dst, tokens = (f[:, i].contiguous() for i in range(3))
+        for work in ((), (None,), (torch.full((1024,), 5, dtype=torch.int32, device=DEV),)):
+            t, o = dev(table), dict(lens=empty(rows), pool=empty(2), shared=empty(n), moves=empty((2, m)), granted=empty(m, torch.uint8))
+            ctx.wf_kv_fork(src, dst, tokens, m, rows, dev(lens), o["lens"], dev(pool), o["pool"], dev(ring), t, dev(shared), o["shared"],
+                           o["moves"][0], o["moves"][1], o["granted"], *work)
+            same(dict(o, table=t), want)
+            assert not work or work[0] is None or (work[0] == 5).all()
+        bind = ctx._bind
+        for way in (bind, None):
+            ctx._bind = way
+            out = pkg.kv_fork(ctx, src, dst, tokens, dev(lens), dev(pool), dev(ring), dev(table), dev(shared))
+            assert out[0].untyped_storage().nbytes() == 4 * (rows + 2 + n + 2 * m)
+        ctx._bind = bind
