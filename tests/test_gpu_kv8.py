@@ -674,3 +674,39 @@ def test_no_tokens():
         assert pkg.kv_store(ctx, q, k, k, None, none, cache).shape == (0, 8, 64)
         assert pkg.kv_load(ctx, cache, none)[0].shape == (0, 2, 64)
         assert (cache == 5).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("window", [1, 40, 63, 64, 150, 333])
+@pytest.mark.parametrize("hq,hk,d,b", [(8, 1, 128, 32), (10, 2, 128, 16), (6, 3, 256, 32)])
+def test_attend_prompts_of_many_columns_through_windows(hq, hk, d, b, window, dtype):
+    """Windows on the kernel of many columns at 128 and 256 channels too (lengths not known, so that it is taken): several tiles of
+    columns a row, sight that begins past the row's first units, tokens that only some of a wave's columns see."""
+    rows = [(700, 700, None), (390, 130, None), (64, 64, None), (0, 5, 0), (1000, 90, None), (333, 60, -20), (130, 70, 100)]
+    check_attend(hq, hk, d, b, rows, dtype, window=window, seed=d + window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d,nq", [(8, 1, 128, 150), (4, 2, 128, 900), (6, 1, 256, 100)])
+@pytest.mark.parametrize("window", [48, 500])
+def test_attend_uneven_scores_through_windows(window, hq, hk, d, nq, dtype):
+    """Blocks that take nearly all the weight of the queries that see them, where a window hides them from others."""
+    n, b = 1500, 16
+    for i, (far, size) in enumerate((([1499 - nq // 2], 1.0), ([1490], 2.0 ** -12), ([1499 - nq - window // 2, 1499 - nq // 3, 1480], 2.0 ** 12))):
+        rng = np.random.default_rng(200 + i)
+        q, cache, table, kv, q_off, pos = skewed_case(rng, hq, hk, d, b, n, nq, dtype, far, size)
+        scale = 0.5 * d ** -0.5
+        want, mag, dots, top = E.attend(host(q), cache, table, kv, q_off, pos, scale, window)
+        with ctx_of(hq, hk, d, b, cache.n, table.shape[1], dtype) as ctx:
+            for max_kv in (n, 0):
+                got = host(pkg.kv_attend(ctx, q, dev(cache.bytes), dev(table), dev(kv), dev(q_off), dev(pos), scale=scale, window=window,
+                                         max_q=nq, max_kv=max_kv))
+                lim = bound(dtype, want, mag, dots, d, n, top)
+                assert (np.abs(got - want) <= lim).all(), (far, max_kv, float((np.abs(got - want) / lim).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("window", [20, 70])
+def test_attend_through_windows_beside_garbage(window, dtype):
+    """... and blocks before every window that hold no numbers."""
+    test_attend_beside_garbage(4, 1, 128, 16, 150, window, dtype)
