@@ -871,13 +871,14 @@ hipError_t narrow(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_
 }
 
 // (256 channels: four waves, a SIMD each, of two tiles of columns: a prompt of 7,001 of 32 heads 900 us, 892 TFLOP/s, against
-// 1,328 with one; f16 1,007 against 1,380, though some of its registers go to scratch.)
+// 1,328 with one; f16 1,007 against 1,380, though 79 of its registers go to scratch.  Of 128 channels in f16 2 do.)
 template <int D, class M>
 hipError_t wide(const Geo& g, const AttendArgs& a, const AttendWork& w, int64_t columns, hipStream_t s) {
   constexpr int C = 2, W = D == 256 ? 4 : 8, H = kThreads / (D / 4);
   // A CU holds one workgroup of 128 or 256 channels.  The shares of one row are alike and are to run all at once (200 tokens of 32
   // heads of 128 over 16,000 79 us, with twice the shares 113; 400 127 and 195); of several rows, which are not, twice as many
-  // even out (8 rows of 100 tokens over up to 5,000 65 us against 83, 4 of 300 94 against 142).
+  // even out (8 rows of 100 tokens over up to 5,000 65 us against 83, 4 of 300 94 against 142; several rows of one length,
+  // which would be alike too, were not measured).
   const Split sp = split_of<D>(g, a, w, columns, 16 * C * W, w.n_cu * (D > 64 && a.n_rows == 1 ? 1 : 2), kWaves);
   const hipError_t e = launch(attend8_wide<D, C, W, M>, g, a, sp, 64 * W, s);
   if (e != hipSuccess || sp.splits == 1) return e;

@@ -8,7 +8,7 @@
 // memory (2 to 3 us a kernel), not the bytes: a few hundred KB.  Caches of up to kOneBlocks blocks are the work of one
 // workgroup, with what it knows of every block in LDS (4 bytes of it or 2, what 160 KB hold), barriers between the
 // phases and eight loads of a thread on their way at once: one launch.  4 forks among 16 rows and 100 blocks 4.3 us, the copies
-// 3.0 (8.9 us a call of both from Python); 4 of 64 rows of 7,984 blocks released 7.2 us (as kernels of a phase each 15 from Python,
+// 3.0 (9 to 10 us a call of both from Python); 4 of 64 rows of 7,984 blocks released 7.2 us (as kernels of a phase each 15 from Python,
 // so 8); a compaction of 767 blocks and 24 rows 6.0 us, of 6,263 and 96 rows 14.2.
 // Larger ones take a kernel a phase, ids and entries over all CUs: 1,500 rows of up to 377 entries and 249,669 blocks released
 // 3.0 + 6.8 + 3.2 + 4.9 us, of which the walk over the rows' entries (atomics in L2) is the longest; 250 forks of rows of 236
@@ -151,7 +151,7 @@ __device__ __forceinline__ uint32_t sum_of(uint32_t x, uint32_t* part) {
 }
 
 // For one workgroup: entries of a list of up to kOneBlocks that a test picks, in order.  count() takes the
-// test of one's entries in steps of kScan, first() then gives the place of a step's first one in this wave.
+// test of one's entries in steps of kScan, place() after scan() gives where a picked one comes.
 struct Picked {
   uint16_t (*of)[kScan / 64];  // [kSteps][waves]: picked, then picked before
   uint32_t* part;
@@ -262,7 +262,9 @@ __global__ __launch_bounds__(kScan) void release_one(Geo g, ReleaseArgs a) {
 #pragma unroll 8
   for (int b = threadIdx.x; b < g.n_blocks; b += kScan) left[b] = a.shared_in[b];
   __syncthreads();
-  // (few rows end at a time: a wave takes one after the other of those, neighbours go to different waves)
+  // (a wave takes one after the other of the rows that end, neighbours go to different waves: right for few or long ones, 4
+  // of 64 rows of up to 250 entries 8 us from Python and all 64 11.  Each costs a round trip to memory however short it
+  // is: all of 1,500 rows of up to 4 entries 73 us, 40 of them 9; the kernels of a phase each take 9,000 such rows in 16.)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int r0 = 0; r0 < a.n_rows; r0 += kScan) {
     const int r = r0 + lane * (kScan / 64) + wave, len = r < a.n_rows ? a.len_in[r] : 0;
@@ -527,6 +529,9 @@ __global__ __launch_bounds__(kScan) void compact_one(Geo g, CompactArgs a) {
 // A workgroup's step: 16 KiB of a pair of blocks in one layer, four loads of a thread on their way at once (its
 // registers are plain vectors and filled without a condition: what may be missing would go through LDS, one by one).
 // Stores past the caches: 900 blocks of 131 KB 51 -> 47 us (5.1 TB/s), 800 of 66 KB in two layers 47 -> 40; eight loads 52 us.
+// (A streaming kernel reaches 6.2 TB/s.  An 8-bit block is 16 bytes a head longer than whole steps, so its last step copies next to
+// nothing: 8 heads of 16 tokens of 128 channels are 2,056 vectors, two steps and 8 vectors.)  Pairs that are left out are read and
+// passed over one by one: a list of 524,288 for 5 layers with 20 pairs takes 314 us, one of 32,768 22, the 20 alone 3.5 (from Python).
 constexpr int kPiece = 4 * kThreads;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
