@@ -590,7 +590,7 @@ def test_a_context_goes_on_with_fewer_blocks(codes):
         torch.cuda.synchronize()
         free = torch.cuda.mem_get_info()[0]
         ctx.wf_kv_ctx_set_blocks(keep)
-        assert torch.cuda.mem_get_info()[0] == free
+        assert abs(torch.cuda.mem_get_info()[0] - free) < 64 << 20      # (a context's work areas are 272 MiB)
         assert (ctx.n_blocks, ctx.cache_bytes) == (keep, new.cache_bytes)
         g = torch.Generator(device=DEV)
         g.manual_seed(2)
